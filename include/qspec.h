@@ -332,6 +332,95 @@ int qspec_kv_overwrite(const void* kv_verify_f16, const int32_t* n_accept, const
                        int B, int gamma, int D, int S, void* cache_f16, void* stream);
 
 /*
+ * Key/value cache held in 4 bits (paper Sec. 3.1: draft and verify pass share one cache, Sec. 4.1: 4-bit codes with
+ * fp16 scales; the paper keeps the cache itself in fp16, this form is the library's).  A token's key (after rotation)
+ * or value of one head, x[0 .. D-1] in fp16, is stored as
+ *   low = min x (a zero is +0),  step = fp16((max x - low) / 15),  code = clamp(rne((x - low) / step), 0, 15)   (step 0: codes 0)
+ * with the quotient decided exactly; it stands for code * step + low.  step and low are fp16.
+ *   cache   n_pages pages of qspec_kv4_page_bytes bytes.  A page holds page_size tokens (a power of two, 16 or more)
+ *           of every key/value head; per head, page_size * (D + 8) bytes:
+ *             page_size rows of D/2 bytes       key codes, 32-bit word w of a row: features 8w .. 8w+7
+ *             page_size / 16 tiles of 8 D bytes value codes, word w (features 8w .. 8w+7) of token t of the tile
+ *                                               at word 16 w + t
+ *             page_size rows of four fp16       key step, key low, value step, value low
+ *           with the nibble order of a weight word in every word.  D is 64 or 128.
+ *   page_table  int32 [B, max_pages]: token t of sequence b lies in row t % page_size of page
+ *           page_table[b][t / page_size].  An entry outside [0, n_pages) is a page that is not there: nothing is
+ *           written to it, and its tokens are not seen.  NULL: sequence b owns pages b * max_pages .. (n_pages >= B *
+ *           max_pages then).  A sequence holds up to max_pages * page_size tokens, 2^30 at most.
+ *   pos     int32 [B], the position of each sequence's first row of the call: row j (0 .. T-1) of sequence b stands
+ *           at position pos[b] + j.  T = 1 in a draft step, gamma + 1 in a verify pass, the prompt's length at its
+ *           start.  Rows outside [0, max_pages * page_size) have no place in the cache (pos[b] <= -T: an idle
+ *           sequence of a padded batch).
+ * The verify pass appends at the positions that the draft pass wrote, which overwrites them (paper Sec. 3.1, "KV Cache
+ * Overwriting"): rows behind the accepted ones are not seen until they are written again.
+ */
+size_t qspec_kv4_page_bytes(int Hkv, int D, int page_size);
+
+/*
+ * Rotary positions on queries and keys, and the append of keys and values to the 4-bit cache: what stands between
+ * the qkv product and the attention.  Feature pairs (a, b) of a head at position p become
+ *   (mscale (a cos t - b sin t), mscale (b cos t + a sin t)),  t = p * inv_freq[i],
+ * evaluated in binary64 and rounded once to fp16; features from `rot` on are not touched.  Pair i is (i, i + rot/2)
+ * (interleaved = 0) or (2i, 2i + 1) (interleaved = 1).  Scaling for long contexts is a matter of inv_freq and mscale.
+ *   qkv_f16   fp16 [B, T, (Hq + 2 Hkv) D]: query heads, key heads, value heads (as qspec_gemm_w4a16 writes them for the
+ *             merged weight);  inv_freq  binary64 [rot/2], 16-byte aligned, may be NULL for rot = 0;
+ *   0 <= rot <= D, a multiple of 16;  mscale > 0, finite;
+ *   q_f16     out, fp16 [B, T, Hq, D];  cache  in/out.  Rows that have no place in the cache are not stored; their
+ *             queries are written all the same.  Two rows of a call with the same place (pages shared by
+ *             two sequences): either may be the one that stays.
+ */
+int qspec_rope_kv4_append(const void* qkv_f16, const double* inv_freq, const int32_t* pos, const int32_t* page_table,
+                          int B, int T, int Hq, int Hkv, int D, int rot, int interleaved, float mscale,
+                          int page_size, int max_pages, int n_pages, void* q_f16, void* cache, void* stream);
+
+/* Values of rows pos[b] .. pos[b] + T - 1 of the cache: k_f16, v_f16 out, fp16 [B, T, Hkv, D] (code * step + low in
+ * binary32, then rounded and held to fp16's finite range); zeros for rows that have no place in it. */
+int qspec_kv4_read(const void* cache, const int32_t* pos, const int32_t* page_table, int B, int T, int Hkv, int D,
+                   int page_size, int max_pages, int n_pages, void* k_f16, void* v_f16, void* stream);
+
+/*
+ * Attention over the 4-bit cache, on the values it stands for:
+ *   out[b, j, h] = sum_t softmax_t(scale * q[b, j, h] . k[b, t, h / G]) v[b, t, h / G],   G = Hq / Hkv,
+ * over the tokens t that are in the cache with t <= p = pos[b] + j and, if window > 0, t > p - window or t < sinks (the
+ * window counts p itself).  A row that sees nothing gets zeros.  What stands in rows that no row of
+ * the same sequence sees does not matter.  fp32 sums; the weights enter the second product in fp16.
+ *   q_f16   fp16 [B, T, Hq, D], e.g. from qspec_rope_kv4_append, whose rows of the same call are seen;
+ *   1e-10 <= scale <= 1e10;  window >= 0 (0: none);  sinks >= 0 (0 without a window);
+ *   out_f16 out, fp16 [B, T, Hq, D];
+ *   workspace  qspec_attn_kv4_workspace_bytes(...) bytes; the workspace rule at qspec_workspace_bytes holds, and one
+ *           workspace may serve these calls and the products in turn.
+ */
+size_t qspec_attn_kv4_workspace_bytes(int B, int T, int Hq, int Hkv, int D);
+int qspec_attn_kv4(const void* q_f16, const void* cache, const int32_t* pos, const int32_t* page_table,
+                   int B, int T, int Hq, int Hkv, int D, int page_size, int max_pages, int n_pages,
+                   float scale, int window, int sinks, void* out_f16,
+                   void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Sampling from given random numbers, for decoding that is not greedy (paper Sec. 3.1 decodes greedily; the walk over
+ * the drafts is the same).  The tokens of a row are ordered by falling logit, the lowest id first among equals, and
+ * weigh w = exp((logit - max) / temperature), in binary64.  top_k keeps the first top_k of them, min_p those with w >=
+ * min_p, top_p the shortest beginning of what is left that holds top_p of its mass, one token at least.  The row's token is the first whose
+ * running mass exceeds u times the mass kept.
+ *   logits_f16   fp16 [B, gamma+1, V], 16-byte aligned;  u  fp32 [B, gamma+1], in [0, 1) (held to that range);
+ *   temperature, top_p, min_p  fp32 [B] and top_k int32 [B], one per sequence; each may be NULL (1, 1, 0, 0).
+ *                temperature <= 0: the row's top-1.  top_k <= 0, top_p >= 1, min_p <= 0: no limit.
+ *   Logits of -inf and NaN are never chosen; a row of nothing else gets token -1.  A row with +inf chooses among those.
+ *   draft_tokens NULL: out_tokens[b, j] is the token of row j (gamma = 0: one row a sequence, a draft step), n_accept and
+ *                workspace are not used and may be NULL.
+ *                int32 [B, gamma], gamma >= 1: the verify pass.  Draft j is accepted exactly when every earlier draft was
+ *                and it equals the token of row j; n_accept and out_tokens as in qspec_greedy_accept.  (A draft step
+ *                that used the same u for its token agrees with this the more often the closer the distributions are.)
+ *   workspace    qspec_sample_workspace_bytes(B, gamma, V) bytes of scratch, 16-byte aligned, nothing to clear.
+ * 4-byte arrays need 4-byte alignment only.  B >= 1, gamma >= 0, 1 <= V <= 2097152, B * (gamma + 1) <= 65535.
+ */
+size_t qspec_sample_workspace_bytes(int B, int gamma, int V);
+int qspec_sample(const void* logits_f16, const float* u, const float* temperature, const int32_t* top_k,
+                 const float* top_p, const float* min_p, const int32_t* draft_tokens, int B, int gamma, int V,
+                 int32_t* n_accept, int32_t* out_tokens, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
  * Debug entry (benchmark A/B and tests): force the kernel plan the GEMM entry points
  * and qspec_workspace_bytes use, instead of the library's own choice.  `name` is one of
  *   "QSPEC_KERNEL"            value "generic": untiled reference kernels for M > 32, in both modes

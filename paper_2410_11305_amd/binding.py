@@ -24,6 +24,8 @@ EXPORTS = (
     "qspec_reorder_quant", "qspec_debug_set_plan",
     "qspec_gemm_w4a16_noalloc", "qspec_mlp_draft", "qspec_mlp_draft_workspace_bytes",
     "qspec_w4a4_takes_wide", "qspec_quant_act_wide", "qspec_gemm_w4a4_wide",
+    "qspec_kv4_page_bytes", "qspec_rope_kv4_append", "qspec_kv4_read", "qspec_attn_kv4_workspace_bytes", "qspec_attn_kv4",
+    "qspec_sample_workspace_bytes", "qspec_sample",
 )
 
 
@@ -95,6 +97,20 @@ def lib() -> ctypes.CDLL:
     L.qspec_mlp_draft_workspace_bytes.argtypes = [ci, ci, ci, ci]
     L.qspec_mlp_draft.restype = ci
     L.qspec_mlp_draft.argtypes = [vp, vp, vp, vp, ci, ci, ci, ci, vp, vp, vp, vp, vp, sz, vp, vp]
+    L.qspec_kv4_page_bytes.restype = sz
+    L.qspec_kv4_page_bytes.argtypes = [ci, ci, ci]
+    L.qspec_rope_kv4_append.restype = ci
+    L.qspec_rope_kv4_append.argtypes = [vp, vp, vp, vp, ci, ci, ci, ci, ci, ci, ci, ctypes.c_float, ci, ci, ci, vp, vp, vp]
+    L.qspec_kv4_read.restype = ci
+    L.qspec_kv4_read.argtypes = [vp, vp, vp, ci, ci, ci, ci, ci, ci, ci, vp, vp, vp]
+    L.qspec_attn_kv4_workspace_bytes.restype = sz
+    L.qspec_attn_kv4_workspace_bytes.argtypes = [ci, ci, ci, ci, ci]
+    L.qspec_attn_kv4.restype = ci
+    L.qspec_attn_kv4.argtypes = [vp, vp, vp, vp, ci, ci, ci, ci, ci, ci, ci, ci, ctypes.c_float, ci, ci, vp, vp, sz, vp]
+    L.qspec_sample_workspace_bytes.restype = sz
+    L.qspec_sample_workspace_bytes.argtypes = [ci, ci, ci]
+    L.qspec_sample.restype = ci
+    L.qspec_sample.argtypes = [vp, vp, vp, vp, vp, vp, vp, ci, ci, ci, vp, vp, vp, sz, vp]
     L.qspec_debug_set_plan.restype = ci
     L.qspec_debug_set_plan.argtypes = [ctypes.c_char_p, ctypes.c_char_p]
     _lib = L
@@ -436,3 +452,146 @@ def kv_overwrite(cache: torch.Tensor, kv_verify: torch.Tensor, n_accept: torch.T
                                     _dev(cache, torch.float16, "cache"), _stream()),
            "qspec_kv_overwrite")
     return cache
+
+
+# ---- the 4-bit key/value cache (layout: include/qspec.h), attention over it, sampling
+
+def _shaped(t: torch.Tensor, dtype, shape, device, name: str) -> int:
+    """_dev for a tensor whose sizes are given by the others: the kernels index by those sizes alone."""
+    if t.device != device:
+        raise ValueError(f"{name} must live on {device}, got {t.device}")
+    if t.shape != shape:
+        raise ValueError(f"{name} must have the shape {tuple(shape)}, got {tuple(t.shape)}")
+    return _dev(t, dtype, name)
+
+
+def _here(t: torch.Tensor, dtype, name: str) -> int:
+    """_dev for the tensor whose device is the call's: the launch goes to the current device's stream."""
+    p = _dev(t, dtype, name)
+    if t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name} lives on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
+    return p
+
+
+def kv4_page_bytes(Hkv: int, D: int, page_size: int) -> int:
+    return lib().qspec_kv4_page_bytes(Hkv, D, page_size)
+
+
+def alloc_kv4_cache(n_pages: int, Hkv: int, D: int, page_size: int) -> torch.Tensor:
+    """A cache of n_pages pages: uint8 [n_pages, kv4_page_bytes], zeroed (not that a row is read before it is written)."""
+    nbytes = kv4_page_bytes(Hkv, D, page_size)
+    if nbytes == 0:
+        raise QSpecError(ERR_SHAPE, "qspec_kv4_page_bytes")
+    return torch.zeros((n_pages, nbytes), dtype=torch.uint8, device="cuda")
+
+
+def _kv4(cache, pos, page_table, Hkv, D, page_size, where):
+    """(cache, pos, table pointers, B, max_pages, n_pages) of a call's cache."""
+    nbytes = kv4_page_bytes(Hkv, D, page_size)
+    if nbytes == 0:
+        raise QSpecError(ERR_SHAPE, where)
+    n_pages, B = cache.shape[0], pos.shape[0]
+    if B == 0 or n_pages == 0:
+        raise QSpecError(ERR_SHAPE, where)
+    device = cache.device
+    table, max_pages = None, n_pages // B
+    if page_table is not None:
+        max_pages = page_table.shape[-1]
+        table = _shaped(page_table, torch.int32, (B, max_pages), device, "page_table")
+    _here(cache, torch.uint8, "cache")
+    return (_shaped(cache, torch.uint8, (n_pages, nbytes), device, "cache"),
+            _shaped(pos, torch.int32, (B,), device, "pos"), table, B, max_pages, n_pages)
+
+
+def rope_kv4_append(qkv: torch.Tensor, inv_freq: torch.Tensor, pos: torch.Tensor, cache: torch.Tensor, Hq: int, Hkv: int,
+                    page_size: int, page_table: torch.Tensor = None, interleaved: bool = False, mscale: float = 1.0,
+                    q: torch.Tensor = None) -> torch.Tensor:
+    """qkv fp16 [B, T, (Hq + 2 Hkv) D], inv_freq float64 [rot/2] (rope.frequencies; None: no rotation), pos int32 [B], cache uint8
+    [pages, kv4_page_bytes] (updated in place), page_table int32 [B, max_pages] or None -> rotated queries fp16 [B, T, Hq, D]."""
+    B, T, width = qkv.shape
+    heads = Hq + 2 * Hkv
+    if heads < 1 or width % heads:
+        raise QSpecError(ERR_SHAPE, "qspec_rope_kv4_append")
+    D = width // heads
+    c, at, table, _, max_pages, n_pages = _kv4(cache, pos, page_table, Hkv, D, page_size, "qspec_rope_kv4_append")
+    x = _shaped(qkv, torch.float16, (pos.shape[0], T, width), cache.device, "qkv")
+    rot, freq = 0, None
+    if inv_freq is not None:
+        rot = 2 * inv_freq.numel()
+        freq = _shaped(inv_freq, torch.float64, (rot // 2,), cache.device, "inv_freq") if rot else None
+    if q is None:
+        q = torch.empty((B, T, Hq, D), dtype=torch.float16, device=cache.device)
+    _check(lib().qspec_rope_kv4_append(x, freq, at, table, B, T, Hq, Hkv, D, rot, int(bool(interleaved)), mscale, page_size, max_pages,
+                                       n_pages, _shaped(q, torch.float16, (B, T, Hq, D), cache.device, "q"), c, _stream()),
+           "qspec_rope_kv4_append")
+    return q
+
+
+def kv4_read(cache: torch.Tensor, pos: torch.Tensor, T: int, Hkv: int, D: int, page_size: int, page_table: torch.Tensor = None,
+             k: torch.Tensor = None, v: torch.Tensor = None):
+    """Values of rows pos[b] .. pos[b] + T - 1 of the cache: (k, v), fp16 [B, T, Hkv, D]; zeros for rows outside of it."""
+    c, at, table, B, max_pages, n_pages = _kv4(cache, pos, page_table, Hkv, D, page_size, "qspec_kv4_read")
+    if T < 1:
+        raise QSpecError(ERR_SHAPE, "qspec_kv4_read")
+    shape = (B, T, Hkv, D)
+    k = torch.empty(shape, dtype=torch.float16, device=cache.device) if k is None else k
+    v = torch.empty(shape, dtype=torch.float16, device=cache.device) if v is None else v
+    _check(lib().qspec_kv4_read(c, at, table, B, T, Hkv, D, page_size, max_pages, n_pages, _shaped(k, torch.float16, shape, cache.device, "k"),
+                                _shaped(v, torch.float16, shape, cache.device, "v"), _stream()), "qspec_kv4_read")
+    return k, v
+
+
+def attn_kv4_workspace_bytes(B: int, T: int, Hq: int, Hkv: int, D: int) -> int:
+    return lib().qspec_attn_kv4_workspace_bytes(B, T, Hq, Hkv, D)
+
+
+def attn_kv4(q: torch.Tensor, cache: torch.Tensor, pos: torch.Tensor, Hkv: int, page_size: int, page_table: torch.Tensor = None,
+             scale: float = None, window: int = 0, sinks: int = 0, out: torch.Tensor = None,
+             workspace: torch.Tensor = None) -> torch.Tensor:
+    """Attention of q fp16 [B, T, Hq, D] (rows at positions pos[b] ..) over the 4-bit cache -> fp16 [B, T, Hq, D].  scale: 1 / sqrt(D)
+    by default; window > 0: the last `window` tokens and the first `sinks`.  Hot loops pass out and a workspace."""
+    B, T, Hq, D = q.shape
+    c, at, table, _, max_pages, n_pages = _kv4(cache, pos, page_table, Hkv, D, page_size, "qspec_attn_kv4")
+    x = _shaped(q, torch.float16, (pos.shape[0], T, Hq, D), cache.device, "q")
+    if out is None:
+        out = torch.empty_like(q)
+    if workspace is None:
+        workspace = alloc_workspace(attn_kv4_workspace_bytes(B, T, Hq, Hkv, D))
+    _check(lib().qspec_attn_kv4(x, c, at, table, B, T, Hq, Hkv, D, page_size, max_pages, n_pages, D ** -0.5 if scale is None else scale,
+                                window, sinks, _shaped(out, torch.float16, q.shape, cache.device, "out"),
+                                _shaped(workspace, torch.uint8, (workspace.numel(),), cache.device, "workspace"), workspace.numel(), _stream()),
+           "qspec_attn_kv4")
+    return out
+
+
+def sample_workspace_bytes(B: int, gamma: int, V: int) -> int:
+    return lib().qspec_sample_workspace_bytes(B, gamma, V)
+
+
+def sample(logits: torch.Tensor, u: torch.Tensor, temperature: torch.Tensor = None, top_k: torch.Tensor = None,
+           top_p: torch.Tensor = None, min_p: torch.Tensor = None, draft: torch.Tensor = None, n_accept: torch.Tensor = None,
+           out_tokens: torch.Tensor = None, workspace: torch.Tensor = None):
+    """A token per row of logits fp16 [B, gamma+1, V] by the random numbers u fp32 [B, gamma+1]; temperature, top_p, min_p fp32 [B] and
+    top_k int32 [B], each optional.  Returns (None, tokens int32 [B, gamma+1]), or with draft int32 [B, gamma] the acceptance of the
+    drafts: (n_accept int32 [B], out_tokens int32 [B, gamma+1]), as greedy_accept does."""
+    B, rows, V = logits.shape
+    gamma, device = rows - 1, logits.device
+    x = _here(logits, torch.float16, "logits")
+    per = [None if t is None else _shaped(t, dtype, (B,), device, name)
+           for t, dtype, name in ((temperature, torch.float32, "temperature"), (top_k, torch.int32, "top_k"),
+                                  (top_p, torch.float32, "top_p"), (min_p, torch.float32, "min_p"))]
+    if out_tokens is None:
+        out_tokens = torch.empty((B, rows), dtype=torch.int32, device=device)
+    drafts = accepted = ws = None
+    nbytes = 0
+    if draft is not None:
+        if n_accept is None:
+            n_accept = torch.empty((B,), dtype=torch.int32, device=device)
+        if workspace is None:
+            workspace = torch.empty(max(sample_workspace_bytes(B, gamma, V), 16), dtype=torch.uint8, device=device)
+        drafts = _shaped(draft, torch.int32, (B, gamma), device, "draft")
+        accepted = _shaped(n_accept, torch.int32, (B,), device, "n_accept")
+        ws, nbytes = _shaped(workspace, torch.uint8, (workspace.numel(),), device, "workspace"), workspace.numel()
+    _check(lib().qspec_sample(x, _shaped(u, torch.float32, (B, rows), device, "u"), *per, drafts, B, gamma, V, accepted,
+                              _shaped(out_tokens, torch.int32, (B, rows), device, "out_tokens"), ws, nbytes, _stream()), "qspec_sample")
+    return (None if draft is None else n_accept), out_tokens

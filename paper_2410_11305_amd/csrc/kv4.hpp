@@ -1,0 +1,236 @@
+// Key/value cache held in 4 bits: its layout, rotary positions with the append to it, and reading it back.
+//
+// Quantisation, per token and head over its D features (asymmetric: the rotated keys of a token are far from
+// symmetric, and the extra fp16 per row is 3 % of it), everything that decides a code exact:
+//   low = min x, step = fp16((max x - low) / 15), code = clamp(rne((x - low) / step), 0, 15); step 0 gives codes 0
+// A value is code * step + low.
+//
+// A page holds P tokens of every key/value head; per head, one region of P (D + 8) bytes:
+//   keys    P rows of D/2 bytes, word w holding features 8w .. 8w+7
+//   values  P/16 tiles of 8 D bytes: word w (features 8w .. 8w+7) of token t of the tile at word w * 16 + t
+//   rows    P times {key step, key low, value step, value low}, fp16
+// Codes of a word stand in the order of nibble_pos.  Both products of the attention contract over what a lane can load
+// in 16 bytes: features of one token for q k^T, four tokens of one word for p v.
+#pragma once
+#include "common.hpp"
+#include "producers.hpp"
+#include "quant_act.hpp"
+
+namespace qspec {
+
+struct KvShape {
+  const int32_t* pos;        // [B]: position of each sequence's first row of this call
+  const int32_t* table;      // [B][max_pages], or null: sequence b holds pages b * max_pages ..
+  int T, Hkv, page_shift, max_pages, n_pages;
+};
+
+// 4-byte values that no launch in flight writes, at an address the whole wavefront shares: a scalar load
+typedef const __attribute__((address_space(4))) int32_t* scalar_i32_ptr;
+__device__ __forceinline__ int32_t scalar_load(const int32_t* p, size_t i) { return ((scalar_i32_ptr)(uintptr_t)p)[i]; }
+
+// Page of position at of sequence b, or -1 where there is none (positions outside the sequence's pages, table
+// entries outside the cache).
+__device__ __forceinline__ int kv_page(const KvShape& s, int b, long long at) {
+  if (at < 0 || (at >> s.page_shift) >= s.max_pages) return -1;
+  const size_t i = (size_t)b * s.max_pages + (size_t)(at >> s.page_shift);
+  const int page = s.table != nullptr ? s.table[i] : (int)i;
+  return page >= 0 && page < s.n_pages ? page : -1;
+}
+
+// float64 to fp16 in one rounding: to float32 with the last bit set where that is inexact (round to odd: 13 bits more
+// than fp16 has are enough), then to nearest even.
+__device__ inline _Float16 half_of_f64(double v) {
+  float f = (float)v;
+  const double back = (double)f;
+  uint32_t bits = __builtin_bit_cast(uint32_t, f);
+  if (back != v && (bits & 1u) == 0) bits += fabs(back) < fabs(v) ? 1u : 0xFFFFFFFFu;
+  return (_Float16)(back != v ? __builtin_bit_cast(float, bits) : f);
+}
+
+// cos and sin of `turns` whole turns, to a few units in the last place of binary64: the nearest quarter turn off, then
+// the Taylor series on +-pi/4 (the first terms left out are below 2^-58).
+__device__ inline void cos_sin_turns(double turns, double& c, double& s) {
+  const double r = turns - rint(turns);
+  const double quarter = rint(r * 4.0);
+  const double y = fma(quarter, -0.25, r) * 6.283185307179586477;
+  const double z = y * y;
+  double ps = 1.0 / 355687428096000.0;
+  ps = fma(ps, z, -1.0 / 1307674368000.0);
+  ps = fma(ps, z, 1.0 / 6227020800.0);
+  ps = fma(ps, z, -1.0 / 39916800.0);
+  ps = fma(ps, z, 1.0 / 362880.0);
+  ps = fma(ps, z, -1.0 / 5040.0);
+  ps = fma(ps, z, 1.0 / 120.0);
+  ps = fma(ps, z, -1.0 / 6.0);
+  const double sy = fma(ps * z, y, y);
+  double pc = 1.0 / 20922789888000.0;
+  pc = fma(pc, z, -1.0 / 87178291200.0);
+  pc = fma(pc, z, 1.0 / 479001600.0);
+  pc = fma(pc, z, -1.0 / 3628800.0);
+  pc = fma(pc, z, 1.0 / 40320.0);
+  pc = fma(pc, z, -1.0 / 720.0);
+  pc = fma(pc, z, 1.0 / 24.0);
+  pc = fma(pc, z, -0.5);
+  const double cy = fma(pc, z, 1.0);
+  const int q = (int)quarter & 3;
+  const double u = (q & 1) ? sy : cy, v = (q & 1) ? cy : sy;
+  c = (q == 1 || q == 2) ? -u : u;
+  s = (q & 2) ? -v : v;
+}
+
+struct AppendArgs {
+  KvShape kv;
+  const uint4* qkv;          // fp16 [B*T][(Hq + 2 Hkv) D]
+  const double* inv_freq;    // [rot/2], radians per position
+  uint4* q;                  // fp16 [B*T][Hq D]
+  uint8_t* cache;
+  int Hq, rot, interleaved;
+  float mscale;
+};
+
+// Largest and smallest of a head's values, over the row of LANES = D / 8 lanes that holds it.
+template <int LANES>
+__device__ inline float row_max(float a) {
+  a = fmaxf(a, dpp_f32<0xB1>(a));
+  a = fmaxf(a, dpp_f32<0x4E>(a));
+  a = fmaxf(a, dpp_f32<0x141>(a));
+  if (LANES == 16) a = fmaxf(a, dpp_f32<0x140>(a));
+  return a;
+}
+
+// Code word of 8 values of a head, and the head's step and minimum.  The quotient is formed in binary64, where the difference of two fp16 values
+// is exact and a quotient that is not itself half way between two integers is far enough from it to stay on its side.
+template <int LANES>
+__device__ inline uint32_t kv_code_word(const float (&v)[8], _Float16& step, _Float16& low) {
+  float hi = v[0], lo = v[0];
+#pragma unroll
+  for (int e = 1; e < 8; ++e) { hi = fmaxf(hi, v[e]); lo = fminf(lo, v[e]); }
+  hi = row_max<LANES>(hi);
+  lo = -row_max<LANES>(-lo) + 0.0f;                         // (a zero is +0, here and in the step)
+  hi += 0.0f;
+  low = (_Float16)lo;                                       // exact: one of the values
+  step = half_of_f64(((double)hi - (double)lo) / 15.0);
+  const double s = (double)(float)step;
+  if (!(s > 0.0)) return 0u;
+  double y = __builtin_amdgcn_rcp(s);
+  y = fma(fma(-s, y, 1.0), y, y);
+  y = fma(fma(-s, y, 1.0), y, y);
+  uint32_t w = 0;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const double d = (double)v[e] - (double)lo;
+    double t = d * y;
+    t = fma(fma(-t, s, d), y, t);
+    const int code = min(max((int)rint(t), 0), 15);
+    w |= (uint32_t)code << (4 * nibble_pos(e));
+  }
+  return w;
+}
+
+// grid (B*T, parts of the heads): a workgroup takes one token and 256 / (D/8) of its Hq + 2 Hkv heads, a row of D/8
+// lanes a head, 8 features a lane.
+template <int D>
+__global__ __launch_bounds__(256) void rope_kv4_append_kernel(AppendArgs p) {
+  constexpr int LANES = D / 8, PER = 256 / LANES;
+  __shared__ double2 turn[D / 2];                           // cos, sin of each pair's angle, times mscale
+  const int token = blockIdx.x, b = token / p.kv.T, j = token - b * p.kv.T;
+  const int l = threadIdx.x & (LANES - 1);
+  const int heads = p.Hq + 2 * p.kv.Hkv;
+  const int head = blockIdx.y * PER + (int)threadIdx.x / LANES;
+  const bool live = head < heads;
+  const uint4* const row = p.qkv + ((size_t)token * heads + min(head, heads - 1)) * LANES;
+  const int half = p.rot >> 1;
+  const bool turns = 8 * l < p.rot && head < p.Hq + p.kv.Hkv;
+  const uint4 mine = row[l];
+  uint4 other = mine;
+  const bool upper = 8 * l >= half;
+  if (turns && !p.interleaved) other = row[upper ? l - (half >> 3) : l + (half >> 3)];
+  const long long at = (long long)p.kv.pos[b] + j;
+  if ((int)threadIdx.x < half) {
+    double c, s;
+    cos_sin_turns((double)at * (p.inv_freq[threadIdx.x] * 0.15915494309189533577), c, s);
+    turn[threadIdx.x] = double2{c * (double)p.mscale, s * (double)p.mscale};
+  }
+  __syncthreads();
+  const v8h x = __builtin_bit_cast(v8h, mine), z = __builtin_bit_cast(v8h, other);
+  v8h h = x;
+  if (turns) {
+    if (p.interleaved) {
+#pragma unroll
+      for (int e = 0; e < 8; e += 2) {
+        const double2 t = turn[4 * l + e / 2];
+        const double a = (double)(float)x[e], c = (double)(float)x[e + 1];
+        h[e] = half_of_f64(a * t.x - c * t.y);
+        h[e + 1] = half_of_f64(c * t.x + a * t.y);
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const double2 t = turn[8 * l + e - (upper ? half : 0)];
+        const double a = (double)(float)x[e], c = (double)(float)z[e];
+        h[e] = half_of_f64(a * t.x + (upper ? c : -c) * t.y);
+      }
+    }
+  }
+  if (live && head < p.Hq) p.q[((size_t)token * p.Hq + head) * LANES + l] = __builtin_bit_cast(uint4, h);
+  float v[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] = (float)h[e];
+  _Float16 step, low;
+  const uint32_t word = kv_code_word<LANES>(v, step, low);  // (every lane: the folds)
+  const int page = kv_page(p.kv, b, at);
+  if (!live || head < p.Hq || page < 0) return;
+  const bool value = head >= p.Hq + p.kv.Hkv;
+  const int kv_head = head - p.Hq - (value ? p.kv.Hkv : 0);
+  const int P = 1 << p.kv.page_shift, slot = (int)(at & (P - 1));
+  uint8_t* const region = p.cache + ((size_t)page * p.kv.Hkv + kv_head) * ((size_t)P * (D + 8));
+  uint32_t* const place = value ? reinterpret_cast<uint32_t*>(region + (size_t)P * (D / 2) + (size_t)(slot >> 4) * (8 * D)) + l * 16 + (slot & 15)
+                                : reinterpret_cast<uint32_t*>(region + (size_t)slot * (D / 2)) + l;
+  *place = word;
+  if (l == 0) *reinterpret_cast<v2h*>(region + (size_t)P * D + (size_t)slot * 8 + (value ? 4 : 0)) = v2h{step, low};
+}
+
+struct KvReadArgs {
+  KvShape kv;
+  const uint8_t* cache;
+  uint4* k;                  // fp16 [B*T][Hkv D]
+  uint4* v;
+};
+
+// 8 codes of a word times step plus low, each rounded once to binary32 and once to fp16.  (A step that was rounded up can
+// carry the 15th code of a row that fills fp16's range past its end: the largest finite value then.)
+__device__ inline v8h kv_values(uint32_t w, _Float16 step, _Float16 low) {
+  v8h h;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const float x = rounded_f32(fmaf((float)((w >> (4 * nibble_pos(e))) & 15u), (float)step, (float)low));
+    h[e] = (_Float16)fminf(fmaxf(x, -65504.0f), 65504.0f);
+  }
+  return h;
+}
+
+// grid (B*T, parts of Hkv D / 8 words of a token).  Rows without a place in the cache come back as zeros.
+template <int D>
+__global__ __launch_bounds__(256) void kv4_read_kernel(KvReadArgs p) {
+  constexpr int LANES = D / 8;
+  const int token = blockIdx.x, b = token / p.kv.T;
+  const int i = blockIdx.y * 256 + threadIdx.x, head = i / LANES, w = i & (LANES - 1);
+  if (head >= p.kv.Hkv) return;
+  const long long at = (long long)p.kv.pos[b] + (token - b * p.kv.T);
+  const int page = kv_page(p.kv, b, at);
+  const size_t o = ((size_t)token * p.kv.Hkv + head) * LANES + w;
+  if (page < 0) {
+    p.k[o] = p.v[o] = uint4{0u, 0u, 0u, 0u};
+    return;
+  }
+  const int P = 1 << p.kv.page_shift, slot = (int)(at & (P - 1));
+  const uint8_t* const region = p.cache + ((size_t)page * p.kv.Hkv + head) * ((size_t)P * (D + 8));
+  typedef _Float16 v4h __attribute__((ext_vector_type(4)));
+  const v4h par = *reinterpret_cast<const v4h*>(region + (size_t)P * D + (size_t)slot * 8);
+  const uint32_t kw = reinterpret_cast<const uint32_t*>(region + (size_t)slot * (D / 2))[w];
+  const uint32_t vw = reinterpret_cast<const uint32_t*>(region + (size_t)P * (D / 2) + (size_t)(slot >> 4) * (8 * D))[w * 16 + (slot & 15)];
+  p.k[o] = __builtin_bit_cast(uint4, kv_values(kw, par.x, par.y));
+  p.v[o] = __builtin_bit_cast(uint4, kv_values(vw, par.z, par.w));
+}
+
+}  // namespace qspec

@@ -11,16 +11,19 @@
 #include <tuple>
 
 #include "accept.hpp"
+#include "attn_kv4.hpp"
 #include "common.hpp"
 #include "gemm_generic.hpp"
 #include "gemm_stream.hpp"
 #include "gemm_tile16.hpp"
 #include "gemm_tile16w2.hpp"
 #include "gemm_tile4.hpp"
+#include "kv4.hpp"
 #include "mlp_chain.hpp"
 #include "pack.hpp"
 #include "producers.hpp"
 #include "quant_act.hpp"
+#include "sample.hpp"
 
 using namespace qspec;
 
@@ -806,6 +809,58 @@ inline int check_accept_shape(int B, int gamma, int V) {
   return QSPEC_OK;
 }
 
+// ---------------------------------------------------------------- the 4-bit key/value cache
+inline int log2_exact(int v) { return __builtin_ctz((unsigned)v); }
+
+// Shapes that the cache and its readers take.  Positions, table indexes and steps stay in 32 bits, pages below 2 GiB; the
+// cache as a whole may be larger.
+int check_kv_cache(int Hkv, int D, int page_size) {
+  if (D != 64 && D != 128) return QSPEC_ERR_SHAPE;
+  if (Hkv < 1 || page_size < 16 || (page_size & (page_size - 1)) != 0) return QSPEC_ERR_SHAPE;
+  if ((long long)Hkv * page_size * (D + 8) >= 0x7fffffffLL) return QSPEC_ERR_SHAPE;
+  return QSPEC_OK;
+}
+
+int check_kv(const int32_t* page_table, int B, int T, int Hkv, int D, int page_size, int max_pages, int n_pages) {
+  if (int st = check_kv_cache(Hkv, D, page_size)) return st;
+  if (B < 1 || T < 1 || max_pages < 1 || n_pages < 1) return QSPEC_ERR_SHAPE;
+  if ((long long)B * T > 0x7fffffffLL || (long long)max_pages * page_size > (1LL << 30)) return QSPEC_ERR_SHAPE;
+  if (T > (1 << 20)) return QSPEC_ERR_SHAPE;
+  if (!page_table && (long long)B * max_pages > n_pages) return QSPEC_ERR_SHAPE;    // sequence b owns pages b * max_pages ..
+  return QSPEC_OK;
+}
+
+inline KvShape kv_shape(const int32_t* pos, const int32_t* page_table, int T, int Hkv, int page_size, int max_pages, int n_pages) {
+  return KvShape{pos, page_table, T, Hkv, log2_exact(page_size), max_pages, n_pages};
+}
+
+// Blocks of 16 rows that a wavefront of the attention carries: as many as the rows of a sequence and key/value head fill, 4 at most.
+inline int attn_row_blocks(int T, int G) { return (long long)T * G <= 16 ? 1 : (long long)T * G <= 32 ? 2 : 4; }
+
+int check_attn(int B, int T, int Hq, int Hkv, int D) {
+  if (D != 64 && D != 128) return QSPEC_ERR_SHAPE;
+  if (B < 1 || T < 1 || T > (1 << 20) || Hkv < 1 || Hq < Hkv || Hq % Hkv != 0) return QSPEC_ERR_SHAPE;
+  if ((long long)B * T * Hq * D * 2 >= 0x7fffffffLL) return QSPEC_ERR_SHAPE;
+  return QSPEC_OK;
+}
+
+size_t attn_workspace_bytes(int T, int G, int D) {
+  return kAttnTicketBytes + (size_t)2 * kAttnMaxWorkgroups * 16 * attn_row_blocks(T, G) * attn_part_floats(D) * sizeof(float);
+}
+
+template <int D>
+void launch_attn(const AttnArgs& a, int nb, hipStream_t s) {
+  if (nb == 1) launch_kernel((attn_kv4_kernel<D, 1>), dim3(kAttnMaxWorkgroups), dim3(kAttnThreads), 0, s, a);
+  else if (nb == 2) launch_kernel((attn_kv4_kernel<D, 2>), dim3(kAttnMaxWorkgroups / 2), dim3(kAttnThreads), 0, s, a);
+  else launch_kernel((attn_kv4_kernel<D, 4>), dim3(kAttnMaxWorkgroups / 2), dim3(kAttnThreads), 0, s, a);
+}
+
+int check_sample_shape(int B, int gamma, int V) {
+  if (B < 1 || gamma < 0 || V < 1 || V > kSampleMaxV) return QSPEC_ERR_SHAPE;
+  if ((long long)B * ((long long)gamma + 1) > 65535) return QSPEC_ERR_SHAPE;
+  return QSPEC_OK;
+}
+
 // ---------------------------------------------------------------- the three products
 int check_gemm(const void* packed, const void* act, const float* sa, int M, int N, int K, int group, void* y_f16) {
   if (!packed || !act || !y_f16) return QSPEC_ERR_NULL;
@@ -1164,6 +1219,99 @@ int qspec_kv_overwrite(const void* kv_verify_f16, const int32_t* n_accept, const
   if (int st = check_device()) return st;
   KvArgs a{static_cast<const uint4*>(kv_verify_f16), static_cast<uint4*>(cache_f16), n_accept, pos, gamma, D / 8, S};
   launch_kernel(kv_overwrite_kernel, dim3(B * (gamma + 1)), dim3(256), 0, static_cast<hipStream_t>(stream), a);
+  return launch_status();
+}
+
+size_t qspec_kv4_page_bytes(int Hkv, int D, int page_size) {
+  return check_kv_cache(Hkv, D, page_size) == QSPEC_OK ? (size_t)Hkv * page_size * (D + 8) : 0;
+}
+
+int qspec_rope_kv4_append(const void* qkv_f16, const double* inv_freq, const int32_t* pos, const int32_t* page_table,
+                          int B, int T, int Hq, int Hkv, int D, int rot, int interleaved, float mscale,
+                          int page_size, int max_pages, int n_pages, void* q_f16, void* cache, void* stream) {
+  if (!qkv_f16 || !pos || !q_f16 || !cache || (rot > 0 && !inv_freq)) return QSPEC_ERR_NULL;
+  if (int st = check_kv(page_table, B, T, Hkv, D, page_size, max_pages, n_pages)) return st;
+  if (Hq < 1 || rot < 0 || rot > D || rot % 16 != 0 || (interleaved != 0 && interleaved != 1)) return QSPEC_ERR_SHAPE;
+  if (!(mscale > 0.0f) || !(mscale <= 3.0e38f)) return QSPEC_ERR_SHAPE;
+  const long long heads = (long long)Hq + 2LL * Hkv;
+  if ((long long)B * T * heads * D * 2 >= 0x7fffffffLL) return QSPEC_ERR_SHAPE;
+  if (misaligned(qkv_f16) || misaligned(q_f16) || misaligned(cache) || misaligned(inv_freq) || misaligned4(pos) || misaligned4(page_table))
+    return QSPEC_ERR_ALIGN;
+  if (int st = check_device()) return st;
+  AppendArgs a{kv_shape(pos, page_table, T, Hkv, page_size, max_pages, n_pages), static_cast<const uint4*>(qkv_f16), inv_freq,
+               static_cast<uint4*>(q_f16), static_cast<uint8_t*>(cache), Hq, rot, interleaved, mscale};
+  const dim3 grid(B * T, blocks_for((size_t)heads * (D / 8), 256));
+  if (D == 128) launch_kernel(rope_kv4_append_kernel<128>, grid, dim3(256), 0, static_cast<hipStream_t>(stream), a);
+  else launch_kernel(rope_kv4_append_kernel<64>, grid, dim3(256), 0, static_cast<hipStream_t>(stream), a);
+  return launch_status();
+}
+
+int qspec_kv4_read(const void* cache, const int32_t* pos, const int32_t* page_table, int B, int T, int Hkv, int D,
+                   int page_size, int max_pages, int n_pages, void* k_f16, void* v_f16, void* stream) {
+  if (!cache || !pos || !k_f16 || !v_f16) return QSPEC_ERR_NULL;
+  if (int st = check_kv(page_table, B, T, Hkv, D, page_size, max_pages, n_pages)) return st;
+  if ((long long)B * T * Hkv * D * 2 >= 0x7fffffffLL) return QSPEC_ERR_SHAPE;
+  if (misaligned(cache) || misaligned(k_f16) || misaligned(v_f16) || misaligned4(pos) || misaligned4(page_table)) return QSPEC_ERR_ALIGN;
+  if (int st = check_device()) return st;
+  KvReadArgs a{kv_shape(pos, page_table, T, Hkv, page_size, max_pages, n_pages), static_cast<const uint8_t*>(cache),
+               static_cast<uint4*>(k_f16), static_cast<uint4*>(v_f16)};
+  const dim3 grid(B * T, blocks_for((size_t)Hkv * (D / 8), 256));
+  if (D == 128) launch_kernel(kv4_read_kernel<128>, grid, dim3(256), 0, static_cast<hipStream_t>(stream), a);
+  else launch_kernel(kv4_read_kernel<64>, grid, dim3(256), 0, static_cast<hipStream_t>(stream), a);
+  return launch_status();
+}
+
+size_t qspec_attn_kv4_workspace_bytes(int B, int T, int Hq, int Hkv, int D) {
+  return check_attn(B, T, Hq, Hkv, D) == QSPEC_OK ? attn_workspace_bytes(T, Hq / Hkv, D) : 0;
+}
+
+int qspec_attn_kv4(const void* q_f16, const void* cache, const int32_t* pos, const int32_t* page_table,
+                   int B, int T, int Hq, int Hkv, int D, int page_size, int max_pages, int n_pages,
+                   float scale, int window, int sinks, void* out_f16,
+                   void* workspace, size_t workspace_bytes, void* stream) {
+  if (!q_f16 || !cache || !pos || !out_f16 || !workspace) return QSPEC_ERR_NULL;
+  if (int st = check_attn(B, T, Hq, Hkv, D)) return st;
+  if (int st = check_kv(page_table, B, T, Hkv, D, page_size, max_pages, n_pages)) return st;
+  // (the bounds of the scale keep every score inside binary32, and off the reference of a row that has seen nothing)
+  if (!(scale >= 1e-10f) || !(scale <= 1e10f) || window < 0 || sinks < 0 || (window == 0 && sinks > 0)) return QSPEC_ERR_SHAPE;
+  if (misaligned(q_f16) || misaligned(cache) || misaligned(out_f16) || misaligned(workspace) || misaligned4(pos) || misaligned4(page_table))
+    return QSPEC_ERR_ALIGN;
+  const int G = Hq / Hkv, nb = attn_row_blocks(T, G);
+  if (workspace_bytes < attn_workspace_bytes(T, G, D)) return QSPEC_ERR_WORKSPACE;
+  const long long blocks = ((long long)T * G + 16 * nb - 1) / (16 * nb);
+  if (B * blocks > 0x7fffffffLL) return QSPEC_ERR_SHAPE;
+  if (int st = check_device()) return st;
+  AttnArgs a{kv_shape(pos, page_table, T, Hkv, page_size, max_pages, n_pages), static_cast<const uint16_t*>(q_f16),
+             static_cast<const uint8_t*>(cache), static_cast<uint16_t*>(out_f16), static_cast<unsigned*>(workspace),
+             reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + kAttnTicketBytes), B, Hq, G, (int)blocks,
+             window, sinks, scale * 1.44269504f};
+  if (D == 128) launch_attn<128>(a, nb, static_cast<hipStream_t>(stream));
+  else launch_attn<64>(a, nb, static_cast<hipStream_t>(stream));
+  return launch_status();
+}
+
+size_t qspec_sample_workspace_bytes(int B, int gamma, int V) {
+  return check_sample_shape(B, gamma, V) == QSPEC_OK ? (size_t)B * (gamma + 1) * sizeof(int32_t) : 0;
+}
+
+int qspec_sample(const void* logits_f16, const float* u, const float* temperature, const int32_t* top_k,
+                 const float* top_p, const float* min_p, const int32_t* draft_tokens, int B, int gamma, int V,
+                 int32_t* n_accept, int32_t* out_tokens, void* workspace, size_t workspace_bytes, void* stream) {
+  if (!logits_f16 || !u || !out_tokens || (draft_tokens && (!n_accept || !workspace))) return QSPEC_ERR_NULL;
+  if (int st = check_sample_shape(B, gamma, V)) return st;
+  if (draft_tokens && gamma == 0) return QSPEC_ERR_SHAPE;
+  if (misaligned(logits_f16) || misaligned4(u) || misaligned4(temperature) || misaligned4(top_k) || misaligned4(top_p) ||
+      misaligned4(min_p) || misaligned4(draft_tokens) || misaligned4(n_accept) || misaligned4(out_tokens) || misaligned(workspace))
+    return QSPEC_ERR_ALIGN;
+  if (draft_tokens && workspace_bytes < qspec_sample_workspace_bytes(B, gamma, V)) return QSPEC_ERR_WORKSPACE;
+  if (int st = check_device()) return st;
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  int32_t* const tokens = draft_tokens ? static_cast<int32_t*>(workspace) : out_tokens;
+  SampleArgs a{static_cast<const uint16_t*>(logits_f16), u, temperature, top_k, top_p, min_p, tokens, V, gamma + 1};
+  const dim3 grid(B * (gamma + 1));
+  if (V % 8 == 0) launch_kernel(sample_kernel<true>, grid, dim3(kSampleThreads), 0, s, a);
+  else launch_kernel(sample_kernel<false>, grid, dim3(kSampleThreads), 0, s, a);
+  if (draft_tokens) launch_kernel(accept_tokens_kernel, dim3(B), dim3(64), 0, s, AcceptTokensArgs{tokens, draft_tokens, n_accept, out_tokens, gamma});
   return launch_status();
 }
 

@@ -1,0 +1,192 @@
+"""Sampling from given random numbers, against the oracle: tokens have to be equal."""
+import math
+
+import numpy as np
+import pytest
+
+from oracle import sample_oracle as so
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def env():
+    import torch
+    from paper_2410_11305_amd import binding as B
+    assert torch.cuda.is_available()
+    B.lib()
+    return torch, B
+
+
+def dev(torch, a):
+    return None if a is None else torch.from_numpy(np.ascontiguousarray(a)).cuda()
+
+
+def run(env, logits, u, temperature=None, top_k=None, top_p=None, min_p=None, draft=None):
+    torch, B = env
+    f32 = lambda a: None if a is None else dev(torch, np.asarray(a, dtype=np.float32))
+    n, out = B.sample(dev(torch, logits), f32(u), f32(temperature), None if top_k is None else dev(torch, np.asarray(top_k, dtype=np.int32)),
+                      f32(top_p), f32(min_p), dev(torch, draft))
+    torch.cuda.synchronize()
+    return (None if n is None else n.cpu().numpy()), out.cpu().numpy()
+
+
+def want(logits, u, temperature=None, top_k=None, top_p=None, min_p=None):
+    Bn, rows, _ = logits.shape
+    one = lambda a, b, d: d if a is None else float(np.float32(a[b]))
+    return np.array([[so.sample(logits[b, j], float(np.float32(u[b][j])), one(temperature, b, 1.0), int(one(top_k, b, 0)), one(top_p, b, 1.0),
+                                one(min_p, b, 0.0)) for j in range(rows)] for b in range(Bn)])
+
+
+def params(rng, Bn):
+    t = np.where(rng.random(Bn) < 0.15, 0.0, rng.uniform(0.2, 2.0, Bn))
+    k = np.where(rng.random(Bn) < 0.5, 0, rng.integers(1, 60, Bn))
+    p = np.where(rng.random(Bn) < 0.4, 1.0, rng.uniform(0.05, 1.0, Bn))
+    m = np.where(rng.random(Bn) < 0.6, 0.0, rng.uniform(0.0, 0.3, Bn))
+    return dict(temperature=t, top_k=k, top_p=p, min_p=m)
+
+
+@pytest.mark.parametrize("Bn,rows,V", [(1, 1, 1), (2, 2, 7), (3, 1, 8), (5, 4, 1000), (4, 2, 4099), (2, 3, 8192), (2, 2, 8200), (3, 1, 32000), (1, 2, 65521),
+                                       (1, 1, 65528), (1, 1, 65536), (2, 1, 128256), (1, 1, 200003)])
+def test_tokens_match_the_oracle(env, Bn, rows, V):
+    rng = np.random.default_rng(V + Bn)
+    logits = (rng.standard_normal((Bn, rows, V)) * 2.5).astype(np.float16)
+    u, p = rng.random((Bn, rows)), params(rng, Bn)
+    assert (run(env, logits, u, **p)[1] == want(logits, u, **p)).all()
+    assert (run(env, logits, u)[1] == want(logits, u)).all()                     # no limits
+
+
+@pytest.mark.parametrize("seed", range(6))
+def test_many_small_rows_with_every_limit(env, seed):
+    """Few distinct logits: the limits fall inside runs of equal ones."""
+    rng = np.random.default_rng(seed)
+    Bn, rows, V = 64, 3, 203
+    logits = (rng.integers(-6, 7, (Bn, rows, V)) * (0.25 if seed % 2 else 1.0)).astype(np.float16)
+    if seed >= 3:
+        logits[rng.random(logits.shape) < 0.6] = -np.inf
+    u, p = rng.random((Bn, rows)), params(rng, Bn)
+    assert (run(env, logits, u, **p)[1] == want(logits, u, **p)).all()
+
+
+@pytest.mark.parametrize("V", [512, 70000])
+def test_equal_logits_walk_by_index(env, V):
+    """Everything weighs one, so the borders are exact: u picks the index, top_p a power of two cuts."""
+    logits = np.full((4, 2, V), -1.5, dtype=np.float16)
+    u = np.array([[0.0, 0.25], [0.5, 0.75], [0.25, 0.5], [1.0 - 2.0 ** -24, 0.5]])
+    got = run(env, logits, u, top_p=[1.0, 1.0, 0.5, 0.25])[1]
+    assert got.tolist() == [[0, V // 4], [V // 2, 3 * V // 4], [V // 8, V // 4], [V // 4 - 1, V // 8]]
+    assert run(env, logits, u, top_k=[1, 2, 8, V + 5])[1].tolist() == [[0, 0], [1, 1], [2, 4], [V - 1, V // 2]]
+
+
+def test_all_values_of_fp16(env):
+    """One token of every finite value, hot and cold, from both ends."""
+    bits = np.arange(65536, dtype=np.uint16)
+    row = bits.view(np.float16)[np.isfinite(bits.view(np.float16))]
+    rng = np.random.default_rng(1)
+    row = rng.permutation(row)
+    for t in (1e4, 30.0, 1.0, 0.01, 1e-30, np.inf):
+        u = rng.random((1, 40))
+        logits = np.broadcast_to(row, (1, 40, row.size)).copy()
+        assert (run(env, logits, u, temperature=[t])[1] == want(logits, u, temperature=[t])).all(), t
+
+
+def test_masked_rows_infinities_and_nan(env):
+    V = 100
+    logits = np.zeros((8, 1, V), dtype=np.float16)
+    logits[0] = -np.inf
+    logits[1] = np.nan
+    logits[2] = -np.inf; logits[2, 0, 77] = -65504.0
+    logits[3] = np.nan; logits[3, 0, 5] = -7.0; logits[3, 0, 9] = -7.0
+    logits[4, 0, 30] = logits[4, 0, 60] = np.inf
+    logits[5, 0, ::2] = -0.0
+    logits[6] = -np.inf; logits[6, 0, 99] = 65504.0; logits[6, 0, 0] = -65504.0
+    logits[7] = np.inf
+    u = np.full((8, 1), 0.6)
+    assert run(env, logits, u)[1].ravel().tolist() == [-1, -1, 77, 9, 60, 60, 99, 60]
+    assert run(env, logits, u, temperature=[0.0] * 8)[1].ravel().tolist() == [-1, -1, 77, 5, 30, 0, 99, 0]
+
+
+def test_parameters_out_of_range(env):
+    rng = np.random.default_rng(4)
+    logits = rng.standard_normal((8, 1, 300)).astype(np.float16)
+    top = int(np.argmax(logits[0, 0]))
+    logits[:] = logits[0]
+    order = np.argsort(-logits[0, 0].astype(np.float64), kind="stable")
+    got = run(env, logits, [[0.5], [0.5], [0.5], [0.999], [np.nan], [-3.0], [2.0], [0.5]],
+              temperature=[-1.0, np.nan, 1.0, 1.0, 1.0, 1.0, 1.0, 1.0], top_k=[0, 0, 0, -5, 3, 3, 3, 0], top_p=[1, 1, -0.5, np.nan, 1, 1, 1, 7.0],
+              min_p=[0, 0, 0, np.nan, 0, 0, 0, 5.0])[1].ravel().tolist()
+    plain = so.sample(logits[0, 0], float(np.float32(0.999)))
+    assert got == [top, top, top, plain, top, top, int(order[2]), top]
+
+
+@pytest.mark.parametrize("Bn,gamma,V", [(1, 1, 9), (16, 3, 1003), (5, 5, 32000), (2, 70, 50), (3, 63, 17), (3, 64, 17)])
+def test_drafts_are_accepted_as_far_as_they_agree(env, Bn, gamma, V):
+    rng = np.random.default_rng(gamma)
+    logits = (rng.standard_normal((Bn, gamma + 1, V)) * 2.0).astype(np.float16)
+    u, p = rng.random((Bn, gamma + 1)), params(rng, Bn)
+    tokens = want(logits, u, **p)
+    draft = tokens[:, :gamma].astype(np.int32).copy()
+    for b in range(Bn):
+        if b % 3:
+            at = rng.integers(0, gamma)
+            draft[b, at] = (draft[b, at] + 1) % V
+    n, out = run(env, logits, u, draft=draft, **p)
+    n_ref, out_ref = so.accept(tokens, draft)
+    assert n.tolist() == n_ref.tolist() and out.tolist() == out_ref.tolist()
+
+
+def test_greedy_sampling_is_greedy_acceptance(env):
+    torch, B = env
+    from paper_2410_11305_amd import synth
+    logits, draft, _ = synth.accept_case(11, 12, 3, 32000)
+    n, out = run(env, logits, np.zeros((12, 4)), temperature=np.zeros(12), draft=draft)
+    a, b = B.greedy_accept(dev(torch, logits), dev(torch, draft))
+    assert n.tolist() == a.tolist() and out.tolist() == b.tolist()
+
+
+def test_captured_calls_on_another_stream(env):
+    """Two graphs with a buffer set of their own each, replayed with eager work in between; dirty scratch."""
+    torch, B = env
+    rng = np.random.default_rng(6)
+    Bn, gamma, V = 6, 3, 5000
+    logits = dev(torch, (rng.standard_normal((Bn, gamma + 1, V)) * 2).astype(np.float16))
+    u = torch.rand((Bn, gamma + 1), device="cuda")
+    p = {k: dev(torch, np.asarray(v, dtype=np.int32 if k == "top_k" else np.float32)) for k, v in params(rng, Bn).items()}
+    draft = torch.zeros((Bn, gamma), dtype=torch.int32, device="cuda")
+    ws = torch.full((B.sample_workspace_bytes(Bn, gamma, V) + 64,), 0xA5, dtype=torch.uint8, device="cuda")
+    n, out = torch.empty(Bn, dtype=torch.int32, device="cuda"), torch.empty((Bn, gamma + 1), dtype=torch.int32, device="cuda")
+    call = lambda: B.sample(logits, u, **p, draft=draft, n_accept=n, out_tokens=out, workspace=ws)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        call()
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        call()
+    for r in range(4):
+        logits.copy_(dev(torch, (rng.standard_normal((Bn, gamma + 1, V)) * 2).astype(np.float16)))
+        u.copy_(dev(torch, rng.random((Bn, gamma + 1)).astype(np.float32)))
+        tokens = B.sample(logits, u, **p)[1]
+        draft.copy_(tokens[:, :gamma])
+        draft[r % Bn, r % gamma] = V
+        n.fill_(-7); out.fill_(-7)
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        n_ref, out_ref = so.accept(tokens.cpu().numpy(), draft.cpu().numpy())
+        assert n.tolist() == n_ref.tolist() and out.tolist() == out_ref.tolist()
+        assert (tokens.cpu().numpy() == want(logits.cpu().numpy(), u.cpu().numpy(), **{k: v.cpu().numpy() for k, v in p.items()})).all()
+
+
+def test_shares_follow_the_random_number(env):
+    """A grid of u over one row: every token is drawn as often as its weight says."""
+    V, N = 64, 4096
+    rng = np.random.default_rng(8)
+    row = (rng.standard_normal(V) * 1.5).astype(np.float16)
+    logits = np.broadcast_to(row, (1, N, V)).copy()
+    got = run(env, logits, ((np.arange(N) + 0.5) / N)[None])[1].ravel()
+    w = np.exp(row.astype(np.float64) - row.max())
+    share = w / w.sum()
+    assert np.abs(np.bincount(got, minlength=V) - share * N).max() <= 1.0
