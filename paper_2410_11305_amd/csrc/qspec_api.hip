@@ -839,7 +839,7 @@ inline int attn_row_blocks(int T, int G) { return (long long)T * G <= 16 ? 1 : (
 
 int check_attn(int B, int T, int Hq, int Hkv, int D) {
   if (D != 64 && D != 128) return QSPEC_ERR_SHAPE;
-  if (B < 1 || T < 1 || T > (1 << 20) || Hkv < 1 || Hq < Hkv || Hq % Hkv != 0) return QSPEC_ERR_SHAPE;
+  if (B < 1 || T < 1 || T > (1 << 20) || Hkv < 1 || Hq < Hkv || Hq % Hkv != 0 || Hq / Hkv > 255) return QSPEC_ERR_SHAPE;
   if ((long long)B * T * Hq * D * 2 >= 0x7fffffffLL) return QSPEC_ERR_SHAPE;
   return QSPEC_OK;
 }
@@ -848,11 +848,15 @@ size_t attn_workspace_bytes(int T, int G, int D) {
   return kAttnTicketBytes + (size_t)2 * kAttnMaxWorkgroups * 16 * attn_row_blocks(T, G) * attn_part_floats(D) * sizeof(float);
 }
 
+template <int D, int NB>
+void launch_attn_inst(const AttnArgs& a, hipStream_t s) {
+  launch_kernel((attn_kv4_kernel<D, NB>), dim3(kAttnMaxWorkgroups), dim3(64 * attn_waves(NB)), 0, s, a);
+}
 template <int D>
 void launch_attn(const AttnArgs& a, int nb, hipStream_t s) {
-  if (nb == 1) launch_kernel((attn_kv4_kernel<D, 1>), dim3(kAttnMaxWorkgroups), dim3(kAttnThreads), 0, s, a);
-  else if (nb == 2) launch_kernel((attn_kv4_kernel<D, 2>), dim3(kAttnMaxWorkgroups / 2), dim3(kAttnThreads), 0, s, a);
-  else launch_kernel((attn_kv4_kernel<D, 4>), dim3(kAttnMaxWorkgroups / 2), dim3(kAttnThreads), 0, s, a);
+  if (nb == 1) launch_attn_inst<D, 1>(a, s);
+  else if (nb == 2) launch_attn_inst<D, 2>(a, s);
+  else launch_attn_inst<D, 4>(a, s);
 }
 
 int check_sample_shape(int B, int gamma, int V) {
@@ -1279,12 +1283,13 @@ int qspec_attn_kv4(const void* q_f16, const void* cache, const int32_t* pos, con
   const int G = Hq / Hkv, nb = attn_row_blocks(T, G);
   if (workspace_bytes < attn_workspace_bytes(T, G, D)) return QSPEC_ERR_WORKSPACE;
   const long long blocks = ((long long)T * G + 16 * nb - 1) / (16 * nb);
-  if (B * blocks > 0x7fffffffLL) return QSPEC_ERR_SHAPE;
+  // the kernel counts the steps of the call in 32 bits
+  if (B * blocks * Hkv > 0x7fffffffLL / (((long long)max_pages * page_size + kAttnStep - 1) / kAttnStep + 1)) return QSPEC_ERR_SHAPE;
   if (int st = check_device()) return st;
   AttnArgs a{kv_shape(pos, page_table, T, Hkv, page_size, max_pages, n_pages), static_cast<const uint16_t*>(q_f16),
              static_cast<const uint8_t*>(cache), static_cast<uint16_t*>(out_f16), static_cast<unsigned*>(workspace),
              reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + kAttnTicketBytes), B, Hq, G, (int)blocks,
-             window, sinks, scale * 1.44269504f};
+             G > 1 ? (uint32_t)(((1ULL << 32) + G - 1) / G) : 0u, window, sinks, scale * 1.44269504f};
   if (D == 128) launch_attn<128>(a, nb, static_cast<hipStream_t>(stream));
   else launch_attn<64>(a, nb, static_cast<hipStream_t>(stream));
   return launch_status();
