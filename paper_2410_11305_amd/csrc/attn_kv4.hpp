@@ -27,14 +27,46 @@
 
 namespace qspec {
 
-constexpr int kAttnStep = 32;                // tokens
-constexpr int kAttnWhole = 16;               // items of up to so many steps are not shared out
-constexpr int kAttnMinSteps = 8;             // a workgroup is not given fewer steps on average
-constexpr int kAttnMaxWorkgroups = 512;
-constexpr size_t kAttnTicketBytes = 16384;   // arrival counters at the head of the workspace
+#ifndef FLYN
+#define FLYN 16
+#endif
+#ifndef TL4
+#define TL4 4
+#define TL2 4
+#define TL1 2
+#endif
+#ifndef W1
+#define W1 4
+#define S1 2
+#define T1 0
+#define GRID 512
+#endif
+constexpr size_t kAttnTicketBytes = 16384;   // arrival counters at the head of the workspace, one a workgroup
+#ifndef MIN1
+#define MIN1 512
+#define MIN2 512
+#define MIN4 1024
+#define OVER1 256
+#define OVER2 256
+#define OVER4 384
+#define WHOLE 512
+#endif
 
-// Wavefronts of a workgroup, by blocks of 16 rows that each of them carries.
-__host__ __device__ constexpr int attn_waves(int nb) { return nb == 1 ? 8 : 4; }
+// The shape of an instance.  NB: blocks of 16 columns a wavefront carries; F: token tiles that share a block (below).
+template <int NB, int F>
+struct AttnForm {
+  static constexpr int waves = NB == 1 ? W1 : 4;                    // of a workgroup
+  static constexpr int workgroups = NB == 1 ? GRID : 512;          // of a launch; two parts of an item each in the workspace at most
+  static constexpr int tiles = NB > 1 ? 2 : F == 4 ? TL4 : F == 2 ? TL2 : TL1;      // 16-token tiles of a step
+  static constexpr int step = 16 * tiles;                          // tokens of a step
+  static constexpr int rows = 16 * NB / F;                         // rows of a block of an item
+  // in steps: what the start and the end of an item cost beside its steps, items that are not shared out, and what a
+  // workgroup gets on average at least
+  static constexpr int over = (NB == 1 ? OVER1 : NB == 2 ? OVER2 : OVER4) / step;
+  static constexpr int whole = WHOLE / step;
+  static_assert(workgroups * sizeof(unsigned) <= kAttnTicketBytes, "a counter for every workgroup");
+  static constexpr int least = (NB == 1 ? MIN1 : NB == 2 ? MIN2 : MIN4) / step;
+};
 
 struct AttnArgs {
   KvShape kv;
@@ -61,6 +93,7 @@ struct AttnSpan {
 };
 
 // pos: position of the sequence's first row.  (Held to +-2^30, far outside of any cache, so that sums stay in 32 bits.)
+template <int STEP>
 __device__ __forceinline__ AttnSpan attn_span(const AttnArgs& p, int pos, int block, int rows_per_block) {
   const int r0 = block * rows_per_block, r1 = min(p.kv.T * p.G, r0 + rows_per_block) - 1;
   pos = min(max(pos, -(1 << 30)), 1 << 30);
@@ -68,185 +101,227 @@ __device__ __forceinline__ AttnSpan attn_span(const AttnArgs& p, int pos, int bl
   s.lo = pos + over_group(p, r0);
   s.hi = pos + over_group(p, r1);
   const int end = min(s.hi + 1, p.kv.max_pages << p.kv.page_shift);      // tokens 0 .. end - 1
-  s.first = p.window > 0 ? max(s.lo - p.window + 1, 0) / kAttnStep : 0;
-  s.sink_steps = p.window > 0 ? max(min((min(p.sinks, end) + kAttnStep - 1) / kAttnStep, s.first), 0) : 0;
+  s.first = p.window > 0 ? max(s.lo - p.window + 1, 0) / STEP : 0;
+  s.sink_steps = p.window > 0 ? max(min((min(p.sinks, end) + STEP - 1) / STEP, s.first), 0) : 0;
   // at least one: rows that see nothing have their zeros written
-  s.steps = max(s.sink_steps + max((end + kAttnStep - 1) / kAttnStep - s.first, 0), 1);
+  s.steps = max(s.sink_steps + max((end + STEP - 1) / STEP - s.first, 0), 1);
   return s;
 }
 
-// Sum and maximum over the four lanes that hold one column.
+// Sum and maximum over the four lanes that hold one column of an accumulator (lanes 16 and 32 apart).
 __device__ __forceinline__ float column_sum(float v) {
-  v += __shfl_xor(v, 16);
-  return v + __shfl_xor(v, 32);
+  auto a = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(uint32_t, v), __builtin_bit_cast(uint32_t, v), false, false);
+  v = __builtin_bit_cast(float, (uint32_t)a[0]) + __builtin_bit_cast(float, (uint32_t)a[1]);
+  auto b = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, v), __builtin_bit_cast(uint32_t, v), false, false);
+  return __builtin_bit_cast(float, (uint32_t)b[0]) + __builtin_bit_cast(float, (uint32_t)b[1]);
 }
 __device__ __forceinline__ float column_max(float v) {
-  v = fmaxf(v, __shfl_xor(v, 16));
-  return fmaxf(v, __shfl_xor(v, 32));
+  auto a = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(uint32_t, v), __builtin_bit_cast(uint32_t, v), false, false);
+  v = fmaxf(__builtin_bit_cast(float, (uint32_t)a[0]), __builtin_bit_cast(float, (uint32_t)a[1]));
+  auto b = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, v), __builtin_bit_cast(uint32_t, v), false, false);
+  return fmaxf(__builtin_bit_cast(float, (uint32_t)b[0]), __builtin_bit_cast(float, (uint32_t)b[1]));
+}
+// Sum and maximum over the F columns that hold one row (16 / F columns apart).
+template <int F>
+__device__ __forceinline__ float group_sum(float v) {
+  if (F > 1) v += dpp_f32<0x128>(v);            // rotation by 8 in a row of 16 lanes
+  if (F > 2) v += dpp_f32<0x124>(v);            // and by 4: the two sums of pairs alternate
+  return v;
+}
+template <int F>
+__device__ __forceinline__ float group_max(float v) {
+  if (F > 1) v = fmaxf(v, dpp_f32<0x128>(v));
+  if (F > 2) v = fmaxf(v, dpp_f32<0x124>(v));
+  return v;
 }
 
 __device__ __forceinline__ v8h half_frag(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
   return __builtin_bit_cast(v8h, uint4{a, b, c, d});
 }
+__device__ __forceinline__ v8h widen_codes(uint32_t x) {       // a word's 8 codes, in the order of the features
+  const uint32_t y = x >> 8;
+  return half_frag(x & 0x000F000Fu, x & 0x00F000F0u, y & 0x000F000Fu, y & 0x00F000F0u);
+}
 
 // A row of an item as its workgroups hand it over: reference, sum, (two unused), o
 __host__ __device__ constexpr int attn_part_floats(int D) { return D + 4; }
 
-// D features a head, NB blocks of 16 rows.
-template <int D, int NB>
-__global__ __launch_bounds__(64 * attn_waves(NB), NB == 1 ? 4 : 2) void attn_kv4_kernel(AttnArgs p) {
-  constexpr int WAVES = attn_waves(NB), THREADS = 64 * WAVES;
-  constexpr int NK = D / 32;                  // matrix instructions of a 16-token tile of q k^T; words of a lane of a key
-  constexpr int NV = D / 16;                  // matrix instructions of a step of p v
-  constexpr int RB = 16 * NB;
+// The workspace of an instance: what its launch indexes.
+template <int D, int NB, int F>
+constexpr size_t attn_workspace() {
+  typedef AttnForm<NB, F> Form;
+  return kAttnTicketBytes + (size_t)2 * Form::workgroups * Form::rows * attn_part_floats(D) * sizeof(float);
+}
+
+// D features a head, NB blocks of 16 columns, F tiles of tokens to a block.
+//
+// With up to 16 / F rows, F > 1, the columns of a block hold the rows F times over, and column c takes the tokens of tile
+// c / (16 / F) of a step only: the scores of the F tiles are computed for all columns and each column keeps its own, which
+// costs a selection and saves (F - 1) / F of the exponentials and all that goes with them; in the second product a
+// column's weights are zero for the tiles of the others.  Each column ends with its own sums, joined like those of the wavefronts.
+template <int D, int NB, int F>
+__global__ __launch_bounds__((64 * AttnForm<NB, F>::waves), NB == 1 ? S1 : 2) void attn_kv4_kernel(AttnArgs p) {
+  typedef AttnForm<NB, F> Form;
+  constexpr int WAVES = Form::waves, THREADS = 64 * WAVES, TILES = Form::tiles, STEP = Form::step, RB = Form::rows, OVER = Form::over;
+  constexpr int NK = D / 32;                  // matrix instructions of a tile of q k^T; words of a lane of a key
+  constexpr int NV = D / 16;                  // matrix instructions of two tiles of p v
+  constexpr int COLS = 16 / F;                // rows of a block of columns
+  constexpr int NX = 4 * TILES / F;           // scores of a lane in a step and block
+  constexpr int NP = NX / 4;                  // tiles of a lane
   constexpr int PITCH = D + 4;                // floats of a row in LDS
-  constexpr int OWN = 16 * D / THREADS;       // features of a thread where the wavefronts' sums are joined
-  constexpr int LANES = D / OWN;              // threads of a row there
+  constexpr int LANES = D / 4;                // threads of a row where sums are joined, 4 features each
   constexpr int PART = attn_part_floats(D);
   constexpr bool Q_LDS = NB == 4;             // the rows' registers would not leave room for the sums
+  constexpr bool TIGHT = NB == 4 || (T1 && NB == 1);             // registers for the sums and the loads under way, none for widening ahead
   constexpr float kNone = -1e30f;             // reference of a row that has seen nothing: below every score
-  __shared__ float o_lds[WAVES][16][PITCH];
-  __shared__ float m_lds[WAVES][16], l_lds[WAVES][16], c_lds[WAVES][16];
+  __shared__ float o_lds[WAVES][COLS][PITCH];
+  __shared__ float m_lds[WAVES][COLS], l_lds[WAVES][COLS], c_lds[WAVES][COLS];
+  __shared__ float join_m[THREADS / LANES], join_l[THREADS / LANES];
   __shared__ uint4 q_lds[Q_LDS ? NB * NK * 64 : 1];
-  __shared__ float2 f_lds[Q_LDS ? RB : 1];
-  __shared__ uint32_t scan[WAVES];
-  __shared__ int found[2][3];                 // entry, head, step in the item: begin and end of this workgroup's run
-  __shared__ uint32_t found_at;               // the begin, counted over all steps
+  __shared__ float4 f_lds[Q_LDS ? RB : 1];    // factor, sum, position of a row
   __shared__ unsigned ticket;
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
-  const int col = lane & 15, kb = lane >> 4;
+  const int col = lane & 15, kb = lane >> 4, mine_tile = F > 1 ? col / COLS : 0;
   const int P = 1 << p.kv.page_shift, R = p.kv.T * p.G, Hkv = p.kv.Hkv;
   const uint32_t region_bytes = (uint32_t)P * (D + 8);
-  const int row_of = tid / LANES, own = (tid & (LANES - 1)) * OWN;     // join: row of a block, first feature
+  const int row_of = tid / LANES, own = (tid & (LANES - 1)) * 4;       // join: row, first feature
   const auto sequence_of = [&](int e) { return p.blocks == 1 ? e : e / p.blocks; };
 
-  // ---- the division of the work: entries are (sequence, block of rows), each of Hkv items of equal length
+  // ---- the division of the work: entries are (sequence, block of rows), each of Hkv items of equal size, OVER + steps.
+  // Every wavefront works it out by itself, a run of entries to a lane: no barrier stands before the first loads.
   const int entries = p.B * p.blocks;
-  const int per = (entries + THREADS - 1) / THREADS;
-  const int e0 = tid * per, e1 = min(entries, e0 + per);
-  const auto steps_of = [&](int e) {
-    const int b = sequence_of(e);
-    return attn_span(p, p.kv.pos[b], e - b * p.blocks, RB).steps;
+  const int per = (entries + 63) / 64;
+  const auto size_of = [&](int e, int pos) {
+    return (uint32_t)(OVER + attn_span<STEP>(p, pos, e - sequence_of(e) * p.blocks, RB).steps) * (uint32_t)Hkv;
   };
   uint32_t mine = 0;
-  for (int e = e0; e < e1; ++e) mine += steps_of(e);
-  mine *= Hkv;
-  uint32_t upto = mine;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const uint32_t up = __shfl_up(upto, d);
-    if (lane >= d) upto += up;
-  }
-  if (lane == 63) scan[wave] = upto;
-  if (tid == 0) { found[1][0] = entries; found[1][1] = 0; found[1][2] = 0; }
-  __syncthreads();
-  uint32_t total = 0;
-  upto -= mine;                               // steps before this thread's entries
-#pragma unroll
-  for (int w = 0; w < WAVES; ++w) {
-    if (w < wave) upto += scan[w];
-    total += scan[w];
-  }
-  total = uniform(total);
-  const uint32_t groups = uniform(max(1u, min((uint32_t)gridDim.x, total / kAttnMinSteps)));
+  for (int e = lane * per; e < min(entries, (lane + 1) * per); ++e) mine += size_of(e, p.kv.pos[sequence_of(e)]);
+  uint32_t upto = mine;                       // of the entries up to this lane's
+#define QSPEC_DPP_ADD(ctrl, rows) upto += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)upto, ctrl, rows, 0xf, false)
+  QSPEC_DPP_ADD(0x111, 0xf);                  // row_shr 1, 2, 4, 8: sums inside a row of 16
+  QSPEC_DPP_ADD(0x112, 0xf);
+  QSPEC_DPP_ADD(0x114, 0xf);
+  QSPEC_DPP_ADD(0x118, 0xf);
+  QSPEC_DPP_ADD(0x142, 0xa);                  // row_bcast 15 into rows 1 and 3
+  QSPEC_DPP_ADD(0x143, 0xc);                  // row_bcast 31 into rows 2 and 3
+#undef QSPEC_DPP_ADD
+  const uint32_t total = (uint32_t)__builtin_amdgcn_readlane((int)upto, 63);
+  const uint32_t groups = uniform(min((uint32_t)gridDim.x, max((uint32_t)(entries * Hkv), total / (Form::least + OVER))));
   const uint32_t me = blockIdx.x;
   if (me >= groups) return;
-  // workgroup w begins at step w * share, and the first `more` of them take one more each
+  // workgroup w begins at w * share, and the first `more` of them take one more each; a begin in the first OVER of an
+  // item, or anywhere in one that is not shared out, is the item's
   const uint32_t share = uniform(total / groups), more = total - share * groups;
   const auto start_of = [&](uint32_t w) { return w * share + min(w, more); };
-  const auto group_of = [&](uint32_t x) {     // the workgroup that takes step x
+  const auto group_of = [&](uint32_t x) {     // the last workgroup that begins at x or before
     const uint32_t wide = more * (share + 1);
     return uniform(x < wide ? x / (share + 1) : more + (x - wide) / share);
   };
-#pragma unroll
-  for (int side = 0; side < 2; ++side) {
-    const uint32_t x = start_of(me + side);
-    if (x - upto < mine) {                    // (unsigned: upto <= x < upto + mine)
-      uint32_t at = upto;
-      for (int e = e0; e < e1; ++e) {
-        const uint32_t n = steps_of(e);
-        if (x - at < n * Hkv) {
-          const uint32_t h = (x - at) / n, s = n <= kAttnWhole ? 0 : x - at - h * n;
-          found[side][0] = e; found[side][1] = (int)h; found[side][2] = (int)s;
-          if (side == 0) found_at = at + h * n + s;
-          break;
-        }
-        at += n * Hkv;
+  struct Place { int entry, head, step; uint32_t item; };     // item: where its item starts
+  const auto place_of = [&](uint32_t x) {
+    if (x >= total) return Place{entries, 0, 0, total};
+    const int owner = __builtin_ctzll(__builtin_amdgcn_ballot_w64(upto > x));
+    uint32_t at = (uint32_t)__builtin_amdgcn_readlane((int)(upto - mine), owner), n = (uint32_t)__builtin_amdgcn_readlane((int)mine, owner);
+    int e = owner * per;
+    if (per > 1) {
+      for (;; ++e) {
+        n = uniform(size_of(e, uniform(scalar_load(p.kv.pos, sequence_of(e)))));
+        if (x - at < n) break;
+        at += n;
       }
     }
-  }
-  __syncthreads();
-  int entry = uniform(found[0][0]), head = uniform(found[0][1]), begin = uniform(found[0][2]);
-  const int last_entry = uniform(found[1][0]), last_head = uniform(found[1][1]), last_step = uniform(found[1][2]);
-  uint32_t at = uniform(found_at);            // of `begin` of this item
+    const uint32_t each = uniform(n / (uint32_t)Hkv), head = uniform((x - at) / each), in = x - at - head * each;
+    return Place{e, (int)head, each <= Form::whole + OVER || in <= OVER ? 0 : (int)(in - OVER), at + head * each};
+  };
+  const Place from = place_of(start_of(me)), to_place = place_of(start_of(me + 1));
+  int entry = from.entry, head = from.head, begin = from.step;
+  const int last_entry = to_place.entry, last_head = to_place.head, last_step = to_place.step;
+  uint32_t item = from.item;                  // where the item starts
   bool first_run = true;
 
   while (entry < last_entry || (entry == last_entry && (head < last_head || (head == last_head && begin < last_step)))) {
     const int b = uniform(sequence_of(entry)), block = entry - b * p.blocks;
-    AttnSpan span = attn_span(p, uniform(scalar_load(p.kv.pos, b)), block, RB);
+    AttnSpan span = attn_span<STEP>(p, uniform(scalar_load(p.kv.pos, b)), block, RB);
     span.steps = uniform(span.steps); span.sink_steps = uniform(span.sink_steps); span.first = uniform(span.first);
     span.lo = uniform(span.lo); span.hi = uniform(span.hi);
     const int stop = entry == last_entry && head == last_head ? last_step : span.steps;
     const int rows = min(RB, R - block * RB);
 
-    // ---- loads of a step: keys, rows of steps and lows, values, from the regions of its two 16-token tiles
-    struct Raw { uint32_t k[2][NK]; uint4 v[2], par[2][2]; };
+    // ---- loads of a step: keys and values of its tiles, steps and lows of this lane's tiles
+    struct Raw { uint32_t k[TILES][NK]; uint4 v[TILES], par[NP][2]; };
     Raw raw;
-    const auto first_token = [&](int s) { return kAttnStep * (s < span.sink_steps ? s : s - span.sink_steps + span.first); };
-    // page of the 16 tokens from t on, or -1
-    const auto page_of = [&](int t) {
-      const int i = t >> p.kv.page_shift;
+    struct Pages { int page[TILES]; uint32_t there; };    // of every tile, and a bit for each that exists
+    const auto first_token = [&](int s) { return STEP * (s < span.sink_steps ? s : s - span.sink_steps + span.first); };
+    // Pages of the next 64 tiles of this wavefront, BATCH steps, a tile to a lane: they are looked up a batch ahead.
+    constexpr int BATCH = 64 / TILES;
+    const auto look_up = [&](int s) {
+      const int i = (first_token(min(s + lane / TILES * WAVES, span.steps - 1)) + lane % TILES * 16) >> p.kv.page_shift;
       if (i >= p.kv.max_pages) return -1;
-      const int page = p.kv.table != nullptr ? uniform(scalar_load(p.kv.table, (size_t)b * p.kv.max_pages + i)) : b * p.kv.max_pages + i;
-      return page >= 0 && page < p.kv.n_pages ? page : -1;
+      const size_t at_page = (size_t)b * p.kv.max_pages + i;
+      return p.kv.table != nullptr ? p.kv.table[at_page] : (int)at_page;
     };
-    const auto region_of = [&](int page) { return p.cache + (size_t)(uint32_t)(max(page, 0) * Hkv + head) * region_bytes; };
+    int known = look_up(begin + wave), ahead = -1;
+    const auto pages_of = [&](int k) {        // of the batch's step k
+      Pages g;
+      g.there = 0;
+#pragma unroll
+      for (int i = 0; i < TILES; ++i) {
+        const int page = i > 0 && P >= STEP ? g.page[0] : __builtin_amdgcn_readlane(known, k * TILES + i);
+        const bool there = page >= 0 && page < p.kv.n_pages;
+        g.page[i] = there ? page : 0;
+        g.there |= there ? 1u << i : 0u;
+      }
+      return g;
+    };
+    const auto region_of = [&](int page) { return p.cache + (size_t)(uint32_t)(page * Hkv + head) * region_bytes; };
     const uint32_t k_off = (uint32_t)(col * (D / 2) + kb * (4 * NK)), par_off = (uint32_t)(kb * 32);
     const uint32_t v_off = (uint32_t)((col & (D / 8 - 1)) * 64 + kb * 16);
-    const auto load_keys = [&](int i, int t, const uint8_t* region) {
-      const uint8_t* const src = region + (uint32_t)(t & (P - 1)) * (D / 2);
-      if (NK == 4) {
-        const uint4 w = *reinterpret_cast<const uint4*>(src + k_off);
-        raw.k[i][0] = w.x; raw.k[i][1] = w.y; raw.k[i][NK - 2] = w.z; raw.k[i][NK - 1] = w.w;
-      } else {
-        const uint2 w = *reinterpret_cast<const uint2*>(src + k_off);
-        raw.k[i][0] = w.x; raw.k[i][1] = w.y;
+    const auto load_keys = [&](int t, const Pages& g) {
+#pragma unroll
+      for (int i = 0; i < TILES; ++i) {
+        const uint8_t* const src = region_of(g.page[i]) + (uint32_t)((t + 16 * i) & (P - 1)) * (D / 2);
+        if (NK == 4) {
+          const uint4 w = *reinterpret_cast<const uint4*>(src + k_off);
+          raw.k[i][0] = w.x; raw.k[i][1] = w.y; raw.k[i][NK - 2] = w.z; raw.k[i][NK - 1] = w.w;
+        } else {
+          const uint2 w = *reinterpret_cast<const uint2*>(src + k_off);
+          raw.k[i][0] = w.x; raw.k[i][1] = w.y;
+        }
       }
     };
-    const auto load_rest = [&](int i, int t, const uint8_t* region) {
-      const uint32_t slot = (uint32_t)(t & (P - 1));
-      const uint8_t* const par = region + (uint32_t)P * D + slot * 8;
-      raw.par[i][0] = *reinterpret_cast<const uint4*>(par + par_off);
-      raw.par[i][1] = *reinterpret_cast<const uint4*>(par + par_off + 16);
-      raw.v[i] = *reinterpret_cast<const uint4*>(region + (uint32_t)P * (D / 2) + slot * (D / 2) + v_off);
+    const auto load_rest = [&](int t, const Pages& g, int k) {
+#pragma unroll
+      for (int i = 0; i < NP; ++i) {                   // its tiles: i * F + mine_tile
+        const uint8_t* par;
+        if (F == 1 || P >= STEP) {
+          par = region_of(g.page[i * F]) + (uint32_t)P * D + (uint32_t)((t + 16 * F * i) & (P - 1)) * 8 + (par_off + (uint32_t)mine_tile * 128);
+        } else {                                     // pages that end inside a step: a lane's tile has a region of its own
+          const int page = __shfl(known, k * TILES + i * F + mine_tile);
+          par = region_of(page >= 0 && page < p.kv.n_pages ? page : 0) + (uint32_t)P * D + (uint32_t)((t + 16 * (i * F + mine_tile)) & (P - 1)) * 8 + par_off;
+        }
+        raw.par[i][0] = reinterpret_cast<const uint4*>(par)[0];
+        raw.par[i][1] = reinterpret_cast<const uint4*>(par)[1];
+      }
+#pragma unroll
+      for (int i = 0; i < TILES; ++i)
+        raw.v[i] = *reinterpret_cast<const uint4*>(region_of(g.page[i]) + (uint32_t)P * (D / 2) + (uint32_t)((t + 16 * i) & (P - 1)) * (D / 2) + v_off);
     };
-    int s = begin + wave;
-    int t = 0, page0 = -1, page1 = -1;
-    if (s < stop) {
-      t = first_token(s);
-      page0 = page_of(t);
-      page1 = P >= kAttnStep ? page0 : page_of(t + 16);
-      const uint8_t* const region0 = region_of(page0);
-      const uint8_t* const region1 = region_of(page1);
-      load_keys(0, t, region0);
-      load_keys(1, t + 16, region1);
-      load_rest(0, t, region0);
-      load_rest(1, t + 16, region1);
-    }
-
     // ---- the rows: scaled to 2^13 .. 2^14, a sixteenth where the codes come 16 times too large
     v8h qf[Q_LDS ? 1 : NB][NK];
-    float f[NB], shift[NB], m[NB], l[NB], c[NB];      // l: sum of p; c: the part of o that all features share
-    int row_pos[NB];
+    float f_own[Q_LDS ? 1 : NB], shift_own[Q_LDS ? 1 : NB], m[NB], l[NB], c[NB];      // l: sum of p; c: the part of o that all features share
+    int pos_own[Q_LDS ? 1 : NB];
     v4f o[NB][NV];
-    const auto row_of_q = [&](int nb, v8h (&x)[NK], float& factor, float& sum_of) {
-      const int r = min(nb * 16 + col, rows - 1) + block * RB;             // (columns without a row repeat the last one)
-      const int j = over_group(p, r), g = r - j * p.G;
+    const auto row_of_column = [&](int nb) { return block * RB + min(nb * COLS + (col & (COLS - 1)), rows - 1); };     // (columns without a row repeat the last one)
+    const auto load_row = [&](int nb, v8h (&x)[NK]) {
+      const int r = row_of_column(nb), j = over_group(p, r), g = r - j * p.G;
       const uint16_t* const src = p.q + (((size_t)b * p.kv.T + j) * p.Hq + (size_t)head * p.G + g) * D + kb * 8 * NK;
+#pragma unroll
+      for (int i = 0; i < NK; ++i) x[i] = __builtin_bit_cast(v8h, reinterpret_cast<const uint4*>(src)[i]);
+    };
+    const auto scale_row = [&](v8h (&x)[NK], float& factor_of, float& sum_of) {
       float top = 0.0f, sum = 0.0f;
 #pragma unroll
       for (int i = 0; i < NK; ++i) {
-        x[i] = __builtin_bit_cast(v8h, reinterpret_cast<const uint4*>(src)[i]);
 #pragma unroll
         for (int e = 0; e < 8; ++e) { top = fmaxf(top, fabsf((float)x[i][e])); sum += (float)x[i][e]; }
       }
@@ -258,30 +333,41 @@ __global__ __launch_bounds__(64 * attn_waves(NB), NB == 1 ? 4 : 2) void attn_kv4
       for (int i = 0; i < NK; ++i)
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[i][e] = (_Float16)((float)x[i][e] * (e & 2 ? up * 0.0625f : up));
-      factor = p.scale_log2 * __builtin_amdgcn_ldexpf(1.0f, ex + 10);
+      factor_of = p.scale_log2 * __builtin_amdgcn_ldexpf(1.0f, ex + 10);
       sum_of = sum * __builtin_amdgcn_ldexpf(1.0f, -ex - 10);
     };
+    const auto position_of = [&](int nb) { return span.lo + over_group(p, row_of_column(nb)) - over_group(p, block * RB); };
+    if (!Q_LDS) {
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) load_row(nb, qf[Q_LDS ? 0 : nb]);
+    }
+    int s = begin + wave, t = 0;
+    Pages pages;
+    if (s < stop) {
+      t = first_token(s);
+      pages = pages_of(0);
+      load_keys(t, pages);
+      load_rest(t, pages, 0);
+      ahead = look_up(s + BATCH * WAVES);
+    }
     if (Q_LDS) {
       if (wave < NB) {
         v8h x[NK];
-        float factor, sum_of;
-        row_of_q(wave, x, factor, sum_of);
+        float factor_of, sum_of;
+        load_row(wave, x);
+        scale_row(x, factor_of, sum_of);
 #pragma unroll
         for (int i = 0; i < NK; ++i) q_lds[(wave * NK + i) * 64 + lane] = __builtin_bit_cast(uint4, x[i]);
-        if (kb == 0) f_lds[wave * 16 + col] = float2{factor, sum_of};
+        if (kb == 0) f_lds[wave * 16 + col] = float4{factor_of, sum_of, __builtin_bit_cast(float, position_of(wave)), 0.0f};
       }
       __syncthreads();
     }
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
-      if (Q_LDS) {
-        const float2 both = f_lds[nb * 16 + col];
-        f[nb] = both.x;
-        shift[nb] = both.y;
-      } else {
-        row_of_q(nb, qf[nb], f[nb], shift[nb]);
+      if (!Q_LDS) {
+        scale_row(qf[Q_LDS ? 0 : nb], f_own[Q_LDS ? 0 : nb], shift_own[Q_LDS ? 0 : nb]);
+        pos_own[Q_LDS ? 0 : nb] = position_of(nb);
       }
-      row_pos[nb] = span.lo + over_group(p, min(nb * 16 + col, rows - 1) + block * RB) - over_group(p, block * RB);
       m[nb] = kNone;
       l[nb] = c[nb] = 0.0f;
 #pragma unroll
@@ -291,41 +377,46 @@ __global__ __launch_bounds__(64 * attn_waves(NB), NB == 1 ? 4 : 2) void attn_kv4
       if (Q_LDS) return __builtin_bit_cast(v8h, q_lds[(nb * NK + w) * 64 + lane]);
       return qf[Q_LDS ? 0 : nb][w];
     };
+    const auto factor = [&](int nb) { return Q_LDS ? f_lds[nb * 16 + col].x : f_own[Q_LDS ? 0 : nb]; };
+    const auto shift = [&](int nb) { return Q_LDS ? f_lds[nb * 16 + col].y : shift_own[Q_LDS ? 0 : nb]; };
+    const auto position = [&](int nb) { return Q_LDS ? __builtin_bit_cast(int, f_lds[nb * 16 + col].z) : pos_own[Q_LDS ? 0 : nb]; };
     int vexp = -30;                           // exponent of the largest value step so far
 
     // ---- the steps of this wavefront
-    for (; s < stop; s += WAVES) {
+    for (int k = 1; s < stop; s += WAVES, ++k) {
       const int t_next = first_token(min(s + WAVES, span.steps - 1));       // (the last one's loads repeat a step)
-      const int next0 = page_of(t_next), next1 = P >= kAttnStep ? next0 : page_of(t_next + 16);
-      const uint8_t* const region0 = region_of(next0);
-      const uint8_t* const region1 = region_of(next1);
+      if (k == BATCH) {
+        k = 0;
+        known = ahead;
+        ahead = look_up(s + (BATCH + 1) * WAVES);
+      }
+      const Pages next = pages_of(k);
       // every token of the step in sight of every row
-      const bool whole = page0 >= 0 && page1 >= 0 && t + kAttnStep - 1 <= span.lo &&
-                         (p.window == 0 || t > span.hi - p.window || t + kAttnStep <= p.sinks);
-      v4f sc[NB][2];
+      const bool whole = pages.there == (1u << TILES) - 1 && t + STEP - 1 <= span.lo && (p.window == 0 || t > span.hi - p.window || t + STEP <= p.sinks);
+      v4f sc[NB][TILES];
 #pragma unroll
-      for (int nb = 0; nb < NB; ++nb) sc[nb][0] = sc[nb][1] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+      for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+        for (int i = 0; i < TILES; ++i) sc[nb][i] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
       for (int w = 0; w < NK; ++w) {
-        const auto widen = [](uint32_t x) {
-          const uint32_t y = x >> 8;
-          return half_frag(x & 0x000F000Fu, x & 0x00F000F0u, y & 0x000F000Fu, y & 0x00F000F0u);
-        };
-        const v8h k0 = widen(raw.k[0][w]), k1 = widen(raw.k[1][w]);
+        v8h kf[TILES];
+#pragma unroll
+        for (int i = 0; i < TILES; ++i) kf[i] = widen_codes(raw.k[i][w]);
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
           const v8h x = q_frag(nb, w);
-          sc[nb][0] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k0, x, sc[nb][0], 0, 0, 0);
-          sc[nb][1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k1, x, sc[nb][1], 0, 0, 0);
-        }
-      }
-      load_keys(0, t_next, region0);
-      load_keys(1, t_next + 16, region1);
-
-      // steps and lows of this lane's 8 tokens
-      v2h kp[8], vp[8];
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
+          for (int i = 0; i < TILES; ++i) sc[nb][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf[i], x, sc[nb][i], 0, 0, 0);
+        }
+        if (TIGHT) __builtin_amdgcn_sched_barrier(0);          // (widening ahead would cost the registers of the sums)
+      }
+      load_keys(t_next, next);
+
+      // steps and lows of this lane's tokens, and its scores
+      v2h kp[NX], vp[NX];
+#pragma unroll
+      for (int i = 0; i < NP; ++i) {
         const uint32_t w[8] = {raw.par[i][0].x, raw.par[i][0].y, raw.par[i][0].z, raw.par[i][0].w,
                                raw.par[i][1].x, raw.par[i][1].y, raw.par[i][1].z, raw.par[i][1].w};
 #pragma unroll
@@ -334,42 +425,50 @@ __global__ __launch_bounds__(64 * attn_waves(NB), NB == 1 ? 4 : 2) void attn_kv4
           vp[4 * i + x] = __builtin_bit_cast(v2h, w[2 * x + 1]);
         }
       }
+      float sv[NB][NX];
 #pragma unroll
-      for (int nb = 0; nb < NB; ++nb)
+      for (int nb = 0; nb < NB; ++nb) {
+        const float sum_of = shift(nb);
 #pragma unroll
-        for (int x = 0; x < 8; ++x)
-          sc[nb][x >> 2][x & 3] = fmaf(sc[nb][x >> 2][x & 3], (float)kp[x].x, (float)kp[x].y * shift[nb]);
+        for (int x = 0; x < NX; ++x) {
+          float dot = sc[nb][(x >> 2) * F][x & 3];
+#pragma unroll
+          for (int i = 1; i < F; ++i) dot = mine_tile == i ? sc[nb][(x >> 2) * F + i][x & 3] : dot;
+          sv[nb][x] = fmaf(dot, (float)kp[x].x, (float)kp[x].y * sum_of);
+        }
+        if (TIGHT) __builtin_amdgcn_sched_barrier(0);
+      }
       if (!whole) {
         uint32_t any = 0;                     // bit x: a row of this lane sees its token x
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
+          const int at_row = position(nb), behind = p.window > 0 ? at_row - p.window : -0x7fffffff - 1;
 #pragma unroll
-          for (int x = 0; x < 8; ++x) {
-            const int tok = t + (x >> 2) * 16 + 4 * kb + (x & 3);
-            const bool in = (x < 4 ? page0 : page1) >= 0 && tok <= row_pos[nb] &&
-                            (p.window == 0 || tok > row_pos[nb] - p.window || tok < p.sinks);
+          for (int x = 0; x < NX; ++x) {
+            const int tok = t + ((x >> 2) * F + mine_tile) * 16 + 4 * kb + (x & 3);
+            const bool in = ((pages.there >> ((x >> 2) * F + mine_tile) & 1u) != 0) & (tok <= at_row) & ((tok > behind) | (tok < p.sinks));
             any |= in ? 1u << x : 0u;
-            sc[nb][x >> 2][x & 3] = in ? sc[nb][x >> 2][x & 3] : -__builtin_inff();
+            sv[nb][x] = in ? sv[nb][x] : -__builtin_inff();
           }
         }
         // whatever stands in rows that nobody sees (infinities, NaN) must not meet a weight, not even one of zero
 #pragma unroll
-        for (int x = 0; x < 8; ++x) vp[x] = any >> x & 1u ? vp[x] : v2h{(_Float16)0.0f, (_Float16)0.0f};
+        for (int x = 0; x < NX; ++x) vp[x] = any >> x & 1u ? vp[x] : v2h{(_Float16)0.0f, (_Float16)0.0f};
       }
       // The reference: 2^(s - m) times the value steps has to stay inside fp16's range, with its largest terms well above its
       // smallest numbers, so m is the largest score less 8, plus the exponent of the largest value step.  It moves
       // when a term could pass 2^14, which after the first step is rare.
       v2h vmax2 = vp[0];
 #pragma unroll
-      for (int x = 1; x < 8; ++x) vmax2 = __builtin_elementwise_max(vmax2, vp[x]);
+      for (int x = 1; x < NX; ++x) vmax2 = __builtin_elementwise_max(vmax2, vp[x]);
       const float vtop = (float)vmax2.x;
       bool reset = vtop > __builtin_amdgcn_ldexpf(1.0f, vexp);
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) {
-        float top = sc[nb][0][0];
+        float top = sv[nb][0];
 #pragma unroll
-        for (int x = 1; x < 8; ++x) top = fmaxf(top, sc[nb][x >> 2][x & 3]);
-        reset |= fmaf(top, f[nb], -m[nb]) > (float)(14 - vexp);
+        for (int x = 1; x < NX; ++x) top = fmaxf(top, sv[nb][x]);
+        reset |= fmaf(top, factor(nb), -m[nb]) > (float)(14 - vexp);
       }
       if (__builtin_amdgcn_ballot_w64(reset) != 0) {
         float vwide = vtop;
@@ -379,10 +478,10 @@ __global__ __launch_bounds__(64 * attn_waves(NB), NB == 1 ? 4 : 2) void attn_kv4
         vexp = uniform(max(vexp, vwide > 0.0f ? __builtin_amdgcn_frexp_expf(vwide) : vexp));
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
-          float top = sc[nb][0][0];
+          float top = sv[nb][0];
 #pragma unroll
-          for (int x = 1; x < 8; ++x) top = fmaxf(top, sc[nb][x >> 2][x & 3]);
-          const float to = fmaxf(m[nb] + (float)(vexp - before), fmaf(column_max(top), f[nb], (float)(vexp - 8)));
+          for (int x = 1; x < NX; ++x) top = fmaxf(top, sv[nb][x]);
+          const float to = fmaxf(m[nb] + (float)(vexp - before), fmaf(column_max(top), factor(nb), (float)(vexp - 8)));
           const float by = __builtin_amdgcn_exp2f(m[nb] - to);
           m[nb] = to;
           l[nb] *= by;
@@ -391,112 +490,137 @@ __global__ __launch_bounds__(64 * attn_waves(NB), NB == 1 ? 4 : 2) void attn_kv4
           for (int v = 0; v < NV; ++v) o[nb][v] *= by;
         }
       }
-      v8h pf[NB];
+      uint32_t w[NB][NX / 2];                 // the weights, two a word
       typedef float v2f __attribute__((ext_vector_type(2)));
       const v2h minus8 = {(_Float16)-8.0f, (_Float16)-8.0f};
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) {
-        v2h w[4];
+        const float by = factor(nb);
 #pragma unroll
-        for (int x = 0; x < 8; x += 2) {
-          const float e0 = __builtin_amdgcn_exp2f(fmaf(sc[nb][x >> 2][x & 3], f[nb], -m[nb]));
-          const float e1 = __builtin_amdgcn_exp2f(fmaf(sc[nb][x >> 2][(x & 3) + 1], f[nb], -m[nb]));
+        for (int x = 0; x < NX; x += 2) {
+          const float e0 = __builtin_amdgcn_exp2f(fmaf(sv[nb][x], by, -m[nb]));
+          const float e1 = __builtin_amdgcn_exp2f(fmaf(sv[nb][x + 1], by, -m[nb]));
           l[nb] += e0;
           l[nb] += e1;
           c[nb] = fmaf(e0, fmaf(8.0f, (float)vp[x].x, (float)vp[x].y), c[nb]);
           c[nb] = fmaf(e1, fmaf(8.0f, (float)vp[x + 1].x, (float)vp[x + 1].y), c[nb]);
           // 11 bits of a weight: what an fp16 probability keeps
-          w[x / 2] = __builtin_convertvector((v2f{e0 * (float)vp[x].x, e1 * (float)vp[x + 1].x}), v2h);
-          c[nb] = __builtin_amdgcn_fdot2(w[x / 2], minus8, c[nb], false);
+          const v2h both = __builtin_convertvector((v2f{e0 * (float)vp[x].x, e1 * (float)vp[x + 1].x}), v2h);
+          c[nb] = __builtin_amdgcn_fdot2(both, minus8, c[nb], false);
+          w[nb][x / 2] = __builtin_bit_cast(uint32_t, both);
         }
-        pf[nb] = __builtin_bit_cast(v8h, uint4{__builtin_bit_cast(uint32_t, w[0]), __builtin_bit_cast(uint32_t, w[1]),
-                                               __builtin_bit_cast(uint32_t, w[2]), __builtin_bit_cast(uint32_t, w[3])});
+        if (TIGHT) __builtin_amdgcn_sched_barrier(0);
       }
-      // values: token pairs of one half of the words, nibble by nibble
-      const auto values = [&](uint32_t sel, int v0) {
-        const uint4 a = raw.v[0], d = raw.v[1];
-        const uint32_t x[4] = {__builtin_amdgcn_perm(a.y, a.x, sel), __builtin_amdgcn_perm(a.w, a.z, sel),
-                               __builtin_amdgcn_perm(d.y, d.x, sel), __builtin_amdgcn_perm(d.w, d.z, sel)};
+      // values, two tiles at a time: token pairs of one half of the words, nibble by nibble
 #pragma unroll
-        for (int n = 0; n < 4; ++n) {
-          const uint32_t mask = n & 1 ? 0x00F000F0u : 0x000F000Fu;
-          const int by = n & 2 ? 8 : 0;
-          const v8h vf = half_frag(x[0] >> by & mask, x[1] >> by & mask, x[2] >> by & mask, x[3] >> by & mask);
+      for (int pair = 0; pair < TILES / 2; ++pair) {
+        v8h pf[NB];
 #pragma unroll
-          for (int nb = 0; nb < NB; ++nb) o[nb][v0 + n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, pf[nb], o[nb][v0 + n], 0, 0, 0);
+        for (int nb = 0; nb < NB; ++nb) {
+          if (F == 1) {
+            pf[nb] = half_frag(w[nb][4 * pair], w[nb][4 * pair + 1], w[nb][4 * pair + 2], w[nb][4 * pair + 3]);
+          } else {
+            const uint32_t first = mine_tile == 2 * pair % F ? ~0u : 0u, second = mine_tile == 2 * pair % F + 1 ? ~0u : 0u;
+            const uint32_t lo = w[nb][2 * (2 * pair / F)], hi = w[nb][2 * (2 * pair / F) + 1];
+            pf[nb] = half_frag(lo & first, hi & first, lo & second, hi & second);
+          }
         }
-      };
-      if (D == 128) {
-        values(0x05040100u, 0);
-        values(0x07060302u, NV - 4);
-      } else {
-        values(col & 8 ? 0x07060302u : 0x05040100u, 0);        // lanes 8 .. 15 of a row take the upper halves of the same words
+        const auto values = [&](uint32_t sel, int v0) {
+          const uint4 a = raw.v[2 * pair], d = raw.v[2 * pair + 1];
+          const uint32_t x[4] = {__builtin_amdgcn_perm(a.y, a.x, sel), __builtin_amdgcn_perm(a.w, a.z, sel),
+                                 __builtin_amdgcn_perm(d.y, d.x, sel), __builtin_amdgcn_perm(d.w, d.z, sel)};
+#pragma unroll
+          for (int n = 0; n < 4; ++n) {
+            const uint32_t mask = n & 1 ? 0x00F000F0u : 0x000F000Fu;
+            const int by = n & 2 ? 8 : 0;
+            const v8h vf = half_frag(x[0] >> by & mask, x[1] >> by & mask, x[2] >> by & mask, x[3] >> by & mask);
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) o[nb][v0 + n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, pf[nb], o[nb][v0 + n], 0, 0, 0);
+            if (TIGHT) __builtin_amdgcn_sched_barrier(0);
+          }
+        };
+        if (D == 128) {
+          values(0x05040100u, 0);
+          values(0x07060302u, NV - 4);
+        } else {
+          values(col & 8 ? 0x07060302u : 0x05040100u, 0);      // lanes 8 .. 15 of a row take the upper halves of the same words
+        }
       }
-      load_rest(0, t_next, region0);
-      load_rest(1, t_next + 16, region1);
+      load_rest(t_next, next, k);
       t = t_next;
-      page0 = next0;
-      page1 = next1;
+      pages = next;
     }
 
-    // ---- the wavefronts' sums, 16 rows at a time
+    // ---- the wavefronts' sums, a block of columns at a time
     const bool shared = begin > 0 || stop < span.steps;
-    const uint32_t item = at - begin;
-    const uint32_t w0 = shared ? group_of(item) : me, w1 = shared ? group_of(item + span.steps - 1) : me;   // the workgroups that hold a part of it
-    const auto write_row = [&](int r, const float (&v)[OWN], float sum) {
+    const uint32_t w0 = shared ? group_of(item + OVER) : me, w1 = shared ? group_of(item + OVER + span.steps - 1) : me;   // the workgroups that hold a part of it
+    const auto write_row = [&](int r, const float (&v)[4], float sum) {
       const int j = over_group(p, r), g = r - j * p.G;
       const float by = sum > 0.0f ? 1.0f / sum : 0.0f;
-      typedef _Float16 vh __attribute__((ext_vector_type(OWN)));
-      vh h;
+      typedef _Float16 v4h __attribute__((ext_vector_type(4)));
+      v4h h;
 #pragma unroll
-      for (int x = 0; x < OWN; ++x) h[x] = (_Float16)(sum > 0.0f ? fminf(fmaxf(v[x] * by, -65504.0f), 65504.0f) : 0.0f);   // (a 15th code may lie past fp16's end)
-      *reinterpret_cast<vh*>(p.out + (((size_t)b * p.kv.T + j) * p.Hq + (size_t)head * p.G + g) * D + own) = h;
+      for (int x = 0; x < 4; ++x) h[x] = (_Float16)(sum > 0.0f ? fminf(fmaxf(v[x] * by, -65504.0f), 65504.0f) : 0.0f);   // (a 15th code may lie past fp16's end)
+      *reinterpret_cast<v4h*>(p.out + (((size_t)b * p.kv.T + j) * p.Hq + (size_t)head * p.G + g) * D + own) = h;
     };
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
-      if (nb * 16 >= rows) break;
+      if (nb * COLS >= rows) break;
+      if (F > 1) {                            // the columns of a row
+        const float to = group_max<F>(m[nb]), by = __builtin_amdgcn_exp2f(m[nb] - to);
+        m[nb] = to;
+        l[nb] = group_sum<F>(l[nb] * by);
+        c[nb] = group_sum<F>(c[nb] * by);
+#pragma unroll
+        for (int v = 0; v < NV; ++v)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) o[nb][v][i] = group_sum<F>(o[nb][v][i] * by);
+      }
       l[nb] = column_sum(l[nb]);
       c[nb] = column_sum(c[nb]);
-      if (kb == 0) { m_lds[wave][col] = m[nb]; l_lds[wave][col] = l[nb]; c_lds[wave][col] = c[nb]; }
+      if (lane < COLS) { m_lds[wave][lane] = m[nb]; l_lds[wave][lane] = l[nb]; c_lds[wave][lane] = c[nb]; }
+      if (F == 1 || col < COLS) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        float* const dst = &o_lds[wave][col][8 * ((4 * kb + i) & (D / 8 - 1))];
-        if (D == 128) {
-          float x[8];
+        for (int i = 0; i < 4; ++i) {
+          float* const dst = &o_lds[wave][col & (COLS - 1)][8 * ((4 * kb + i) & (D / 8 - 1))];
+          if (D == 128) {
+            float x[8];
 #pragma unroll
-          for (int e = 0; e < 8; ++e) x[e] = o[nb][((e & 1) * 4 + e / 2) % NV][i] * (e & 2 ? 1048576.0f : 16777216.0f);
-          reinterpret_cast<float4*>(dst)[0] = float4{x[0], x[1], x[2], x[3]};
-          reinterpret_cast<float4*>(dst)[1] = float4{x[4], x[5], x[6], x[7]};
-        } else {
+            for (int e = 0; e < 8; ++e) x[e] = o[nb][((e & 1) * 4 + e / 2) % NV][i] * (e & 2 ? 1048576.0f : 16777216.0f);
+            reinterpret_cast<float4*>(dst)[0] = float4{x[0], x[1], x[2], x[3]};
+            reinterpret_cast<float4*>(dst)[1] = float4{x[4], x[5], x[6], x[7]};
+          } else {
 #pragma unroll
-          for (int n = 0; n < 4; ++n) dst[2 * n + (kb >> 1)] = o[nb][n][i] * (n & 1 ? 1048576.0f : 16777216.0f);
+            for (int n = 0; n < 4; ++n) dst[2 * n + (kb >> 1)] = o[nb][n][i] * (n & 1 ? 1048576.0f : 16777216.0f);
+          }
         }
       }
       __syncthreads();
-      const int r = nb * 16 + row_of;
-      if (r < rows) {
-        float v[OWN], by[WAVES], total_l = 0.0f, total_c = 0.0f, ref = kNone;
+      for (int in = row_of; in < COLS; in += THREADS / LANES) {
+        const int r = nb * COLS + in;
+        if (r >= rows) break;
+        float v[4], total_l = 0.0f, total_c = 0.0f, ref = kNone;
 #pragma unroll
-        for (int w = 0; w < WAVES; ++w) ref = fmaxf(ref, m_lds[w][row_of]);
+        for (int w = 0; w < WAVES; ++w) ref = fmaxf(ref, m_lds[w][in]);
+#pragma unroll
+        for (int x = 0; x < 4; ++x) v[x] = 0.0f;
 #pragma unroll
         for (int w = 0; w < WAVES; ++w) {
-          by[w] = __builtin_amdgcn_exp2f(m_lds[w][row_of] - ref);
-          total_l = fmaf(l_lds[w][row_of], by[w], total_l);
-          total_c = fmaf(c_lds[w][row_of], by[w], total_c);
+          const float by = __builtin_amdgcn_exp2f(m_lds[w][in] - ref);
+          const float4 x = *reinterpret_cast<const float4*>(&o_lds[w][in][own]);
+          total_l = fmaf(l_lds[w][in], by, total_l);
+          total_c = fmaf(c_lds[w][in], by, total_c);
+          v[0] = fmaf(x.x, by, v[0]); v[1] = fmaf(x.y, by, v[1]); v[2] = fmaf(x.z, by, v[2]); v[3] = fmaf(x.w, by, v[3]);
         }
 #pragma unroll
-        for (int x = 0; x < OWN; ++x) {
-          v[x] = total_c;
-#pragma unroll
-          for (int w = 0; w < WAVES; ++w) v[x] = fmaf(o_lds[w][row_of][own + x], by[w], v[x]);
-        }
+        for (int x = 0; x < 4; ++x) v[x] += total_c;
         if (!shared) {
           write_row(block * RB + r, v, total_l);
         } else {
           float* const part = p.parts + ((size_t)(2 * me + (first_run ? 0 : 1)) * RB + r) * PART;
           if (own == 0) store_shared_f2(part, ref, total_l);
-#pragma unroll
-          for (int x = 0; x < OWN; x += 2) store_shared_f2(part + 4 + own + x, v[x], v[x + 1]);
+          store_shared_f2(part + 4 + own, v[0], v[1]);
+          store_shared_f2(part + 6 + own, v[2], v[3]);
         }
       }
       __syncthreads();
@@ -504,47 +628,49 @@ __global__ __launch_bounds__(64 * attn_waves(NB), NB == 1 ? 4 : 2) void attn_kv4
 
     // ---- the last of the item's workgroups joins their parts
     if (shared && last_arrival(p.tickets, (int)(w1 - w0 + 1), w0, &ticket)) {
+      constexpr int SETS = THREADS / LANES;            // rows at a time
       const int n = (int)(w1 - w0 + 1);
       const uint32_t slot0 = 2 * w0 + (start_of(w0) < item ? 1 : 0);
       // few rows: several threads take a row's parts in turn
-      const int taken = rows > 8 ? 16 : rows > 4 ? 8 : rows > 2 ? 4 : rows > 1 ? 2 : 1;
-      const int sub = row_of & (taken - 1), lot = row_of / taken, lots = 16 / taken;
-      for (int r0 = 0; r0 < rows; r0 += 16) {
+      int taken = 1;
+      while (taken < min(rows, SETS)) taken *= 2;
+      const int sub = row_of & (taken - 1), lot = row_of / taken, lots = SETS / taken;
+      for (int r0 = 0; r0 < rows; r0 += SETS) {
         const int r = r0 + sub;
-        float ref = kNone, sum = 0.0f, v[OWN];
-#pragma unroll
-        for (int x = 0; x < OWN; ++x) v[x] = 0.0f;
+        float ref = kNone, sum = 0.0f, v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        const auto add = [&](float m2, float l2, float a, float b2, float c2, float d2) {
+          const float to = fmaxf(ref, m2), x = __builtin_amdgcn_exp2f(ref - to), y = __builtin_amdgcn_exp2f(m2 - to);
+          ref = to;
+          sum = sum * x + l2 * y;
+          v[0] = v[0] * x + a * y; v[1] = v[1] * x + b2 * y; v[2] = v[2] * x + c2 * y; v[3] = v[3] * x + d2 * y;
+        };
         if (r < rows) {
-#pragma unroll 2
-          for (int i = lot; i < n; i += lots) {
-            const float* const part = p.parts + ((size_t)(i == 0 ? slot0 : 2 * (w0 + i)) * RB + r) * PART;
-            const float2 head2 = load_shared_f2(part);
-            float2 in[OWN / 2];
+          constexpr int FLY = FLYN;                    // parts on their way together: each is a trip past the caches
+          for (int i0 = lot; i0 < n; i0 += FLY * lots) {
+            float2 ml[FLY], in[FLY][2];
 #pragma unroll
-            for (int x = 0; x < OWN / 2; ++x) in[x] = load_shared_f2(part + 4 + own + 2 * x);
-            const float to = fmaxf(ref, head2.x), a = __builtin_amdgcn_exp2f(ref - to), d = __builtin_amdgcn_exp2f(head2.x - to);
-            ref = to;
-            sum = sum * a + head2.y * d;
-#pragma unroll
-            for (int x = 0; x < OWN / 2; ++x) {
-              v[2 * x] = v[2 * x] * a + in[x].x * d;
-              v[2 * x + 1] = v[2 * x + 1] * a + in[x].y * d;
+            for (int y = 0; y < FLY; ++y) {
+              const int i = min(i0 + y * lots, n - 1);
+              const float* const part = p.parts + ((size_t)(i == 0 ? slot0 : 2 * (w0 + i)) * RB + r) * PART;
+              ml[y] = load_shared_f2(part);
+              in[y][0] = load_shared_f2(part + 4 + own);
+              in[y][1] = load_shared_f2(part + 6 + own);
             }
+#pragma unroll
+            for (int y = 0; y < FLY; ++y)
+              if (i0 + y * lots < n) add(ml[y].x, ml[y].y, in[y][0].x, in[y][0].y, in[y][1].x, in[y][1].y);
           }
         }
         if (lots > 1) {
-          if (own == 0) { m_lds[0][row_of] = ref; l_lds[0][row_of] = sum; }
-#pragma unroll
-          for (int x = 0; x < OWN; ++x) o_lds[0][row_of][own + x] = v[x];
+          float* const lot_rows = &o_lds[0][0][0];       // (as many rows as the wavefronts' sums had)
+          if (own == 0) { join_m[row_of] = ref; join_l[row_of] = sum; }
+          if (lot > 0) *reinterpret_cast<float4*>(lot_rows + (size_t)(row_of - taken) * PITCH + own) = float4{v[0], v[1], v[2], v[3]};
           __syncthreads();
           if (lot == 0 && r < rows) {
             for (int k = 1; k < lots; ++k) {
               const int from = k * taken + sub;
-              const float to = fmaxf(ref, m_lds[0][from]), a = __builtin_amdgcn_exp2f(ref - to), d = __builtin_amdgcn_exp2f(m_lds[0][from] - to);
-              ref = to;
-              sum = sum * a + l_lds[0][from] * d;
-#pragma unroll
-              for (int x = 0; x < OWN; ++x) v[x] = v[x] * a + o_lds[0][from][own + x] * d;
+              const float4 x = *reinterpret_cast<const float4*>(lot_rows + (size_t)(from - taken) * PITCH + own);
+              add(join_m[from], join_l[from], x.x, x.y, x.z, x.w);
             }
           }
         }
@@ -552,7 +678,7 @@ __global__ __launch_bounds__(64 * attn_waves(NB), NB == 1 ? 4 : 2) void attn_kv4
         __syncthreads();
       }
     }
-    at += stop - begin;
+    item += (uint32_t)(OVER + span.steps);
     begin = 0;
     first_run = false;
     if (++head == Hkv) { head = 0; ++entry; }

@@ -834,8 +834,13 @@ inline KvShape kv_shape(const int32_t* pos, const int32_t* page_table, int T, in
   return KvShape{pos, page_table, T, Hkv, log2_exact(page_size), max_pages, n_pages};
 }
 
-// Blocks of 16 rows that a wavefront of the attention carries: as many as the rows of a sequence and key/value head fill, 4 at most.
-inline int attn_row_blocks(int T, int G) { return (long long)T * G <= 16 ? 1 : (long long)T * G <= 32 ? 2 : 4; }
+// The instance for rows = T * G rows of a sequence and key/value head: as many tiles to a block of columns as the rows leave
+// room for, or as many blocks as they fill, 4 at most.
+struct AttnPlan { int nb, f; };
+inline AttnPlan attn_plan(int T, int G) {
+  const long long rows = (long long)T * G;
+  return rows <= 4 ? AttnPlan{1, 4} : rows <= 8 ? AttnPlan{1, 2} : rows <= 16 ? AttnPlan{1, 1} : rows <= 32 ? AttnPlan{2, 1} : AttnPlan{4, 1};
+}
 
 int check_attn(int B, int T, int Hq, int Hkv, int D) {
   if (D != 64 && D != 128) return QSPEC_ERR_SHAPE;
@@ -844,19 +849,29 @@ int check_attn(int B, int T, int Hq, int Hkv, int D) {
   return QSPEC_OK;
 }
 
+template <int D>
+size_t attn_workspace_of(AttnPlan plan) {
+  if (plan.f == 4) return attn_workspace<D, 1, 4>();
+  if (plan.f == 2) return attn_workspace<D, 1, 2>();
+  if (plan.nb == 1) return attn_workspace<D, 1, 1>();
+  return plan.nb == 2 ? attn_workspace<D, 2, 1>() : attn_workspace<D, 4, 1>();
+}
 size_t attn_workspace_bytes(int T, int G, int D) {
-  return kAttnTicketBytes + (size_t)2 * kAttnMaxWorkgroups * 16 * attn_row_blocks(T, G) * attn_part_floats(D) * sizeof(float);
+  return D == 128 ? attn_workspace_of<128>(attn_plan(T, G)) : attn_workspace_of<64>(attn_plan(T, G));
 }
 
-template <int D, int NB>
+template <int D, int NB, int F>
 void launch_attn_inst(const AttnArgs& a, hipStream_t s) {
-  launch_kernel((attn_kv4_kernel<D, NB>), dim3(kAttnMaxWorkgroups), dim3(64 * attn_waves(NB)), 0, s, a);
+  typedef AttnForm<NB, F> Form;
+  launch_kernel((attn_kv4_kernel<D, NB, F>), dim3(Form::workgroups), dim3(64 * Form::waves), 0, s, a);
 }
 template <int D>
-void launch_attn(const AttnArgs& a, int nb, hipStream_t s) {
-  if (nb == 1) launch_attn_inst<D, 1>(a, s);
-  else if (nb == 2) launch_attn_inst<D, 2>(a, s);
-  else launch_attn_inst<D, 4>(a, s);
+void launch_attn(const AttnArgs& a, AttnPlan plan, hipStream_t s) {
+  if (plan.f == 4) launch_attn_inst<D, 1, 4>(a, s);
+  else if (plan.f == 2) launch_attn_inst<D, 1, 2>(a, s);
+  else if (plan.nb == 1) launch_attn_inst<D, 1, 1>(a, s);
+  else if (plan.nb == 2) launch_attn_inst<D, 2, 1>(a, s);
+  else launch_attn_inst<D, 4, 1>(a, s);
 }
 
 int check_sample_shape(int B, int gamma, int V) {
@@ -1280,18 +1295,20 @@ int qspec_attn_kv4(const void* q_f16, const void* cache, const int32_t* pos, con
   if (!(scale >= 1e-10f) || !(scale <= 1e10f) || window < 0 || sinks < 0 || (window == 0 && sinks > 0)) return QSPEC_ERR_SHAPE;
   if (misaligned(q_f16) || misaligned(cache) || misaligned(out_f16) || misaligned(workspace) || misaligned4(pos) || misaligned4(page_table))
     return QSPEC_ERR_ALIGN;
-  const int G = Hq / Hkv, nb = attn_row_blocks(T, G);
+  const int G = Hq / Hkv;
+  const AttnPlan plan = attn_plan(T, G);
+  const int rows = 16 * plan.nb / plan.f;
   if (workspace_bytes < attn_workspace_bytes(T, G, D)) return QSPEC_ERR_WORKSPACE;
-  const long long blocks = ((long long)T * G + 16 * nb - 1) / (16 * nb);
-  // the kernel counts the steps of the call in 32 bits
-  if (B * blocks * Hkv > 0x7fffffffLL / (((long long)max_pages * page_size + kAttnStep - 1) / kAttnStep + 1)) return QSPEC_ERR_SHAPE;
+  const long long blocks = ((long long)T * G + rows - 1) / rows;
+  // the kernel counts the steps of the call in 32 bits (32 tokens and a few dozen for each item at most)
+  if (B * blocks * Hkv > 0x7fffffffLL / ((long long)max_pages * page_size / 32 + 64)) return QSPEC_ERR_SHAPE;
   if (int st = check_device()) return st;
   AttnArgs a{kv_shape(pos, page_table, T, Hkv, page_size, max_pages, n_pages), static_cast<const uint16_t*>(q_f16),
              static_cast<const uint8_t*>(cache), static_cast<uint16_t*>(out_f16), static_cast<unsigned*>(workspace),
              reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + kAttnTicketBytes), B, Hq, G, (int)blocks,
              G > 1 ? (uint32_t)(((1ULL << 32) + G - 1) / G) : 0u, window, sinks, scale * 1.44269504f};
-  if (D == 128) launch_attn<128>(a, nb, static_cast<hipStream_t>(stream));
-  else launch_attn<64>(a, nb, static_cast<hipStream_t>(stream));
+  if (D == 128) launch_attn<128>(a, plan, static_cast<hipStream_t>(stream));
+  else launch_attn<64>(a, plan, static_cast<hipStream_t>(stream));
   return launch_status();
 }
 
