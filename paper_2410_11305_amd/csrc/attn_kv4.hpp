@@ -28,7 +28,7 @@
 namespace qspec {
 
 #ifndef FLYN
-#define FLYN 16
+#define FLYN 4
 #endif
 #ifndef TL4
 #define TL4 4
@@ -563,9 +563,8 @@ __global__ __launch_bounds__((64 * AttnForm<NB, F>::waves), NB == 1 ? S1 : 2) vo
       for (int x = 0; x < 4; ++x) h[x] = (_Float16)(sum > 0.0f ? fminf(fmaxf(v[x] * by, -65504.0f), 65504.0f) : 0.0f);   // (a 15th code may lie past fp16's end)
       *reinterpret_cast<v4h*>(p.out + (((size_t)b * p.kv.T + j) * p.Hq + (size_t)head * p.G + g) * D + own) = h;
     };
-#pragma unroll
-    for (int nb = 0; nb < NB; ++nb) {
-      if (nb * COLS >= rows) break;
+    // (Code that runs once an item comes from memory at every launch: one copy of what can be shared, few unrolled loops.)
+    const auto hand_over = [&](int nb) {
       if (F > 1) {                            // the columns of a row
         const float to = group_max<F>(m[nb]), by = __builtin_amdgcn_exp2f(m[nb] - to);
         m[nb] = to;
@@ -595,6 +594,13 @@ __global__ __launch_bounds__((64 * AttnForm<NB, F>::waves), NB == 1 ? S1 : 2) vo
           }
         }
       }
+    };
+#pragma unroll 1
+    for (int nb = 0; nb < NB && nb * COLS < rows; ++nb) {
+      if (NB == 1 || nb == 0) hand_over(0);
+      else if (NB == 2 || nb == 1) hand_over(NB > 1 ? 1 : 0);
+      else if (nb == 2) hand_over(NB > 2 ? 2 : 0);
+      else hand_over(NB > 2 ? 3 : 0);
       __syncthreads();
       for (int in = row_of; in < COLS; in += THREADS / LANES) {
         const int r = nb * COLS + in;
