@@ -1331,8 +1331,7 @@ int qspec_sample(const void* logits_f16, const float* u, const float* temperatur
   int32_t* const tokens = draft_tokens ? static_cast<int32_t*>(workspace) : out_tokens;
   SampleArgs a{static_cast<const uint16_t*>(logits_f16), u, temperature, top_k, top_p, min_p, tokens, V, gamma + 1};
   const dim3 grid(B * (gamma + 1));
-  if (V % 8 == 0) launch_kernel(sample_kernel<true>, grid, dim3(kSampleThreads), 0, s, a);
-  else launch_kernel(sample_kernel<false>, grid, dim3(kSampleThreads), 0, s, a);
+  launch_kernel(sample_kernel, grid, dim3(kSampleThreads), 0, s, a);
   if (draft_tokens) launch_kernel(accept_tokens_kernel, dim3(B), dim3(64), 0, s, AcceptTokensArgs{tokens, draft_tokens, n_accept, out_tokens, gamma});
   return launch_status();
 }

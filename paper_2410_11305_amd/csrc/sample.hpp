@@ -6,21 +6,24 @@
 // order of the draw (falling logit, the lowest index first among equals), so every limit and the draw itself are decided from the counts and
 // exp((value - max) / temperature) in binary64, whatever order the logits arrived in; only the last step, which of the
 // tokens of one value, looks at indices.  No sort, no passes over candidates, every logit read once for the counts and
-// once more for the index.
+// (rows of up to 32768: from registers) once more for the index.
 //
-// A thread owns 64 neighbouring values, which are equally spaced (64 divides every binade): two exponentials give it all 64 weights.
+// A thread owns a block of 64 neighbouring values, which are equally spaced (64 divides every binade): its weights are a
+// geometric series, two exponentials and one multiply-add a value.  Where something is decided inside a block, every
+// wavefront takes the block a value to a lane, so nothing is walked and nothing handed around.
 #pragma once
 #include "accept.hpp"
 #include "common.hpp"
+#include "producers.hpp"
 
 namespace qspec {
 
 constexpr int kSampleThreads = 1024;
 constexpr int kSampleWaves = kSampleThreads / 64;
-constexpr int kSampleOwn = 64;                                // values of a thread
-constexpr int kSampleCounts = 65535;                          // logits whose counts fit 16 bits, whatever they are
-constexpr int kSampleRound = 8 * kSampleThreads;              // logits of one trip
-constexpr int kSampleMaxV = 256 * kSampleRound;               // a table of 16 counters per trip takes the histogram's place
+constexpr int kSampleRound = 8 * kSampleThreads;              // logits of one trip, 8 to a thread
+constexpr int kSampleKept = 4;                                // trips that stay in registers
+constexpr int kSampleMaxV = 256 * kSampleRound;
+constexpr int kSampleExtras = kSampleMaxV / 32768;            // halves of a counter's range that a row can run over
 
 struct SampleArgs {
   const uint16_t* logits;    // fp16 [rows][V]
@@ -64,17 +67,19 @@ __device__ __forceinline__ double sample_value(uint32_t key) {
   return (double)half_bits_to_float((uint16_t)(key & 0x8000u ? key ^ 0x8000u : key ^ 0xFFFFu));
 }
 
-// Piece i of a row: 8 logits from 8 i on, -inf past the end.  VEC: rows start on 16 bytes and V % 8 == 0.
-template <bool VEC>
+typedef unsigned short v2us __attribute__((ext_vector_type(2)));
+
+// Piece i of a row: 8 logits from 8 i on, -inf past the end.  (Rows start wherever V puts them.)
 __device__ __forceinline__ uint4 sample_piece(const uint16_t* row, int V, int i) {
   uint4 q = {0xFC00FC00u, 0xFC00FC00u, 0xFC00FC00u, 0xFC00FC00u};
-  if (VEC) {
-    if (8 * i < V) q = reinterpret_cast<const uint4*>(row)[i];
-  } else {
-    uint32_t h[8];
+  if (8 * i + 8 <= V) {
+    __builtin_memcpy(&q, row + 8 * i, 16);
+  } else if (8 * i < V) {
+    uint32_t w[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
-    for (int e = 0; e < 8; ++e) h[e] = 8 * i + e < V ? row[8 * i + e] : 0xFC00u;
-    q = uint4{h[0] | h[1] << 16, h[2] | h[3] << 16, h[4] | h[5] << 16, h[6] | h[7] << 16};
+    for (int e = 0; e < 7; ++e)
+      if (8 * i + e < V) w[e >> 1] = e & 1 ? (w[e >> 1] & 0xFFFFu) | (uint32_t)row[8 * i + e] << 16 : (w[e >> 1] & 0xFFFF0000u) | row[8 * i + e];
+    q = uint4{w[0], w[1], w[2], w[3]};
   }
   return q;
 }
@@ -83,223 +88,293 @@ __device__ __forceinline__ uint32_t piece_bits(const uint4& q, int e) {
   return e & 1 ? w[e >> 1] >> 16 : w[e >> 1] & 0xFFFFu;
 }
 
+// Inclusive sum over the lanes up to this one.
+__device__ __forceinline__ uint32_t lane_scan(uint32_t v) {
+#define QSPEC_DPP_ADD(ctrl, rows) v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, ctrl, rows, 0xf, false)
+  QSPEC_DPP_ADD(0x111, 0xf);                  // row_shr 1, 2, 4, 8: inside a row of 16
+  QSPEC_DPP_ADD(0x112, 0xf);
+  QSPEC_DPP_ADD(0x114, 0xf);
+  QSPEC_DPP_ADD(0x118, 0xf);
+  QSPEC_DPP_ADD(0x142, 0xa);                  // row_bcast 15 into rows 1 and 3
+  QSPEC_DPP_ADD(0x143, 0xc);                  // row_bcast 31 into rows 2 and 3
+#undef QSPEC_DPP_ADD
+  return v;
+}
+template <int CTRL, int ROWS>
+__device__ __forceinline__ double dpp_or_zero(double v) {
+  const unsigned long long b = __builtin_bit_cast(unsigned long long, v);
+  const unsigned lo = (unsigned)__builtin_amdgcn_update_dpp(0, (int)(unsigned)b, CTRL, ROWS, 0xf, false);
+  const unsigned hi = (unsigned)__builtin_amdgcn_update_dpp(0, (int)(unsigned)(b >> 32), CTRL, ROWS, 0xf, false);
+  return __builtin_bit_cast(double, ((unsigned long long)hi << 32) | lo);
+}
+__device__ __forceinline__ double lane_scan(double v) {
+  v += dpp_or_zero<0x111, 0xf>(v);
+  v += dpp_or_zero<0x112, 0xf>(v);
+  v += dpp_or_zero<0x114, 0xf>(v);
+  v += dpp_or_zero<0x118, 0xf>(v);
+  v += dpp_or_zero<0x142, 0xa>(v);
+  v += dpp_or_zero<0x143, 0xc>(v);
+  return v;
+}
+
 // grid rows.
-template <bool VEC>
 __global__ __launch_bounds__(kSampleThreads) void sample_kernel(SampleArgs p) {
-  __shared__ uint32_t hist[32768];                            // two values' counts a word
-  __shared__ uint32_t wave_u[kSampleWaves];
+  __shared__ __align__(16) uint32_t hist[32768];              // two values' counts a word
+  __shared__ uint32_t extra[kSampleExtras];                   // values that stand for 32768 tokens more, each time they are named
+  __shared__ uint32_t extras;
+  __shared__ uint32_t wave_u[3][kSampleWaves];
   __shared__ double wave_d[kSampleWaves];
-  __shared__ double shared_mass;
-  __shared__ uint32_t shared_key, shared_rank;
+  __shared__ uint32_t border[4], border_before[4];            // blocks in which something is decided, and the tokens before them
+  __shared__ double border_mass[4];                           // ... and the mass
+  __shared__ uint32_t cell_found[2];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int r = blockIdx.x, b = r / p.per;
   const uint16_t* const row = p.logits + (size_t)r * p.V;
-  const int own = kSampleThreads - 1 - tid;                   // block of values, the largest first
-  // (word i of a block stands at i ^ block: a wavefront reads 32 blocks at once without meeting in a bank)
-  const auto word_of = [](uint32_t d) { return (d & ~31u) | ((d ^ (d >> 5)) & 31u); };
+  const uint32_t own = kSampleThreads - 1 - tid;              // this thread's block, the largest values first
+  const int pieces = (p.V + 7) / 8, trips = (pieces + kSampleThreads - 1) / kSampleThreads;
+  // (16 bytes c of a block stand at c ^ block: 8 threads read 8 blocks without meeting in a bank)
+  const auto place_of = [](uint32_t word) { return (word & ~28u) | ((word ^ (word >> 3)) & 28u); };
+  const auto count_of = [&](uint32_t key) {
+    const uint32_t w = hist[place_of(key >> 1)];
+    uint32_t n = key & 1u ? w >> 16 : w & 0xFFFFu;
+    for (uint32_t i = 0; i < extras; ++i) n += extra[i] == key ? 32768u : 0u;
+    return n;
+  };
 
   // ---- counts
+  uint4 kept[kSampleKept];
 #pragma unroll
-  for (int i = 0; i < 32; ++i) hist[i * kSampleThreads + tid] = 0u;
-  uint32_t count[kSampleOwn];
+  for (int t = 0; t < kSampleKept; ++t) kept[t] = sample_piece(row, p.V, t * kSampleThreads + tid);
 #pragma unroll
-  for (int i = 0; i < kSampleOwn; ++i) count[i] = 0u;
+  for (int i = 0; i < 8; ++i) reinterpret_cast<uint4*>(hist)[i * kSampleThreads + tid] = uint4{0u, 0u, 0u, 0u};
+  if (tid == 0) extras = 0;
+  if (tid < 4) border[tid] = 0xFFFFFFFFu;
   __syncthreads();
-  const int pieces = (p.V + 7) / 8;
-  for (int base = 0; base < pieces; base += kSampleCounts / 8) {
-    const int end = min(pieces, base + kSampleCounts / 8);
-    for (int i = base + tid; i < end; i += kSampleThreads) {
-      const uint4 q = sample_piece<VEC>(row, p.V, i);
+  uint32_t counted = 0;
+  const auto count_piece = [&](const uint4& q) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const uint32_t key = sample_key(piece_bits(q, e));
-        if (key) atomicAdd(&hist[word_of(key >> 1)], key & 1u ? 0x10000u : 1u);
+    for (int e = 0; e < 8; ++e) {
+      const uint32_t key = sample_key(piece_bits(q, e));
+      if (key) {
+        atomicAdd(&hist[place_of(key >> 1)], key & 1u ? 0x10000u : 1u);
+        ++counted;
       }
     }
-    __syncthreads();
+  };
 #pragma unroll
-    for (int i = 0; i < 32; ++i) {
-      uint32_t* const w = &hist[own * 32 + ((i ^ own) & 31)];
-      count[2 * i] += *w & 0xFFFFu;
-      count[2 * i + 1] += *w >> 16;
-      *w = 0u;
+  for (int t = 0; t < kSampleKept; ++t) count_piece(kept[t]);
+#pragma unroll 2
+  for (int t = kSampleKept; t < trips; ++t) count_piece(sample_piece(row, p.V, t * kSampleThreads + tid));
+  __syncthreads();
+  // this thread's 64 values: words in the order of the values
+  const auto own_words = [&](int c) { return reinterpret_cast<const uint4*>(hist)[own * 8 + (c ^ (own & 7u))]; };
+  const auto sum_own = [&] {
+    uint32_t n = 0;
+#pragma unroll
+    for (int c = 0; c < 8; ++c) {
+      const uint4 w = own_words(c);
+      n = __builtin_amdgcn_udot2(__builtin_bit_cast(v2us, w.x), v2us{1, 1}, n, false);
+      n = __builtin_amdgcn_udot2(__builtin_bit_cast(v2us, w.y), v2us{1, 1}, n, false);
+      n = __builtin_amdgcn_udot2(__builtin_bit_cast(v2us, w.z), v2us{1, 1}, n, false);
+      n = __builtin_amdgcn_udot2(__builtin_bit_cast(v2us, w.w), v2us{1, 1}, n, false);
     }
+    return n;
+  };
+  uint32_t here = sum_own();
+  uint32_t upto = lane_scan(here);
+  if (lane == 63) {
+    wave_u[0][wave] = upto;
+    wave_u[1][wave] = 0;
+  }
+  const uint32_t seen_wave = lane_scan(counted);
+  if (lane == 63) wave_u[1][wave] = seen_wave;
+  __syncthreads();
+  uint32_t before = upto - here, tokens = 0, seen = 0;
+  for (int w = 0; w < kSampleWaves; ++w) {
+    before += w < wave ? wave_u[0][w] : 0u;
+    tokens += wave_u[0][w];
+    seen += wave_u[1][w];
+  }
+  if (tokens != seen) {
+    // A counter ran over (more than 65535 equal logits; every overflow loses counts, so it shows in the sum).  Again, 32768
+    // tokens at a time, each time taking 32768 off the counters that have them.
     __syncthreads();
-  }
-
-  // ---- the largest value, and how many tokens come before this thread's
-  uint32_t here = 0, top = 0;
 #pragma unroll
-  for (int i = 0; i < kSampleOwn; ++i) {
-    here += count[i];
-    if (count[i]) top = (uint32_t)(own * kSampleOwn + i);
+    for (int i = 0; i < 8; ++i) reinterpret_cast<uint4*>(hist)[i * kSampleThreads + tid] = uint4{0u, 0u, 0u, 0u};
+    __syncthreads();
+    for (int t0 = 0; t0 < trips; t0 += 4) {
+      for (int t = t0; t < min(trips, t0 + 4); ++t) count_piece(sample_piece(row, p.V, t * kSampleThreads + tid));
+      __syncthreads();
+      for (uint32_t key = own * 64; key < own * 64 + 64; ++key) {
+        uint32_t* const w = &hist[place_of(key >> 1)];
+        const uint32_t bit = key & 1u ? 0x80000000u : 0x8000u;
+        if (*w & bit) {
+          *w -= bit;
+          extra[atomicAdd(&extras, 1u)] = key;
+        }
+      }
+      __syncthreads();
+    }
+    here = sum_own();
+    for (uint32_t i = 0; i < extras; ++i) here += extra[i] >> 6 == own ? 32768u : 0u;
+    upto = lane_scan(here);
+    if (lane == 63) wave_u[0][wave] = upto;
+    __syncthreads();
+    before = upto - here;
+    for (int w = 0; w < wave; ++w) before += wave_u[0][w];
   }
-  top = wave_max_u32(top);
-  if (lane == 0) wave_u[wave] = top;
-  __syncthreads();
-  for (int w = 0; w < kSampleWaves; ++w) top = max(top, wave_u[w]);
-  __syncthreads();
-  if (top == 0) {                                             // nothing to choose from
+  if (seen == 0) {                                            // nothing to choose from
     if (tid == 0) p.tokens[r] = -1;
     return;
   }
-  uint32_t upto = here;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const uint32_t up = __shfl_up(upto, d);
-    if (lane >= d) upto += up;
-  }
-  if (lane == 63) wave_u[wave] = upto;
-  __syncthreads();
-  uint32_t before = upto - here;
-  for (int w = 0; w < wave; ++w) before += wave_u[w];
 
-  // ---- this thread's part of the mass
+  // ---- the largest value: in the first block that has any
+  if (here && before == 0) border[3] = own;
+  __syncthreads();
+  const uint32_t top_block = border[3];
+  const uint64_t any = __builtin_amdgcn_ballot_w64(count_of(top_block * 64 + 63 - lane) != 0);
+  const uint32_t top = top_block * 64 + 63 - (uint32_t)__builtin_ctzll(any);
+
   const float temperature = p.temperature ? p.temperature[b] : 1.0f;
   const bool greedy = !(temperature > 0.0f);
   const uint32_t k = greedy ? 1u : p.top_k && p.top_k[b] > 0 ? (uint32_t)p.top_k[b] : 0xFFFFFFFFu;
   const double least = p.min_p && p.min_p[b] > 0.0f ? fmin((double)p.min_p[b], 1.0) : 0.0;
+  const float share = p.top_p ? p.top_p[b] : 1.0f;
+  const double u = (double)fminf(fmaxf(p.u[r], 0.0f), 0.99999994f);
   const double inverse = greedy ? 0.0 : 1.0 / (double)temperature;
   const double top_value = sample_value(top);
-  const bool infinite = top == 0xFC00u;                        // +inf: the others weigh nothing beside it
-  const uint32_t high = min((uint32_t)(own * kSampleOwn + kSampleOwn - 1), top);
-  double first = 0.0, ratio = 0.0;
-  if (here && before < k) {
-    first = high == top ? 1.0 : infinite ? 0.0 : exp_negative((sample_value(high) - top_value) * inverse);
-    ratio = infinite ? 0.0 : exp_negative((sample_value(own * kSampleOwn) - sample_value(own * kSampleOwn + 1)) * inverse);
-  }
-  // f(value, tokens of it, weight) for this thread's values from the largest on, within top_k and min_p, until it returns true
-  const auto walk = [&](auto f) {
-    double w = first;
-    uint32_t at = before;
-#pragma unroll
-    for (int i = kSampleOwn - 1; i >= 0; --i) {
-      const uint32_t key = (uint32_t)(own * kSampleOwn + i);
-      if (key <= high) {
-        const uint32_t n = at >= k ? 0u : min(count[i], k - at);
-        if (n && w > 0.0 && !(w < least)) {
-          if (f(key, n, w)) return;
-        }
-        at += count[i];
-        w *= ratio;
-      }
-    }
+  // (beside +inf the others weigh nothing)
+  const auto weight_of = [&](uint32_t key) {
+    return key == top ? 1.0 : top == 0xFC00u ? 0.0 : exp_negative((sample_value(key) - top_value) * inverse);
   };
+
+  // ---- this thread's part of the mass: its largest value's weight times a polynomial in the ratio of neighbours
   double mass = 0.0;
-  if (here && before < k) walk([&](uint32_t, uint32_t n, double w) { mass = fma((double)n, w, mass); return false; });
-  double sum = mass;
+  const bool in = here && before < k;
+  if (in) {
+    const uint32_t low = own * 64, high = min(low + 63u, top);
+    const double first = weight_of(high), ratio = top == 0xFC00u ? 0.0 : exp_negative((sample_value(low) - sample_value(low + 1)) * inverse);
+    const bool all = !(least > 0.0) || weight_of(low) >= least;
+    if (all && before + here <= k) {
+      for (int c = 0; c < 8; ++c) {
+        const uint4 w4 = own_words(c);
+        const uint32_t w[4] = {w4.x, w4.y, w4.z, w4.w};
 #pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const double up = __shfl_up(sum, d);
-    if (lane >= d) sum += up;
+        for (int e = 0; e < 8; ++e) {
+          const uint32_t key = low + 8 * c + e;
+          const uint32_t n = extras ? count_of(key) : e & 1 ? w[e >> 1] >> 16 : w[e >> 1] & 0xFFFFu;
+          mass = key <= high ? fma(mass, ratio, (double)n) : mass;
+        }
+      }
+      mass *= first;
+    } else if (first >= least) {              // cut inside, by top_k or min_p: at most two such blocks
+      const int slot = before + here > k ? 0 : 1;
+      border[slot] = own;
+      border_before[slot] = before;
+    }
   }
+  __syncthreads();
+  // A block, a value to a lane: how many of its tokens are within top_k and min_p, their weight, and the mass up to them.
+  struct Block { uint32_t key, n; double weight, upto; };
+  const auto block_of = [&](uint32_t block, uint32_t tokens_before, double mass_before) {
+    Block x;
+    x.key = block * 64 + 63 - lane;
+    const uint32_t n = x.key <= top ? count_of(x.key) : 0u;
+    const uint32_t at = tokens_before + lane_scan(n) - n;
+    x.weight = n ? weight_of(x.key) : 0.0;
+    x.n = at >= k || x.weight < least ? 0u : min(n, k - at);
+    x.upto = mass_before + lane_scan((double)x.n * x.weight);
+    return x;
+  };
+#pragma unroll 1
+  for (int slot = 0; slot < 2; ++slot) {
+    const uint32_t block = border[slot];
+    if (block != 0xFFFFFFFFu) {
+      const double cut = lane_value_f64(block_of(block, border_before[slot], 0.0).upto, 63);
+      if (block == own) mass = cut;
+    }
+  }
+  const double sum = lane_scan(mass);
   if (lane == 63) wave_d[wave] = sum;
   __syncthreads();
   double wave_base = 0.0, total = 0.0;
   for (int w = 0; w < kSampleWaves; ++w) {
-    if (w == wave) wave_base = total;
+    wave_base = w == wave ? total : wave_base;
     total += wave_d[w];
   }
-  const double up = __shfl_up(sum, 1);
-  const double from = lane ? wave_base + up : wave_base, to = wave_base + sum;     // (to is the next thread's from, bit for bit)
+  const double shifted = __shfl_up(sum, 1);
+  const double from = lane ? wave_base + shifted : wave_base, to = wave_base + sum;     // (to is the next thread's from, bit for bit)
 
-  // ---- top-p: the shortest beginning that holds this much
-  const float share = p.top_p ? p.top_p[b] : 1.0f;
-  double kept = total;
+  // ---- top-p: the shortest beginning that holds this much (one token at least)
+  double kept_mass = total;
   if (share < 1.0f) {
-    const double limit = fmax((double)share * total, 1e-300);              // (the first token is always kept)
-    if (from < limit && limit <= to) {
-      double cum = from, cut = from;
-      walk([&](uint32_t, uint32_t n, double w) {
-        const double all = fma((double)n, w, cum);
-        cut = all;
-        if (all >= limit) {
-          cut = fma(fmin(fmax(ceil((limit - cum) / w), 1.0), (double)n), w, cum);
-          return true;
-        }
-        cum = all;
-        return false;
-      });
-      shared_mass = cut;
-    }
+    const double limit = fmax((double)share * total, 1e-300);
+    if (from < limit && limit <= to) { border[2] = own; border_before[2] = before; border_mass[2] = from; }
     __syncthreads();
-    kept = shared_mass;
+    const Block x = block_of(border[2], border_before[2], border_mass[2]);
+    // the value in which the mass is reached; rounding may leave that to the last one
+    const uint64_t hit = __builtin_amdgcn_ballot_w64(x.n && x.upto >= limit), have = __builtin_amdgcn_ballot_w64(x.n && x.weight > 0.0);
+    const int at = hit ? __builtin_ctzll(hit) : 63 - __builtin_clzll(have | 1ull);
+    const double start = x.upto - (double)x.n * x.weight;
+    const double cut = hit ? fma(fmin(fmax(ceil((limit - start) / x.weight), 1.0), (double)x.n), x.weight, start) : x.upto;
+    kept_mass = lane_value_f64(cut, at);
   }
 
   // ---- the draw
-  const double u = (double)fminf(fmaxf(p.u[r], 0.0f), 0.99999994f);
-  const double target = u * kept;
-  if (from <= target && target < to) {
-    double cum = from;
-    uint32_t key = 0, rank = 0;
-    walk([&](uint32_t v, uint32_t n, double w) {
-      const double all = fma((double)n, w, cum);
-      key = v;
-      rank = min((uint32_t)fmin((target - cum) / w, 4e9), n - 1);
-      cum = all;
-      return all > target;
-    });
-    shared_key = key;
-    shared_rank = rank;
-  }
+  const double target = u * kept_mass;
+  if (from <= target && target < to) { border[3] = own; border_before[3] = before; border_mass[3] = from; }
   __syncthreads();
-  const uint32_t key = shared_key, rank = shared_rank;
+  const Block x = block_of(border[3], border_before[3], border_mass[3]);
+  const uint64_t hit = __builtin_amdgcn_ballot_w64(x.n && x.upto > target), have = __builtin_amdgcn_ballot_w64(x.n && x.weight > 0.0);
+  const int at = hit ? __builtin_ctzll(hit) : 63 - __builtin_clzll(have | 1ull);
+  const double into = fmax(target - (x.upto - (double)x.n * x.weight), 0.0) / x.weight;
+  const uint32_t key = (uint32_t)__builtin_amdgcn_readlane((int)x.key, at);
+  const uint32_t rank = (uint32_t)__builtin_amdgcn_readlane((int)(x.n ? min((uint32_t)fmin(into, 4e9), x.n - 1) : 0u), at);
 
   // ---- which of the tokens of that value: matches of every wavefront and trip, in the order of the indices
+  __syncthreads();
   uint32_t* const table = hist;
-  const int trips = (pieces + kSampleThreads - 1) / kSampleThreads;
-  for (int t = 0; t < trips; ++t) {
-    const uint4 q = sample_piece<VEC>(row, p.V, t * kSampleThreads + tid);
-    uint32_t n = 0;
+  for (int i = tid; i < trips * kSampleWaves; i += kSampleThreads) table[i] = 0u;
+  __syncthreads();
+  const auto matches = [&](const uint4& q) {
+    uint32_t found = 0;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) n += (uint32_t)__popcll(__ballot(sample_key(piece_bits(q, e)) == key));
-    if (lane == 0) table[t * kSampleWaves + wave] = n;
-  }
+    for (int e = 0; e < 8; ++e) found |= sample_key(piece_bits(q, e)) == key ? 1u << e : 0u;
+    return found;
+  };
+  const auto note = [&](int t, const uint4& q) {
+    const uint32_t found = matches(q);
+    if (found) atomicAdd(&table[t * kSampleWaves + wave], (uint32_t)__popc(found));
+  };
+#pragma unroll
+  for (int t = 0; t < kSampleKept; ++t)
+    if (t < trips) note(t, kept[t]);
+#pragma unroll 2
+  for (int t = kSampleKept; t < trips; ++t) note(t, sample_piece(row, p.V, t * kSampleThreads + tid));
   __syncthreads();
   if (wave == 0) {
     const int cells = trips * kSampleWaves, per = (cells + 63) / 64;
     uint32_t n = 0;
     for (int i = 0; i < per; ++i) n += lane * per + i < cells ? table[lane * per + i] : 0u;
-    uint32_t sum_n = n;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-      const uint32_t below = __shfl_up(sum_n, d);
-      if (lane >= d) sum_n += below;
-    }
-    uint32_t at = sum_n - n;
-    if (at <= rank && rank < sum_n) {
+    const uint32_t sum_n = lane_scan(n);
+    uint32_t before_n = sum_n - n;
+    if (before_n <= rank && rank < sum_n) {
       int i = lane * per;
-      while (at + table[i] <= rank) at += table[i++];
-      wave_u[0] = (uint32_t)i;
-      wave_u[1] = rank - at;
+      while (before_n + table[i] <= rank) before_n += table[i++];
+      cell_found[0] = (uint32_t)i;
+      cell_found[1] = rank - before_n;
     }
   }
   __syncthreads();
-  const int cell = (int)wave_u[0];
+  const int cell = (int)cell_found[0];
   if (wave == (cell & (kSampleWaves - 1))) {
     const int piece = cell / kSampleWaves * kSampleThreads + tid;
-    const uint4 q = sample_piece<VEC>(row, p.V, piece);
-    uint32_t n = 0;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) n += sample_key(piece_bits(q, e)) == key ? 1u : 0u;
-    uint32_t sum_n = n;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-      const uint32_t below = __shfl_up(sum_n, d);
-      if (lane >= d) sum_n += below;
-    }
-    uint32_t left = wave_u[1];
+    uint32_t found = matches(sample_piece(row, p.V, piece));
+    const uint32_t n = (uint32_t)__popc(found), sum_n = lane_scan(n);
+    uint32_t left = cell_found[1];
     if (sum_n - n <= left && left < sum_n) {
-      left -= sum_n - n;
-      int found = 0;
-#pragma unroll
-      for (int e = 7; e >= 0; --e) {
-        // matches of this piece before element e
-        uint32_t first_of = 0;
-        for (int i = 0; i < e; ++i) first_of += sample_key(piece_bits(q, i)) == key ? 1u : 0u;
-        if (sample_key(piece_bits(q, e)) == key && first_of == left) found = e;
-      }
-      p.tokens[r] = 8 * piece + found;
+      for (left -= sum_n - n; left; --left) found &= found - 1;        // the lowest set bit off
+      p.tokens[r] = 8 * piece + __builtin_ctz(found);
     }
   }
 }

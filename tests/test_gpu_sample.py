@@ -78,6 +78,23 @@ def test_equal_logits_walk_by_index(env, V):
     assert run(env, logits, u, top_k=[1, 2, 8, V + 5])[1].tolist() == [[0, 0], [1, 1], [2, 4], [V - 1, V // 2]]
 
 
+def test_more_equal_logits_than_a_counter_holds(env):
+    """Rows of 70000 to 400000 logits of which one or two values make up nearly everything: past 65535, past 131071, both
+    halves of a counter word, and exactly at the border."""
+    for V, values, shares in ((65536, (1.5,), (1.0,)), (65535, (1.5,), (1.0,)), (140000, (0.25, 0.25048828125), (0.5, 0.5)), (400000, (-2.0, 3.0), (0.6, 0.39)),
+                              (131072, (0.0,), (1.0,)), (200001, (5.0, -7.0), (0.001, 0.99))):
+        rng = np.random.default_rng(V)
+        row = np.full(V, values[0], dtype=np.float16)
+        pick = rng.random(V)
+        if len(values) > 1:
+            row[pick >= shares[0]] = values[1]
+            row[pick >= sum(shares)] = rng.standard_normal(int((pick >= sum(shares)).sum()))
+        u = np.r_[0.0, rng.random(1), 1.0 - 2.0 ** -24]
+        logits = np.broadcast_to(row, (1, 3, V)).copy()
+        for p in (dict(), dict(top_p=[0.37]), dict(top_k=[V // 2 + 1]), dict(min_p=[0.5], top_p=[0.9], temperature=[0.7])):
+            assert (run(env, logits, u[None], **p)[1] == want(logits, u[None], **p)).all(), (V, p)
+
+
 def test_all_values_of_fp16(env):
     """One token of every finite value, hot and cold, from both ends."""
     bits = np.arange(65536, dtype=np.uint16)
