@@ -6,7 +6,7 @@
 // order of the draw (falling logit, the lowest index first among equals), so every limit and the draw itself are decided from the counts and
 // exp((value - max) / temperature) in binary64, whatever order the logits arrived in; only the last step, which of the
 // tokens of one value, looks at indices.  No sort, no passes over candidates, every logit read once for the counts and
-// (rows of up to 32768: from registers) once more for the index.
+// (rows of up to 65536: from registers) once more for the index.
 //
 // A thread owns a block of 64 neighbouring values, which are equally spaced (64 divides every binade): its weights are a
 // geometric series, two exponentials and one multiply-add a value.  Where something is decided inside a block, every
@@ -21,7 +21,7 @@ namespace qspec {
 constexpr int kSampleThreads = 1024;
 constexpr int kSampleWaves = kSampleThreads / 64;
 constexpr int kSampleRound = 8 * kSampleThreads;              // logits of one trip, 8 to a thread
-constexpr int kSampleKept = 4;                                // trips that stay in registers
+constexpr int kSampleKept = 8;                                // trips that stay in registers
 constexpr int kSampleMaxV = 256 * kSampleRound;
 constexpr int kSampleExtras = kSampleMaxV / 32768;            // halves of a counter's range that a row can run over
 
@@ -59,13 +59,12 @@ __device__ inline double exp_negative(double x) {
   return __builtin_amdgcn_ldexp(e, (int)n);
 }
 
-// Order of the values as 16 bits (half_order_key); 0 for what cannot be drawn, -inf and NaN.
-__device__ __forceinline__ uint32_t sample_key(uint32_t bits) {
-  return (bits & 0x7FFFu) > 0x7C00u || bits == 0xFC00u ? 0u : half_order_key(bits);
-}
+// Values by number, in their order (half_order_key): 0x8000 + magnitude bits, 0x7FFF - magnitude bits for negative ones;
+// 0x7FFF is -0, whose tokens count as those of 0x8000.  64 neighbours from a multiple of 64 on are equally spaced.
 __device__ __forceinline__ double sample_value(uint32_t key) {
   return (double)half_bits_to_float((uint16_t)(key & 0x8000u ? key ^ 0x8000u : key ^ 0xFFFFu));
 }
+constexpr int kNumber = 0x3F8;                                // v_cmp_class: everything but NaN and -inf
 
 typedef unsigned short v2us __attribute__((ext_vector_type(2)));
 
@@ -83,11 +82,6 @@ __device__ __forceinline__ uint4 sample_piece(const uint16_t* row, int V, int i)
   }
   return q;
 }
-__device__ __forceinline__ uint32_t piece_bits(const uint4& q, int e) {
-  const uint32_t w[4] = {q.x, q.y, q.z, q.w};
-  return e & 1 ? w[e >> 1] >> 16 : w[e >> 1] & 0xFFFFu;
-}
-
 // Inclusive sum over the lanes up to this one.
 __device__ __forceinline__ uint32_t lane_scan(uint32_t v) {
 #define QSPEC_DPP_ADD(ctrl, rows) v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, ctrl, rows, 0xf, false)
@@ -132,11 +126,17 @@ __global__ __launch_bounds__(kSampleThreads) void sample_kernel(SampleArgs p) {
   const uint16_t* const row = p.logits + (size_t)r * p.V;
   const uint32_t own = kSampleThreads - 1 - tid;              // this thread's block, the largest values first
   const int pieces = (p.V + 7) / 8, trips = (pieces + kSampleThreads - 1) / kSampleThreads;
-  // (16 bytes c of a block stand at c ^ block: 8 threads read 8 blocks without meeting in a bank)
-  const auto place_of = [](uint32_t word) { return (word & ~28u) | ((word ^ (word >> 3)) & 28u); };
+  // The counter of a value is a half of its magnitude's word, the upper one for negative values: counting takes the bits of
+  // a logit as they are.  16 bytes c of 64 words stand at c ^ (the number of the 64): threads that read neighbouring
+  // blocks do not meet in a bank.
+  const auto place_of = [](uint32_t byte) { return byte ^ ((byte >> 4) & 0x70u); };
+  uint8_t* const bytes = reinterpret_cast<uint8_t*>(hist);
   const auto count_of = [&](uint32_t key) {
-    const uint32_t w = hist[place_of(key >> 1)];
-    uint32_t n = key & 1u ? w >> 16 : w & 0xFFFFu;
+    const bool below = key < 0x8000u;
+    const uint32_t w = *reinterpret_cast<const uint32_t*>(bytes + place_of((below ? 0x7FFFu - key : key - 0x8000u) * 4));
+    uint32_t n = below ? w >> 16 : w & 0xFFFFu;
+    if (key == 0x8000u) n += w >> 16;
+    if (key == 0x7FFFu) n = 0;
     for (uint32_t i = 0; i < extras; ++i) n += extra[i] == key ? 32768u : 0u;
     return n;
   };
@@ -144,7 +144,8 @@ __global__ __launch_bounds__(kSampleThreads) void sample_kernel(SampleArgs p) {
   // ---- counts
   uint4 kept[kSampleKept];
 #pragma unroll
-  for (int t = 0; t < kSampleKept; ++t) kept[t] = sample_piece(row, p.V, t * kSampleThreads + tid);
+  for (int t = 0; t < kSampleKept; ++t)
+    if (t < trips) kept[t] = sample_piece(row, p.V, t * kSampleThreads + tid);
 #pragma unroll
   for (int i = 0; i < 8; ++i) reinterpret_cast<uint4*>(hist)[i * kSampleThreads + tid] = uint4{0u, 0u, 0u, 0u};
   if (tid == 0) extras = 0;
@@ -152,44 +153,60 @@ __global__ __launch_bounds__(kSampleThreads) void sample_kernel(SampleArgs p) {
   __syncthreads();
   uint32_t counted = 0;
   const auto count_piece = [&](const uint4& q) {
+    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      const uint32_t key = sample_key(piece_bits(q, e));
-      if (key) {
-        atomicAdd(&hist[place_of(key >> 1)], key & 1u ? 0x10000u : 1u);
+      const uint32_t x = w[e >> 1];
+      const uint32_t byte = e & 1 ? x >> 14 & 0x1FFFCu : x << 2 & 0x1FFFCu;
+      const uint32_t one = max(e & 1 ? x >> 15 & 0x10000u : x << 1 & 0x10000u, 1u);
+      if (__builtin_amdgcn_classh(__builtin_bit_cast(v2h, x)[e & 1], kNumber)) {
+        atomicAdd(reinterpret_cast<uint32_t*>(bytes + place_of(byte)), one);
         ++counted;
       }
     }
   };
 #pragma unroll
-  for (int t = 0; t < kSampleKept; ++t) count_piece(kept[t]);
-#pragma unroll 2
-  for (int t = kSampleKept; t < trips; ++t) count_piece(sample_piece(row, p.V, t * kSampleThreads + tid));
+  for (int t = 0; t < kSampleKept; ++t)
+    if (t < trips) count_piece(kept[t]);
+  const auto further = [&](int t0, int t1, auto f) {          // trips that are not kept, four on their way together
+    for (int t = t0; t < t1; t += 4) {
+      uint4 q[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) q[i] = sample_piece(row, p.V, (t + i) * kSampleThreads + tid);    // (past the end: -inf)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) f(t + i, q[i]);
+    }
+  };
+  further(kSampleKept, trips, [&](int, const uint4& q) { count_piece(q); });
   __syncthreads();
-  // this thread's 64 values: words in the order of the values
-  const auto own_words = [&](int c) { return reinterpret_cast<const uint4*>(hist)[own * 8 + (c ^ (own & 7u))]; };
+  // this thread's 64 values: 64 words, upwards or (negative values; the upper half of the wavefronts) downwards
+  const bool negative = own < 512u;
+  const uint32_t group = negative ? 511u - own : own - 512u;
+  const auto own_words = [&](uint32_t c) { return *reinterpret_cast<const uint4*>(bytes + (group * 256 + ((c ^ (group & 7u)) << 4))); };
   const auto sum_own = [&] {
     uint32_t n = 0;
-#pragma unroll
-    for (int c = 0; c < 8; ++c) {
+    const v2us half = negative ? v2us{0, 1} : v2us{1, 0};
+#pragma unroll 4
+    for (uint32_t c = 0; c < 16; ++c) {
       const uint4 w = own_words(c);
-      n = __builtin_amdgcn_udot2(__builtin_bit_cast(v2us, w.x), v2us{1, 1}, n, false);
-      n = __builtin_amdgcn_udot2(__builtin_bit_cast(v2us, w.y), v2us{1, 1}, n, false);
-      n = __builtin_amdgcn_udot2(__builtin_bit_cast(v2us, w.z), v2us{1, 1}, n, false);
-      n = __builtin_amdgcn_udot2(__builtin_bit_cast(v2us, w.w), v2us{1, 1}, n, false);
+      n = __builtin_amdgcn_udot2(__builtin_bit_cast(v2us, w.x), half, n, false);
+      n = __builtin_amdgcn_udot2(__builtin_bit_cast(v2us, w.y), half, n, false);
+      n = __builtin_amdgcn_udot2(__builtin_bit_cast(v2us, w.z), half, n, false);
+      n = __builtin_amdgcn_udot2(__builtin_bit_cast(v2us, w.w), half, n, false);
     }
+    if (group == 0) n = negative ? n - (hist[0] >> 16) : n + (hist[0] >> 16);        // -0 counts as 0
     return n;
   };
   uint32_t here = sum_own();
   uint32_t upto = lane_scan(here);
+  const uint32_t seen_wave = lane_scan(counted);
   if (lane == 63) {
     wave_u[0][wave] = upto;
-    wave_u[1][wave] = 0;
+    wave_u[1][wave] = seen_wave;
   }
-  const uint32_t seen_wave = lane_scan(counted);
-  if (lane == 63) wave_u[1][wave] = seen_wave;
   __syncthreads();
   uint32_t before = upto - here, tokens = 0, seen = 0;
+#pragma unroll
   for (int w = 0; w < kSampleWaves; ++w) {
     before += w < wave ? wave_u[0][w] : 0u;
     tokens += wave_u[0][w];
@@ -203,14 +220,15 @@ __global__ __launch_bounds__(kSampleThreads) void sample_kernel(SampleArgs p) {
     for (int i = 0; i < 8; ++i) reinterpret_cast<uint4*>(hist)[i * kSampleThreads + tid] = uint4{0u, 0u, 0u, 0u};
     __syncthreads();
     for (int t0 = 0; t0 < trips; t0 += 4) {
-      for (int t = t0; t < min(trips, t0 + 4); ++t) count_piece(sample_piece(row, p.V, t * kSampleThreads + tid));
+      further(t0, min(trips, t0 + 4), [&](int, const uint4& q) { count_piece(q); });
       __syncthreads();
-      for (uint32_t key = own * 64; key < own * 64 + 64; ++key) {
-        uint32_t* const w = &hist[place_of(key >> 1)];
-        const uint32_t bit = key & 1u ? 0x80000000u : 0x8000u;
+      for (uint32_t i = 0; i < 64; ++i) {
+        const uint32_t magnitude = group * 64 + i;
+        uint32_t* const w = reinterpret_cast<uint32_t*>(bytes + place_of(magnitude * 4));
+        const uint32_t bit = negative ? 0x80000000u : 0x8000u;
         if (*w & bit) {
-          *w -= bit;
-          extra[atomicAdd(&extras, 1u)] = key;
+          atomicSub(w, bit);                                   // (the other half is another thread's)
+          extra[atomicAdd(&extras, 1u)] = negative && magnitude ? 0x7FFFu - magnitude : 0x8000u + magnitude;
         }
       }
       __syncthreads();
@@ -256,14 +274,20 @@ __global__ __launch_bounds__(kSampleThreads) void sample_kernel(SampleArgs p) {
     const double first = weight_of(high), ratio = top == 0xFC00u ? 0.0 : exp_negative((sample_value(low) - sample_value(low + 1)) * inverse);
     const bool all = !(least > 0.0) || weight_of(low) >= least;
     if (all && before + here <= k) {
-      for (int c = 0; c < 8; ++c) {
-        const uint4 w4 = own_words(c);
-        const uint32_t w[4] = {w4.x, w4.y, w4.z, w4.w};
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const uint32_t key = low + 8 * c + e;
-          const uint32_t n = extras ? count_of(key) : e & 1 ? w[e >> 1] >> 16 : w[e >> 1] & 0xFFFFu;
-          mass = key <= high ? fma(mass, ratio, (double)n) : mass;
+      const uint32_t steps = high - low;      // from the least value up to the largest one that counts
+      const uint32_t shift = negative ? 16u : 0u;
+      const auto add = [&](uint32_t i, uint32_t n) { mass = i <= steps ? fma(mass, ratio, (double)n) : mass; };
+      if (extras || group == 0) {
+        for (uint32_t i = 0; i < 64; ++i) add(i, count_of(low + i));
+      } else {
+#pragma unroll 2
+        for (uint32_t c = 0; c < 16; ++c) {
+          uint4 w = own_words(negative ? 15u - c : c);
+          if (negative) w = uint4{w.w, w.z, w.y, w.x};
+          add(4 * c, w.x >> shift & 0xFFFFu);
+          add(4 * c + 1, w.y >> shift & 0xFFFFu);
+          add(4 * c + 2, w.z >> shift & 0xFFFFu);
+          add(4 * c + 3, w.w >> shift & 0xFFFFu);
         }
       }
       mass *= first;
@@ -334,12 +358,19 @@ __global__ __launch_bounds__(kSampleThreads) void sample_kernel(SampleArgs p) {
   // ---- which of the tokens of that value: matches of every wavefront and trip, in the order of the indices
   __syncthreads();
   uint32_t* const table = hist;
-  for (int i = tid; i < trips * kSampleWaves; i += kSampleThreads) table[i] = 0u;
+  for (int i = tid; i < (trips + 3) * kSampleWaves; i += kSampleThreads) table[i] = 0u;      // (trips go by fours)
   __syncthreads();
+  // the value's bits, and the bits of a logit that count (either zero is the value 0)
+  const uint32_t wanted = (key & 0x8000u ? key ^ 0x8000u : key ^ 0xFFFFu) * 0x10001u, counts = wanted ? 0xFFFFFFFFu : 0x7FFF7FFFu;
   const auto matches = [&](const uint4& q) {
-    uint32_t found = 0;
+    const uint32_t w[4] = {(q.x ^ wanted) & counts, (q.y ^ wanted) & counts, (q.z ^ wanted) & counts, (q.w ^ wanted) & counts};
+    uint32_t zeros = 0, found = 0;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) found |= sample_key(piece_bits(q, e)) == key ? 1u << e : 0u;
+    for (int i = 0; i < 4; ++i) zeros |= (w[i] - 0x00010001u) & ~w[i] & 0x80008000u;        // a half that is zero shows
+    if (zeros) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) found |= (e & 1 ? w[e >> 1] >> 16 : w[e >> 1] & 0xFFFFu) == 0 ? 1u << e : 0u;
+    }
     return found;
   };
   const auto note = [&](int t, const uint4& q) {
@@ -349,8 +380,7 @@ __global__ __launch_bounds__(kSampleThreads) void sample_kernel(SampleArgs p) {
 #pragma unroll
   for (int t = 0; t < kSampleKept; ++t)
     if (t < trips) note(t, kept[t]);
-#pragma unroll 2
-  for (int t = kSampleKept; t < trips; ++t) note(t, sample_piece(row, p.V, t * kSampleThreads + tid));
+  further(kSampleKept, trips, note);
   __syncthreads();
   if (wave == 0) {
     const int cells = trips * kSampleWaves, per = (cells + 63) / 64;
