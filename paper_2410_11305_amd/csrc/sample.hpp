@@ -73,12 +73,11 @@ __device__ __forceinline__ uint4 sample_piece(const uint16_t* row, int V, int i)
   uint4 q = {0xFC00FC00u, 0xFC00FC00u, 0xFC00FC00u, 0xFC00FC00u};
   if (8 * i + 8 <= V) {
     __builtin_memcpy(&q, row + 8 * i, 16);
-  } else if (8 * i < V) {
-    uint32_t w[4] = {q.x, q.y, q.z, q.w};
-#pragma unroll
-    for (int e = 0; e < 7; ++e)
-      if (8 * i + e < V) w[e >> 1] = e & 1 ? (w[e >> 1] & 0xFFFFu) | (uint32_t)row[8 * i + e] << 16 : (w[e >> 1] & 0xFFFF0000u) | row[8 * i + e];
-    q = uint4{w[0], w[1], w[2], w[3]};
+  } else {
+#pragma unroll 1
+    for (int e = V - 8 * i - 1; e >= 0; --e)                  // (one piece of a row at most)
+      q = uint4{q.x << 16 | row[8 * i + e], __builtin_amdgcn_alignbit(q.y, q.x, 16), __builtin_amdgcn_alignbit(q.z, q.y, 16),
+                __builtin_amdgcn_alignbit(q.w, q.z, 16)};
   }
   return q;
 }
@@ -121,7 +120,7 @@ __global__ __launch_bounds__(kSampleThreads) void sample_kernel(SampleArgs p) {
   __shared__ uint32_t border[4], border_before[4];            // blocks in which something is decided, and the tokens before them
   __shared__ double border_mass[4];                           // ... and the mass
   __shared__ uint32_t cell_found[2];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int r = blockIdx.x, b = r / p.per;
   const uint16_t* const row = p.logits + (size_t)r * p.V;
   const uint32_t own = kSampleThreads - 1 - tid;              // this thread's block, the largest values first
@@ -140,6 +139,15 @@ __global__ __launch_bounds__(kSampleThreads) void sample_kernel(SampleArgs p) {
     for (uint32_t i = 0; i < extras; ++i) n += extra[i] == key ? 32768u : 0u;
     return n;
   };
+
+  // ---- the sequence's parameters
+  const float temperature = p.temperature ? p.temperature[b] : 1.0f;
+  const bool greedy = !(temperature > 0.0f);
+  const uint32_t k = greedy ? 1u : p.top_k && p.top_k[b] > 0 ? (uint32_t)p.top_k[b] : 0xFFFFFFFFu;
+  const double least = p.min_p && p.min_p[b] > 0.0f ? fmin((double)p.min_p[b], 1.0) : 0.0;
+  const float share = p.top_p ? p.top_p[b] : 1.0f;
+  const double u = (double)fminf(fmaxf(p.u[r], 0.0f), 0.99999994f);
+  const double inverse = greedy ? 0.0 : 1.0 / (double)temperature;
 
   // ---- counts
   uint4 kept[kSampleKept];
@@ -197,21 +205,25 @@ __global__ __launch_bounds__(kSampleThreads) void sample_kernel(SampleArgs p) {
     if (group == 0) n = negative ? n - (hist[0] >> 16) : n + (hist[0] >> 16);        // -0 counts as 0
     return n;
   };
+  // the sum of the wavefronts' numbers before this one, and of all of them
+  const auto over_waves = [&](const uint32_t* each, uint32_t& all) {
+    const uint32_t scan = lane_scan(lane < kSampleWaves ? each[lane] : 0u);
+    all = (uint32_t)__builtin_amdgcn_readlane((int)scan, kSampleWaves - 1);
+    return wave ? (uint32_t)__builtin_amdgcn_readlane((int)scan, wave - 1) : 0u;
+  };
   uint32_t here = sum_own();
   uint32_t upto = lane_scan(here);
-  const uint32_t seen_wave = lane_scan(counted);
-  if (lane == 63) {
-    wave_u[0][wave] = upto;
-    wave_u[1][wave] = seen_wave;
+  if (lane == 63) wave_u[0][wave] = upto;
+  const bool may_run_over = p.V > 65535;
+  if (may_run_over) {
+    const uint32_t seen_wave = lane_scan(counted);
+    if (lane == 63) wave_u[1][wave] = seen_wave;
   }
   __syncthreads();
-  uint32_t before = upto - here, tokens = 0, seen = 0;
-#pragma unroll
-  for (int w = 0; w < kSampleWaves; ++w) {
-    before += w < wave ? wave_u[0][w] : 0u;
-    tokens += wave_u[0][w];
-    seen += wave_u[1][w];
-  }
+  uint32_t tokens, seen;
+  uint32_t before = over_waves(wave_u[0], tokens) + upto - here;
+  seen = tokens;
+  if (may_run_over) over_waves(wave_u[1], seen);
   if (tokens != seen) {
     // A counter ran over (more than 65535 equal logits; every overflow loses counts, so it shows in the sum).  Again, 32768
     // tokens at a time, each time taking 32768 off the counters that have them.
@@ -219,9 +231,16 @@ __global__ __launch_bounds__(kSampleThreads) void sample_kernel(SampleArgs p) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) reinterpret_cast<uint4*>(hist)[i * kSampleThreads + tid] = uint4{0u, 0u, 0u, 0u};
     __syncthreads();
+#pragma unroll 1
     for (int t0 = 0; t0 < trips; t0 += 4) {
-      further(t0, min(trips, t0 + 4), [&](int, const uint4& q) { count_piece(q); });
+#pragma unroll 1
+      for (int i = 8 * t0 * kSampleThreads + tid; i < min(p.V, 8 * (t0 + 4) * kSampleThreads); i += kSampleThreads) {
+        const uint32_t x = row[i];
+        if (__builtin_amdgcn_classh(__builtin_bit_cast(_Float16, (uint16_t)x), kNumber))
+          atomicAdd(reinterpret_cast<uint32_t*>(bytes + place_of(x << 2 & 0x1FFFCu)), max(x << 1 & 0x10000u, 1u));
+      }
       __syncthreads();
+#pragma unroll 1
       for (uint32_t i = 0; i < 64; ++i) {
         const uint32_t magnitude = group * 64 + i;
         uint32_t* const w = reinterpret_cast<uint32_t*>(bytes + place_of(magnitude * 4));
@@ -238,8 +257,7 @@ __global__ __launch_bounds__(kSampleThreads) void sample_kernel(SampleArgs p) {
     upto = lane_scan(here);
     if (lane == 63) wave_u[0][wave] = upto;
     __syncthreads();
-    before = upto - here;
-    for (int w = 0; w < wave; ++w) before += wave_u[0][w];
+    before = over_waves(wave_u[0], tokens) + upto - here;
   }
   if (seen == 0) {                                            // nothing to choose from
     if (tid == 0) p.tokens[r] = -1;
@@ -253,13 +271,6 @@ __global__ __launch_bounds__(kSampleThreads) void sample_kernel(SampleArgs p) {
   const uint64_t any = __builtin_amdgcn_ballot_w64(count_of(top_block * 64 + 63 - lane) != 0);
   const uint32_t top = top_block * 64 + 63 - (uint32_t)__builtin_ctzll(any);
 
-  const float temperature = p.temperature ? p.temperature[b] : 1.0f;
-  const bool greedy = !(temperature > 0.0f);
-  const uint32_t k = greedy ? 1u : p.top_k && p.top_k[b] > 0 ? (uint32_t)p.top_k[b] : 0xFFFFFFFFu;
-  const double least = p.min_p && p.min_p[b] > 0.0f ? fmin((double)p.min_p[b], 1.0) : 0.0;
-  const float share = p.top_p ? p.top_p[b] : 1.0f;
-  const double u = (double)fminf(fmaxf(p.u[r], 0.0f), 0.99999994f);
-  const double inverse = greedy ? 0.0 : 1.0 / (double)temperature;
   const double top_value = sample_value(top);
   // (beside +inf the others weigh nothing)
   const auto weight_of = [&](uint32_t key) {
@@ -273,28 +284,34 @@ __global__ __launch_bounds__(kSampleThreads) void sample_kernel(SampleArgs p) {
     const uint32_t low = own * 64, high = min(low + 63u, top);
     const double first = weight_of(high), ratio = top == 0xFC00u ? 0.0 : exp_negative((sample_value(low) - sample_value(low + 1)) * inverse);
     const bool all = !(least > 0.0) || weight_of(low) >= least;
-    if (all && before + here <= k) {
-      const uint32_t steps = high - low;      // from the least value up to the largest one that counts
+    if (!all || before + here > k || high != low + 63u) {
+      // cut inside by top_k or by min_p, or the block of the largest value: three blocks at most, for a wavefront each
+      if (first >= least) {
+        const int slot = before + here > k ? 0 : all ? 2 : 1;
+        border[slot] = own;
+        border_before[slot] = before;
+      }
+    } else if (extras) {
+#pragma unroll 1
+      for (uint32_t key = low; key <= high; ++key) mass = fma(mass, ratio, (double)count_of(key));
+      mass *= first;
+    } else {
       const uint32_t shift = negative ? 16u : 0u;
-      const auto add = [&](uint32_t i, uint32_t n) { mass = i <= steps ? fma(mass, ratio, (double)n) : mass; };
-      if (extras || group == 0) {
-        for (uint32_t i = 0; i < 64; ++i) add(i, count_of(low + i));
-      } else {
 #pragma unroll 2
-        for (uint32_t c = 0; c < 16; ++c) {
-          uint4 w = own_words(negative ? 15u - c : c);
-          if (negative) w = uint4{w.w, w.z, w.y, w.x};
-          add(4 * c, w.x >> shift & 0xFFFFu);
-          add(4 * c + 1, w.y >> shift & 0xFFFFu);
-          add(4 * c + 2, w.z >> shift & 0xFFFFu);
-          add(4 * c + 3, w.w >> shift & 0xFFFFu);
+      for (uint32_t i = 0; i < 16; ++i) {
+        const uint32_t c = negative ? 15u - i : i;
+        uint4 w = own_words(c);
+        const uint32_t zero = group == 0 && c == 0 ? 1u : 0u;                            // -0 counts as 0
+        const uint32_t least_word = zero ? (negative ? 0u : (w.x & 0xFFFFu) + (w.x >> 16)) : w.x >> shift & 0xFFFFu;
+        const uint32_t n[4] = {least_word, w.y >> shift & 0xFFFFu, w.z >> shift & 0xFFFFu, w.w >> shift & 0xFFFFu};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          // (a count in the low bits of 2^52, and 2^52 off again: two short operations where the conversion takes as long as four)
+          const uint32_t m = n[negative ? 3 - e : e];
+          mass = fma(mass, ratio, __builtin_bit_cast(double, 0x4330000000000000ull | m) - 4503599627370496.0);
         }
       }
       mass *= first;
-    } else if (first >= least) {              // cut inside, by top_k or min_p: at most two such blocks
-      const int slot = before + here > k ? 0 : 1;
-      border[slot] = own;
-      border_before[slot] = before;
     }
   }
   __syncthreads();
@@ -310,24 +327,22 @@ __global__ __launch_bounds__(kSampleThreads) void sample_kernel(SampleArgs p) {
     x.upto = mass_before + lane_scan((double)x.n * x.weight);
     return x;
   };
-#pragma unroll 1
-  for (int slot = 0; slot < 2; ++slot) {
-    const uint32_t block = border[slot];
-    if (block != 0xFFFFFFFFu) {
-      const double cut = lane_value_f64(block_of(block, border_before[slot], 0.0).upto, 63);
-      if (block == own) mass = cut;
-    }
+  if (wave < 3 && border[wave] != 0xFFFFFFFFu) {
+    const double cut = lane_value_f64(block_of(border[wave], border_before[wave], 0.0).upto, 63);
+    if (lane == 0) border_mass[wave] = cut;
   }
+  __syncthreads();
+#pragma unroll
+  for (int slot = 0; slot < 3; ++slot) mass = border[slot] == own ? border_mass[slot] : mass;
   const double sum = lane_scan(mass);
   if (lane == 63) wave_d[wave] = sum;
   __syncthreads();
-  double wave_base = 0.0, total = 0.0;
-  for (int w = 0; w < kSampleWaves; ++w) {
-    wave_base = w == wave ? total : wave_base;
-    total += wave_d[w];
-  }
+  const double waves_scan = lane_scan(lane < kSampleWaves ? wave_d[lane] : 0.0);
+  const double total = lane_value_f64(waves_scan, kSampleWaves - 1);
+  const double wave_base = wave ? lane_value_f64(waves_scan, wave - 1) : 0.0, next_base = lane_value_f64(waves_scan, wave);
   const double shifted = __shfl_up(sum, 1);
-  const double from = lane ? wave_base + shifted : wave_base, to = wave_base + sum;     // (to is the next thread's from, bit for bit)
+  // (to is the next thread's from, bit for bit)
+  const double from = lane ? wave_base + shifted : wave_base, to = lane < 63 ? wave_base + sum : next_base;
 
   // ---- top-p: the shortest beginning that holds this much (one token at least)
   double kept_mass = total;
