@@ -136,6 +136,7 @@ __global__ __launch_bounds__(kSampleThreads) void sample_kernel(SampleArgs p) {
     uint32_t n = below ? w >> 16 : w & 0xFFFFu;
     if (key == 0x8000u) n += w >> 16;
     if (key == 0x7FFFu) n = 0;
+#pragma unroll 1
     for (uint32_t i = 0; i < extras; ++i) n += extra[i] == key ? 32768u : 0u;
     return n;
   };
@@ -188,7 +189,7 @@ __global__ __launch_bounds__(kSampleThreads) void sample_kernel(SampleArgs p) {
   further(kSampleKept, trips, [&](int, const uint4& q) { count_piece(q); });
   __syncthreads();
   // this thread's 64 values: 64 words, upwards or (negative values; the upper half of the wavefronts) downwards
-  const bool negative = own < 512u;
+  const bool negative = wave >= kSampleWaves / 2;             // own < 512
   const uint32_t group = negative ? 511u - own : own - 512u;
   const auto own_words = [&](uint32_t c) { return *reinterpret_cast<const uint4*>(bytes + (group * 256 + ((c ^ (group & 7u)) << 4))); };
   const auto sum_own = [&] {
@@ -253,6 +254,7 @@ __global__ __launch_bounds__(kSampleThreads) void sample_kernel(SampleArgs p) {
       __syncthreads();
     }
     here = sum_own();
+#pragma unroll 1
     for (uint32_t i = 0; i < extras; ++i) here += extra[i] >> 6 == own ? 32768u : 0u;
     upto = lane_scan(here);
     if (lane == 63) wave_u[0][wave] = upto;
@@ -300,15 +302,17 @@ __global__ __launch_bounds__(kSampleThreads) void sample_kernel(SampleArgs p) {
 #pragma unroll 2
       for (uint32_t i = 0; i < 16; ++i) {
         const uint32_t c = negative ? 15u - i : i;
-        uint4 w = own_words(c);
-        const uint32_t zero = group == 0 && c == 0 ? 1u : 0u;                            // -0 counts as 0
-        const uint32_t least_word = zero ? (negative ? 0u : (w.x & 0xFFFFu) + (w.x >> 16)) : w.x >> shift & 0xFFFFu;
-        const uint32_t n[4] = {least_word, w.y >> shift & 0xFFFFu, w.z >> shift & 0xFFFFu, w.w >> shift & 0xFFFFu};
+        const uint4 w = own_words(c);
+        uint32_t n[4] = {w.x >> shift & 0xFFFFu, w.y >> shift & 0xFFFFu, w.z >> shift & 0xFFFFu, w.w >> shift & 0xFFFFu};
+        if (c == 0 && group == 0) n[0] = negative ? 0u : (w.x & 0xFFFFu) + (w.x >> 16);        // -0 counts as 0
+        if (negative) {
+          const uint32_t n0 = n[0], n1 = n[1];
+          n[0] = n[3]; n[1] = n[2]; n[2] = n1; n[3] = n0;
+        }
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           // (a count in the low bits of 2^52, and 2^52 off again: two short operations where the conversion takes as long as four)
-          const uint32_t m = n[negative ? 3 - e : e];
-          mass = fma(mass, ratio, __builtin_bit_cast(double, 0x4330000000000000ull | m) - 4503599627370496.0);
+          mass = fma(mass, ratio, __builtin_bit_cast(double, 0x4330000000000000ull | n[e]) - 4503599627370496.0);
         }
       }
       mass *= first;
