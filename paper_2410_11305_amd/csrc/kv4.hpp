@@ -37,14 +37,15 @@ __device__ __forceinline__ int kv_page(const KvShape& s, int b, long long at) {
   return page >= 0 && page < s.n_pages ? page : -1;
 }
 
-// float64 to fp16 in one rounding: to float32 with the last bit set where that is inexact (round to odd: 13 bits more
-// than fp16 has are enough), then to nearest even.
+// A finite binary64 value to fp16 in one rounding: cut to 20 bits of significand with a last bit that remembers what was
+// cut off (9 bits more than fp16 has; round to odd), put together as binary32, then to nearest even.  Whole-number operations: the
+// conversions from and to binary64 take four times as long as any of them.
 __device__ inline _Float16 half_of_f64(double v) {
-  float f = (float)v;
-  const double back = (double)f;
-  uint32_t bits = __builtin_bit_cast(uint32_t, f);
-  if (back != v && (bits & 1u) == 0) bits += fabs(back) < fabs(v) ? 1u : 0xFFFFFFFFu;
-  return (_Float16)(back != v ? __builtin_bit_cast(float, bits) : f);
+  const uint64_t bits = __builtin_bit_cast(uint64_t, v);
+  const uint32_t high = (uint32_t)(bits >> 32) | min((uint32_t)bits, 1u);
+  // exponents below binary32's become zero, exponents past fp16's stay past them
+  const int magnitude = min(max((int)(high & 0x7FFFFFFFu) - (896 << 20), 0), 200 << 20);
+  return (_Float16)__builtin_bit_cast(float, (high & 0x80000000u) | (uint32_t)magnitude << 3);
 }
 
 // cos and sin of `turns` whole turns, to a few units in the last place of binary64: the nearest quarter turn off, then
@@ -98,36 +99,49 @@ __device__ inline float row_max(float a) {
   return a;
 }
 
-// Code word of 8 values of a head, and the head's step and minimum.  The quotient is formed in binary64, where the difference of two fp16 values
-// is exact and a quotient that is not itself half way between two integers is far enough from it to stay on its side.
+// Code word of 8 values of a head, and the head's step and minimum.  A quotient in binary32 is off by less than 2^-18; where one of the
+// 8 lies nearer to half way between two integers than that, all are formed in binary64, where the difference of two
+// fp16 values is exact and a quotient that is not itself half way is far enough from it to stay on its side.
 template <int LANES>
 __device__ inline uint32_t kv_code_word(const float (&v)[8], _Float16& step, _Float16& low) {
   float hi = v[0], lo = v[0];
 #pragma unroll
   for (int e = 1; e < 8; ++e) { hi = fmaxf(hi, v[e]); lo = fminf(lo, v[e]); }
-  hi = row_max<LANES>(hi);
-  lo = -row_max<LANES>(-lo) + 0.0f;                         // (a zero is +0, here and in the step)
-  hi += 0.0f;
+  hi = row_max<LANES>(hi) + 0.0f;                           // (a zero is +0, here and in the step)
+  lo = -row_max<LANES>(-lo) + 0.0f;
   low = (_Float16)lo;                                       // exact: one of the values
-  step = half_of_f64(((double)hi - (double)lo) / 15.0);
-  const double s = (double)(float)step;
-  if (!(s > 0.0)) return 0u;
-  double y = __builtin_amdgcn_rcp(s);
-  y = fma(fma(-s, y, 1.0), y, y);
-  y = fma(fma(-s, y, 1.0), y, y);
+  // a fifteenth: one remainder step from the rounded reciprocal (halves of fp16 units come out exactly)
+  const double range = (double)hi - (double)lo, fifteenth = range * (1.0 / 15.0);
+  step = half_of_f64(fma(fma(-15.0, fifteenth, range), 1.0 / 15.0, fifteenth));
+  const float s = (float)step;
+  if (!(s > 0.0f)) return 0u;
+  const float y = 1.0f / s;
   uint32_t w = 0;
+  float nearest = 0.0f;
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
-    const double d = (double)v[e] - (double)lo;
-    double t = d * y;
-    t = fma(fma(-t, s, d), y, t);
-    const int code = min(max((int)rint(t), 0), 15);
-    w |= (uint32_t)code << (4 * nibble_pos(e));
+    const float q = (v[e] - lo) * y, t = rintf(q);
+    nearest = fmaxf(nearest, fabsf(q - t));
+    w |= (uint32_t)fminf(t, 15.0f) << (4 * nibble_pos(e));
+  }
+  if (nearest > 0.49999f) {
+    const double s64 = (double)s, lo64 = (double)lo;
+    double y64 = __builtin_amdgcn_rcp(s64);
+    y64 = fma(fma(-s64, y64, 1.0), y64, y64);
+    y64 = fma(fma(-s64, y64, 1.0), y64, y64);
+    w = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const double d = (double)v[e] - lo64;
+      double t = d * y64;
+      t = fma(fma(-t, s64, d), y64, t);
+      w |= (uint32_t)min((int)rint(t), 15) << (4 * nibble_pos(e));
+    }
   }
   return w;
 }
 
-// grid (B*T, parts of the heads): a workgroup takes one token and 256 / (D/8) of its Hq + 2 Hkv heads, a row of D/8
+// grid (B*T, parts): a workgroup takes one token and every parts-th set of 256 / (D/8) of its Hq + 2 Hkv heads, a row of D/8
 // lanes a head, 8 features a lane.
 template <int D>
 __global__ __launch_bounds__(256) void rope_kv4_append_kernel(AppendArgs p) {
@@ -136,58 +150,64 @@ __global__ __launch_bounds__(256) void rope_kv4_append_kernel(AppendArgs p) {
   const int token = blockIdx.x, b = token / p.kv.T, j = token - b * p.kv.T;
   const int l = threadIdx.x & (LANES - 1);
   const int heads = p.Hq + 2 * p.kv.Hkv;
-  const int head = blockIdx.y * PER + (int)threadIdx.x / LANES;
-  const bool live = head < heads;
-  const uint4* const row = p.qkv + ((size_t)token * heads + min(head, heads - 1)) * LANES;
   const int half = p.rot >> 1;
-  const bool turns = 8 * l < p.rot && head < p.Hq + p.kv.Hkv;
-  const uint4 mine = row[l];
-  uint4 other = mine;
-  const bool upper = 8 * l >= half;
-  if (turns && !p.interleaved) other = row[upper ? l - (half >> 3) : l + (half >> 3)];
+  const bool in_rot = 8 * l < p.rot, upper = 8 * l >= half;
+  const uint4* const rows = p.qkv + (size_t)token * heads * LANES + l;
+  const int partner = in_rot && !p.interleaved ? (upper ? -(half >> 3) : half >> 3) : 0;
+  int head = blockIdx.y * PER + (int)threadIdx.x / LANES;
+  uint4 mine = rows[(size_t)min(head, heads - 1) * LANES], other = rows[(size_t)min(head, heads - 1) * LANES + partner];
   const long long at = (long long)p.kv.pos[b] + j;
+  const int page = kv_page(p.kv, b, at);
   if ((int)threadIdx.x < half) {
     double c, s;
     cos_sin_turns((double)at * (p.inv_freq[threadIdx.x] * 0.15915494309189533577), c, s);
     turn[threadIdx.x] = double2{c * (double)p.mscale, s * (double)p.mscale};
   }
   __syncthreads();
-  const v8h x = __builtin_bit_cast(v8h, mine), z = __builtin_bit_cast(v8h, other);
-  v8h h = x;
-  if (turns) {
-    if (p.interleaved) {
+  const int P = 1 << p.kv.page_shift, slot = (int)(at & (P - 1));
+  uint8_t* const regions = p.cache + (size_t)max(page, 0) * p.kv.Hkv * ((size_t)P * (D + 8));
+  for (int base = blockIdx.y * PER; base < heads; base += gridDim.y * PER) {
+    const v8h x = __builtin_bit_cast(v8h, mine), z = __builtin_bit_cast(v8h, other);
+    const int now = head, next = min(head + (int)gridDim.y * PER, heads - 1);
+    head += gridDim.y * PER;
+    mine = rows[(size_t)next * LANES];                      // (the last one's loads repeat a head)
+    other = rows[(size_t)next * LANES + partner];
+    v8h h = x;
+    if (in_rot && now < p.Hq + p.kv.Hkv) {
+      if (p.interleaved) {
 #pragma unroll
-      for (int e = 0; e < 8; e += 2) {
-        const double2 t = turn[4 * l + e / 2];
-        const double a = (double)(float)x[e], c = (double)(float)x[e + 1];
-        h[e] = half_of_f64(a * t.x - c * t.y);
-        h[e + 1] = half_of_f64(c * t.x + a * t.y);
+        for (int e = 0; e < 8; e += 2) {
+          const double2 t = turn[4 * l + e / 2];
+          const double a = (double)(float)x[e], c = (double)(float)x[e + 1];
+          h[e] = half_of_f64(a * t.x - c * t.y);
+          h[e + 1] = half_of_f64(c * t.x + a * t.y);
+        }
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const double2 t = turn[8 * l + e - (upper ? half : 0)];
+          const double a = (double)(float)x[e], c = (double)(float)z[e];
+          h[e] = half_of_f64(a * t.x + (upper ? c : -c) * t.y);
+        }
       }
-    } else {
+    }
+    if (now < p.Hq) p.q[((size_t)token * p.Hq + now) * LANES + l] = __builtin_bit_cast(uint4, h);
+    if (now >= p.Hq && now < heads) {                       // (whole rows of lanes: the folds see each other)
+      float v[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const double2 t = turn[8 * l + e - (upper ? half : 0)];
-        const double a = (double)(float)x[e], c = (double)(float)z[e];
-        h[e] = half_of_f64(a * t.x + (upper ? c : -c) * t.y);
+      for (int e = 0; e < 8; ++e) v[e] = (float)h[e];
+      _Float16 step, low;
+      const uint32_t word = kv_code_word<LANES>(v, step, low);
+      if (page >= 0) {
+        const bool value = now >= p.Hq + p.kv.Hkv;
+        uint8_t* const region = regions + (size_t)(now - p.Hq - (value ? p.kv.Hkv : 0)) * ((size_t)P * (D + 8));
+        uint32_t* const place = value ? reinterpret_cast<uint32_t*>(region + (size_t)P * (D / 2) + (size_t)(slot >> 4) * (8 * D)) + l * 16 + (slot & 15)
+                                      : reinterpret_cast<uint32_t*>(region + (size_t)slot * (D / 2)) + l;
+        *place = word;
+        if (l == 0) *reinterpret_cast<v2h*>(region + (size_t)P * D + (size_t)slot * 8 + (value ? 4 : 0)) = v2h{step, low};
       }
     }
   }
-  if (live && head < p.Hq) p.q[((size_t)token * p.Hq + head) * LANES + l] = __builtin_bit_cast(uint4, h);
-  float v[8];
-#pragma unroll
-  for (int e = 0; e < 8; ++e) v[e] = (float)h[e];
-  _Float16 step, low;
-  const uint32_t word = kv_code_word<LANES>(v, step, low);  // (every lane: the folds)
-  const int page = kv_page(p.kv, b, at);
-  if (!live || head < p.Hq || page < 0) return;
-  const bool value = head >= p.Hq + p.kv.Hkv;
-  const int kv_head = head - p.Hq - (value ? p.kv.Hkv : 0);
-  const int P = 1 << p.kv.page_shift, slot = (int)(at & (P - 1));
-  uint8_t* const region = p.cache + ((size_t)page * p.kv.Hkv + kv_head) * ((size_t)P * (D + 8));
-  uint32_t* const place = value ? reinterpret_cast<uint32_t*>(region + (size_t)P * (D / 2) + (size_t)(slot >> 4) * (8 * D)) + l * 16 + (slot & 15)
-                                : reinterpret_cast<uint32_t*>(region + (size_t)slot * (D / 2)) + l;
-  *place = word;
-  if (l == 0) *reinterpret_cast<v2h*>(region + (size_t)P * D + (size_t)slot * 8 + (value ? 4 : 0)) = v2h{step, low};
 }
 
 struct KvReadArgs {

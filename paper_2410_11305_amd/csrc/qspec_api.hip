@@ -1259,7 +1259,9 @@ int qspec_rope_kv4_append(const void* qkv_f16, const double* inv_freq, const int
   if (int st = check_device()) return st;
   AppendArgs a{kv_shape(pos, page_table, T, Hkv, page_size, max_pages, n_pages), static_cast<const uint4*>(qkv_f16), inv_freq,
                static_cast<uint4*>(q_f16), static_cast<uint8_t*>(cache), Hq, rot, interleaved, mscale};
-  const dim3 grid(B * T, blocks_for((size_t)heads * (D / 8), 256));
+  // a workgroup for every 256 / (D/8) heads where there are few tokens; from 1024 workgroups on fewer, which take several sets of heads each
+  const unsigned sets = blocks_for((size_t)heads * (D / 8), 256), wanted = blocks_for(1024, (unsigned)(B * T));
+  const dim3 grid(B * T, wanted < sets ? wanted : sets);
   if (D == 128) launch_kernel(rope_kv4_append_kernel<128>, grid, dim3(256), 0, static_cast<hipStream_t>(stream), a);
   else launch_kernel(rope_kv4_append_kernel<64>, grid, dim3(256), 0, static_cast<hipStream_t>(stream), a);
   return launch_status();
