@@ -41,7 +41,7 @@ namespace qspec {
 #define T1 0
 #define GRID 512
 #endif
-constexpr size_t kAttnTicketBytes = 16384;   // arrival counters at the head of the workspace, one a workgroup
+constexpr size_t kAttnTicketBytes = 16384;   // arrival counters at the head of the workspace, two a workgroup
 #ifndef MIN1
 #define MIN1 512
 #define MIN2 512
@@ -64,7 +64,7 @@ struct AttnForm {
   // workgroup gets on average at least
   static constexpr int over = (NB == 1 ? OVER1 : NB == 2 ? OVER2 : OVER4) / step;
   static constexpr int whole = WHOLE / step;
-  static_assert(workgroups * sizeof(unsigned) <= kAttnTicketBytes, "a counter for every workgroup");
+  static_assert(2 * workgroups * sizeof(unsigned) <= kAttnTicketBytes, "two counters for every workgroup");
   static constexpr int least = (NB == 1 ? MIN1 : NB == 2 ? MIN2 : MIN4) / step;
 };
 
@@ -563,6 +563,12 @@ __global__ __launch_bounds__((64 * AttnForm<NB, F>::waves), NB == 1 ? S1 : 2) vo
       for (int x = 0; x < 4; ++x) h[x] = (_Float16)(sum > 0.0f ? fminf(fmaxf(v[x] * by, -65504.0f), 65504.0f) : 0.0f);   // (a 15th code may lie past fp16's end)
       *reinterpret_cast<v4h*>(p.out + (((size_t)b * p.kv.T + j) * p.Hq + (size_t)head * p.G + g) * D + own) = h;
     };
+    const auto write_part = [&](uint32_t slot, int r, float ref, float sum, const float (&v)[4]) {
+      float* const part = p.parts + ((size_t)slot * RB + r) * PART;
+      if (own == 0) store_shared_f2(part, ref, sum);
+      store_shared_f2(part + 4 + own, v[0], v[1]);
+      store_shared_f2(part + 6 + own, v[2], v[3]);
+    };
     // (Code that runs once an item comes from memory at every launch: one copy of what can be shared, few unrolled loops.)
     const auto hand_over = [&](int nb) {
       if (F > 1) {                            // the columns of a row
@@ -623,20 +629,29 @@ __global__ __launch_bounds__((64 * AttnForm<NB, F>::waves), NB == 1 ? S1 : 2) vo
         if (!shared) {
           write_row(block * RB + r, v, total_l);
         } else {
-          float* const part = p.parts + ((size_t)(2 * me + (first_run ? 0 : 1)) * RB + r) * PART;
-          if (own == 0) store_shared_f2(part, ref, total_l);
-          store_shared_f2(part + 4 + own, v[0], v[1]);
-          store_shared_f2(part + 6 + own, v[2], v[3]);
+          write_part(2 * me + (first_run ? 0 : 1), r, ref, total_l, v);
         }
       }
       __syncthreads();
     }
 
-    // ---- the last of the item's workgroups joins their parts
-    if (shared && last_arrival(p.tickets, (int)(w1 - w0 + 1), w0, &ticket)) {
+    // ---- the last of the item's workgroups joins their parts; of many parts, the last of each eight theirs first (a
+    // workgroup reads parts past the caches at tens of GB/s: 64 parts of 8 rows in one go take 14 us)
+    const uint32_t parts = w1 - w0 + 1;
+    const auto slot_of = [&](uint32_t w) { return w == w0 ? 2 * w0 + (start_of(w0) < item ? 1 : 0) : 2 * w; };
+#pragma unroll 1
+    for (int stage = parts > 16 ? 0 : 1; shared && stage < 2; ++stage) {
+      uint32_t first = w0, stride = 1, n = parts, counter = w0;
+      if (stage == 0) {
+        first = w0 + ((me - w0) & ~7u);
+        n = min(8u, w1 + 1 - first);
+        counter = Form::workgroups + first;
+      } else if (parts > 16) {
+        stride = 8;
+        n = (parts + 7) / 8;
+      }
+      if (!last_arrival(p.tickets, (int)n, counter, &ticket)) break;
       constexpr int SETS = THREADS / LANES;            // rows at a time
-      const int n = (int)(w1 - w0 + 1);
-      const uint32_t slot0 = 2 * w0 + (start_of(w0) < item ? 1 : 0);
       // few rows: several threads take a row's parts in turn
       int taken = 1;
       while (taken < min(rows, SETS)) taken *= 2;
@@ -652,19 +667,19 @@ __global__ __launch_bounds__((64 * AttnForm<NB, F>::waves), NB == 1 ? S1 : 2) vo
         };
         if (r < rows) {
           constexpr int FLY = FLYN;                    // parts on their way together: each is a trip past the caches
-          for (int i0 = lot; i0 < n; i0 += FLY * lots) {
+          for (int i0 = lot; i0 < (int)n; i0 += FLY * lots) {
             float2 ml[FLY], in[FLY][2];
 #pragma unroll
             for (int y = 0; y < FLY; ++y) {
-              const int i = min(i0 + y * lots, n - 1);
-              const float* const part = p.parts + ((size_t)(i == 0 ? slot0 : 2 * (w0 + i)) * RB + r) * PART;
+              const uint32_t i = min((uint32_t)(i0 + y * lots), n - 1);
+              const float* const part = p.parts + ((size_t)slot_of(first + i * stride) * RB + r) * PART;
               ml[y] = load_shared_f2(part);
               in[y][0] = load_shared_f2(part + 4 + own);
               in[y][1] = load_shared_f2(part + 6 + own);
             }
 #pragma unroll
             for (int y = 0; y < FLY; ++y)
-              if (i0 + y * lots < n) add(ml[y].x, ml[y].y, in[y][0].x, in[y][0].y, in[y][1].x, in[y][1].y);
+              if (i0 + y * lots < (int)n) add(ml[y].x, ml[y].y, in[y][0].x, in[y][0].y, in[y][1].x, in[y][1].y);
           }
         }
         if (lots > 1) {
@@ -680,7 +695,10 @@ __global__ __launch_bounds__((64 * AttnForm<NB, F>::waves), NB == 1 ? S1 : 2) vo
             }
           }
         }
-        if (lot == 0 && r < rows) write_row(block * RB + r, v, sum);
+        if (lot == 0 && r < rows) {
+          if (stage == 1) write_row(block * RB + r, v, sum);
+          else write_part(slot_of(first), r, ref, sum, v);
+        }
         __syncthreads();
       }
     }
