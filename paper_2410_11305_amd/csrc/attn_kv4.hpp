@@ -27,6 +27,9 @@
 
 namespace qspec {
 
+#ifndef QL
+#define QL 4
+#endif
 #ifndef FLYN
 #define FLYN 4
 #endif
@@ -44,12 +47,16 @@ namespace qspec {
 constexpr size_t kAttnTicketBytes = 16384;   // arrival counters at the head of the workspace, two a workgroup
 #ifndef MIN1
 #define MIN1 512
-#define MIN2 512
-#define MIN4 1024
-#define OVER1 256
-#define OVER2 256
-#define OVER4 384
-#define WHOLE 512
+#define MIN2 640
+#define MIN4 1280
+#endif
+#ifndef OVER1
+#define OVER1 1024
+#define OVER2 768
+#define OVER4 512
+#endif
+#ifndef WHOLE
+#define WHOLE 1024
 #endif
 
 // The shape of an instance.  NB: blocks of 16 columns a wavefront carries; F: token tiles that share a block (below).
@@ -171,7 +178,7 @@ __global__ __launch_bounds__((64 * AttnForm<NB, F>::waves), NB == 1 ? S1 : 2) vo
   constexpr int PITCH = D + 4;                // floats of a row in LDS
   constexpr int LANES = D / 4;                // threads of a row where sums are joined, 4 features each
   constexpr int PART = attn_part_floats(D);
-  constexpr bool Q_LDS = NB == 4;             // the rows' registers would not leave room for the sums
+  constexpr bool Q_LDS = NB >= QL;             // the rows' registers would not leave room for the sums
   constexpr bool TIGHT = NB == 4 || (T1 && NB == 1);             // registers for the sums and the loads under way, none for widening ahead
   constexpr float kNone = -1e30f;             // reference of a row that has seen nothing: below every score
   __shared__ float o_lds[WAVES][COLS][PITCH];
@@ -206,7 +213,7 @@ __global__ __launch_bounds__((64 * AttnForm<NB, F>::waves), NB == 1 ? S1 : 2) vo
   QSPEC_DPP_ADD(0x143, 0xc);                  // row_bcast 31 into rows 2 and 3
 #undef QSPEC_DPP_ADD
   const uint32_t total = (uint32_t)__builtin_amdgcn_readlane((int)upto, 63);
-  const uint32_t groups = uniform(min((uint32_t)gridDim.x, max((uint32_t)(entries * Hkv), total / (Form::least + OVER))));
+  const uint32_t groups = uniform(min((uint32_t)gridDim.x, max((uint32_t)(entries * Hkv), (total - (uint32_t)(entries * Hkv) * OVER) / Form::least)));
   const uint32_t me = blockIdx.x;
   if (me >= groups) return;
   // workgroup w begins at w * share, and the first `more` of them take one more each; a begin in the first OVER of an
