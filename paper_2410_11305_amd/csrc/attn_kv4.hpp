@@ -71,6 +71,7 @@ struct AttnForm {
   // workgroup gets on average at least
   static constexpr int over = (NB == 1 ? OVER1 : NB == 2 ? OVER2 : OVER4) / step;
   static constexpr int whole = WHOLE / step;
+  static_assert(over >= 2 * waves && (NB == 1 ? MIN1 : NB == 2 ? MIN2 : MIN4) / step >= 2 * waves, "no workgroup's share rounds down to nothing");
   static_assert(2 * workgroups * sizeof(unsigned) <= kAttnTicketBytes, "two counters for every workgroup");
   static constexpr int least = (NB == 1 ? MIN1 : NB == 2 ? MIN2 : MIN4) / step;
 };
@@ -216,8 +217,8 @@ __global__ __launch_bounds__((64 * AttnForm<NB, F>::waves), NB == 1 ? S1 : 2) vo
   const uint32_t groups = uniform(min((uint32_t)gridDim.x, max((uint32_t)(entries * Hkv), (total - (uint32_t)(entries * Hkv) * OVER) / Form::least)));
   const uint32_t me = blockIdx.x;
   if (me >= groups) return;
-  // workgroup w begins at w * share, and the first `more` of them take one more each; a begin in the first OVER of an
-  // item, or anywhere in one that is not shared out, is the item's
+  // workgroup w begins at w * share, and the first `more` of them take one more each; inside an item it begins a whole
+  // number of rounds of its wavefronts in, or with the item in one that is not shared out
   const uint32_t share = uniform(total / groups), more = total - share * groups;
   const auto start_of = [&](uint32_t w) { return w * share + min(w, more); };
   const auto group_of = [&](uint32_t x) {     // the last workgroup that begins at x or before
@@ -238,7 +239,7 @@ __global__ __launch_bounds__((64 * AttnForm<NB, F>::waves), NB == 1 ? S1 : 2) vo
       }
     }
     const uint32_t each = uniform(n / (uint32_t)Hkv), head = uniform((x - at) / each), in = x - at - head * each;
-    return Place{e, (int)head, each <= Form::whole + OVER || in <= OVER ? 0 : (int)(in - OVER), at + head * each};
+    return Place{e, (int)head, each <= Form::whole + OVER || in < OVER ? 0 : (int)((in - OVER) & ~(WAVES - 1u)), at + head * each};
   };
   const Place from = place_of(start_of(me)), to_place = place_of(start_of(me + 1));
   int entry = from.entry, head = from.head, begin = from.step;
@@ -560,7 +561,7 @@ __global__ __launch_bounds__((64 * AttnForm<NB, F>::waves), NB == 1 ? S1 : 2) vo
 
     // ---- the wavefronts' sums, a block of columns at a time
     const bool shared = begin > 0 || stop < span.steps;
-    const uint32_t w0 = shared ? group_of(item + OVER) : me, w1 = shared ? group_of(item + OVER + span.steps - 1) : me;   // the workgroups that hold a part of it
+    const uint32_t w0 = shared ? group_of(item + OVER + WAVES - 1) : me, w1 = shared ? group_of(item + OVER + span.steps - 1) : me;   // the workgroups that hold a part of it
     const auto write_row = [&](int r, const float (&v)[4], float sum) {
       const int j = over_group(p, r), g = r - j * p.G;
       const float by = sum > 0.0f ? 1.0f / sum : 0.0f;
