@@ -456,21 +456,24 @@ def kv_overwrite(cache: torch.Tensor, kv_verify: torch.Tensor, n_accept: torch.T
 
 # ---- the 4-bit key/value cache (layout: include/qspec.h), attention over it, sampling
 
-def _shaped(t: torch.Tensor, dtype, shape, device, name: str) -> int:
-    """_dev for a tensor whose sizes are given by the others: the kernels index by those sizes alone."""
-    if t.device != device:
-        raise ValueError(f"{name} must live on {device}, got {t.device}")
-    if t.shape != shape:
+def _shaped(t: torch.Tensor, dtype, shape, device: int, name: str) -> int:
+    """_dev for a tensor of device number `device` whose sizes are given by the others: the kernels index by those sizes alone."""
+    if t.get_device() != device or t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
+        if t.is_cuda and t.get_device() != device:
+            raise ValueError(f"{name} must live on cuda:{device}, got {t.device}")
+        _dev(t, dtype, name)
         raise ValueError(f"{name} must have the shape {tuple(shape)}, got {tuple(t.shape)}")
-    return _dev(t, dtype, name)
+    return t.data_ptr()
 
 
-def _here(t: torch.Tensor, dtype, name: str) -> int:
-    """_dev for the tensor whose device is the call's: the launch goes to the current device's stream."""
-    p = _dev(t, dtype, name)
-    if t.device.index != torch.cuda.current_device():
+def _here(t: torch.Tensor, name: str) -> int:
+    """Device number of the tensor that stands for the call's: the launch goes to the current device's stream."""
+    device = t.get_device()
+    if device < 0:
+        raise ValueError(f"{name} must live on the GPU")
+    if device != (torch.cuda.current_device() if _device is None else _device()):
         raise ValueError(f"{name} lives on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
-    return p
+    return device
 
 
 def kv4_page_bytes(Hkv: int, D: int, page_size: int) -> int:
@@ -485,22 +488,27 @@ def alloc_kv4_cache(n_pages: int, Hkv: int, D: int, page_size: int) -> torch.Ten
     return torch.zeros((n_pages, nbytes), dtype=torch.uint8, device="cuda")
 
 
+_page_bytes = {}
+
+
 def _kv4(cache, pos, page_table, Hkv, D, page_size, where):
-    """(cache, pos, table pointers, B, max_pages, n_pages) of a call's cache."""
-    nbytes = kv4_page_bytes(Hkv, D, page_size)
-    if nbytes == 0:
-        raise QSpecError(ERR_SHAPE, where)
+    """(device number, cache, pos, table pointers, B, max_pages, n_pages) of a call's cache."""
+    nbytes = _page_bytes.get((Hkv, D, page_size))
+    if nbytes is None:
+        nbytes = kv4_page_bytes(Hkv, D, page_size)
+        if nbytes == 0:
+            raise QSpecError(ERR_SHAPE, where)
+        _page_bytes[Hkv, D, page_size] = nbytes
     n_pages, B = cache.shape[0], pos.shape[0]
     if B == 0 or n_pages == 0:
         raise QSpecError(ERR_SHAPE, where)
-    device = cache.device
+    device = _here(cache, "cache")
     table, max_pages = None, n_pages // B
     if page_table is not None:
         max_pages = page_table.shape[-1]
         table = _shaped(page_table, torch.int32, (B, max_pages), device, "page_table")
-    _here(cache, torch.uint8, "cache")
-    return (_shaped(cache, torch.uint8, (n_pages, nbytes), device, "cache"),
-            _shaped(pos, torch.int32, (B,), device, "pos"), table, B, max_pages, n_pages)
+    return (device, _shaped(cache, torch.uint8, (n_pages, nbytes), device, "cache"), _shaped(pos, torch.int32, (B,), device, "pos"),
+            table, B, max_pages, n_pages)
 
 
 def rope_kv4_append(qkv: torch.Tensor, inv_freq: torch.Tensor, pos: torch.Tensor, cache: torch.Tensor, Hq: int, Hkv: int,
@@ -513,16 +521,16 @@ def rope_kv4_append(qkv: torch.Tensor, inv_freq: torch.Tensor, pos: torch.Tensor
     if heads < 1 or width % heads:
         raise QSpecError(ERR_SHAPE, "qspec_rope_kv4_append")
     D = width // heads
-    c, at, table, _, max_pages, n_pages = _kv4(cache, pos, page_table, Hkv, D, page_size, "qspec_rope_kv4_append")
-    x = _shaped(qkv, torch.float16, (pos.shape[0], T, width), cache.device, "qkv")
+    device, c, at, table, Bp, max_pages, n_pages = _kv4(cache, pos, page_table, Hkv, D, page_size, "qspec_rope_kv4_append")
+    x = _shaped(qkv, torch.float16, (Bp, T, width), device, "qkv")
     rot, freq = 0, None
     if inv_freq is not None:
         rot = 2 * inv_freq.numel()
-        freq = _shaped(inv_freq, torch.float64, (rot // 2,), cache.device, "inv_freq") if rot else None
+        freq = _shaped(inv_freq, torch.float64, (rot // 2,), device, "inv_freq") if rot else None
     if q is None:
         q = torch.empty((B, T, Hq, D), dtype=torch.float16, device=cache.device)
     _check(lib().qspec_rope_kv4_append(x, freq, at, table, B, T, Hq, Hkv, D, rot, int(bool(interleaved)), mscale, page_size, max_pages,
-                                       n_pages, _shaped(q, torch.float16, (B, T, Hq, D), cache.device, "q"), c, _stream()),
+                                       n_pages, _shaped(q, torch.float16, (B, T, Hq, D), device, "q"), c, _stream()),
            "qspec_rope_kv4_append")
     return q
 
@@ -530,14 +538,14 @@ def rope_kv4_append(qkv: torch.Tensor, inv_freq: torch.Tensor, pos: torch.Tensor
 def kv4_read(cache: torch.Tensor, pos: torch.Tensor, T: int, Hkv: int, D: int, page_size: int, page_table: torch.Tensor = None,
              k: torch.Tensor = None, v: torch.Tensor = None):
     """Values of rows pos[b] .. pos[b] + T - 1 of the cache: (k, v), fp16 [B, T, Hkv, D]; zeros for rows outside of it."""
-    c, at, table, B, max_pages, n_pages = _kv4(cache, pos, page_table, Hkv, D, page_size, "qspec_kv4_read")
+    device, c, at, table, B, max_pages, n_pages = _kv4(cache, pos, page_table, Hkv, D, page_size, "qspec_kv4_read")
     if T < 1:
         raise QSpecError(ERR_SHAPE, "qspec_kv4_read")
     shape = (B, T, Hkv, D)
     k = torch.empty(shape, dtype=torch.float16, device=cache.device) if k is None else k
     v = torch.empty(shape, dtype=torch.float16, device=cache.device) if v is None else v
-    _check(lib().qspec_kv4_read(c, at, table, B, T, Hkv, D, page_size, max_pages, n_pages, _shaped(k, torch.float16, shape, cache.device, "k"),
-                                _shaped(v, torch.float16, shape, cache.device, "v"), _stream()), "qspec_kv4_read")
+    _check(lib().qspec_kv4_read(c, at, table, B, T, Hkv, D, page_size, max_pages, n_pages, _shaped(k, torch.float16, shape, device, "k"),
+                                _shaped(v, torch.float16, shape, device, "v"), _stream()), "qspec_kv4_read")
     return k, v
 
 
@@ -551,15 +559,15 @@ def attn_kv4(q: torch.Tensor, cache: torch.Tensor, pos: torch.Tensor, Hkv: int, 
     """Attention of q fp16 [B, T, Hq, D] (rows at positions pos[b] ..) over the 4-bit cache -> fp16 [B, T, Hq, D].  scale: 1 / sqrt(D)
     by default; window > 0: the last `window` tokens and the first `sinks`.  Hot loops pass out and a workspace."""
     B, T, Hq, D = q.shape
-    c, at, table, _, max_pages, n_pages = _kv4(cache, pos, page_table, Hkv, D, page_size, "qspec_attn_kv4")
-    x = _shaped(q, torch.float16, (pos.shape[0], T, Hq, D), cache.device, "q")
+    device, c, at, table, Bp, max_pages, n_pages = _kv4(cache, pos, page_table, Hkv, D, page_size, "qspec_attn_kv4")
+    x = _shaped(q, torch.float16, (Bp, T, Hq, D), device, "q")
     if out is None:
         out = torch.empty_like(q)
     if workspace is None:
         workspace = alloc_workspace(attn_kv4_workspace_bytes(B, T, Hq, Hkv, D))
     _check(lib().qspec_attn_kv4(x, c, at, table, B, T, Hq, Hkv, D, page_size, max_pages, n_pages, D ** -0.5 if scale is None else scale,
-                                window, sinks, _shaped(out, torch.float16, q.shape, cache.device, "out"),
-                                _shaped(workspace, torch.uint8, (workspace.numel(),), cache.device, "workspace"), workspace.numel(), _stream()),
+                                window, sinks, _shaped(out, torch.float16, q.shape, device, "out"),
+                                _shaped(workspace, torch.uint8, (workspace.numel(),), device, "workspace"), workspace.numel(), _stream()),
            "qspec_attn_kv4")
     return out
 
@@ -575,23 +583,26 @@ def sample(logits: torch.Tensor, u: torch.Tensor, temperature: torch.Tensor = No
     top_k int32 [B], each optional.  Returns (None, tokens int32 [B, gamma+1]), or with draft int32 [B, gamma] the acceptance of the
     drafts: (n_accept int32 [B], out_tokens int32 [B, gamma+1]), as greedy_accept does."""
     B, rows, V = logits.shape
-    gamma, device = rows - 1, logits.device
-    x = _here(logits, torch.float16, "logits")
-    per = [None if t is None else _shaped(t, dtype, (B,), device, name)
-           for t, dtype, name in ((temperature, torch.float32, "temperature"), (top_k, torch.int32, "top_k"),
-                                  (top_p, torch.float32, "top_p"), (min_p, torch.float32, "min_p"))]
+    gamma, device = rows - 1, _here(logits, "logits")
+    x = _shaped(logits, torch.float16, (B, rows, V), device, "logits")
+    t = None if temperature is None else _shaped(temperature, torch.float32, (B,), device, "temperature")
+    k = None if top_k is None else _shaped(top_k, torch.int32, (B,), device, "top_k")
+    tp = None if top_p is None else _shaped(top_p, torch.float32, (B,), device, "top_p")
+    mp = None if min_p is None else _shaped(min_p, torch.float32, (B,), device, "min_p")
     if out_tokens is None:
-        out_tokens = torch.empty((B, rows), dtype=torch.int32, device=device)
+        out_tokens = torch.empty((B, rows), dtype=torch.int32, device=logits.device)
     drafts = accepted = ws = None
     nbytes = 0
     if draft is not None:
+        if gamma == 0:
+            raise QSpecError(ERR_SHAPE, "qspec_sample")
         if n_accept is None:
-            n_accept = torch.empty((B,), dtype=torch.int32, device=device)
+            n_accept = torch.empty((B,), dtype=torch.int32, device=logits.device)
         if workspace is None:
-            workspace = torch.empty(max(sample_workspace_bytes(B, gamma, V), 16), dtype=torch.uint8, device=device)
+            workspace = torch.empty(max(sample_workspace_bytes(B, gamma, V), 16), dtype=torch.uint8, device=logits.device)
         drafts = _shaped(draft, torch.int32, (B, gamma), device, "draft")
         accepted = _shaped(n_accept, torch.int32, (B,), device, "n_accept")
         ws, nbytes = _shaped(workspace, torch.uint8, (workspace.numel(),), device, "workspace"), workspace.numel()
-    _check(lib().qspec_sample(x, _shaped(u, torch.float32, (B, rows), device, "u"), *per, drafts, B, gamma, V, accepted,
+    _check(lib().qspec_sample(x, _shaped(u, torch.float32, (B, rows), device, "u"), t, k, tp, mp, drafts, B, gamma, V, accepted,
                               _shaped(out_tokens, torch.int32, (B, rows), device, "out_tokens"), ws, nbytes, _stream()), "qspec_sample")
     return (None if draft is None else n_accept), out_tokens

@@ -15,7 +15,7 @@
 // accumulators into the next operand without crossing lanes, and a lane's codes of four tokens are 16 bytes of the
 // cache (kv4.hpp).
 //
-// Work: an item is one block of rows of one sequence and one key/value head, a step 32 tokens.  The workgroups share
+// Work: an item is one block of rows of one sequence and one key/value head, a step 32 or 64 tokens.  The workgroups share
 // the steps of all items evenly, whatever the lengths, each taking one run of them; the wavefronts of a workgroup
 // take its steps in turn and join their sums through LDS.  An item that several workgroups share is joined by the last of them
 // to finish (last_arrival), from partial sums in the workspace.  The lengths are known on the device only: every
@@ -27,53 +27,26 @@
 
 namespace qspec {
 
-#ifndef QL
-#define QL 4
-#endif
-#ifndef FLYN
-#define FLYN 4
-#endif
-#ifndef TL4
-#define TL4 4
-#define TL2 4
-#define TL1 2
-#endif
-#ifndef W1
-#define W1 4
-#define S1 2
-#define T1 0
-#define GRID 512
-#endif
 constexpr size_t kAttnTicketBytes = 16384;   // arrival counters at the head of the workspace, two a workgroup
-#ifndef MIN1
-#define MIN1 512
-#define MIN2 640
-#define MIN4 1280
-#endif
-#ifndef OVER1
-#define OVER1 1024
-#define OVER2 768
-#define OVER4 512
-#endif
-#ifndef WHOLE
-#define WHOLE 1024
-#endif
-
 // The shape of an instance.  NB: blocks of 16 columns a wavefront carries; F: token tiles that share a block (below).
+// Two workgroups of four wavefronts to a compute unit: the loop is free of spills (a reload inside it waits for every load
+// under way), and one workgroup's start and end of an item stand beside the other's steps.  Workgroups of eight wavefronts, one
+// to a unit, halve the parts of a shared item but leave those gaps open (64 sequences of up to 2000 tokens, 8 heads of
+// 64, 4 rows: 33 us and 24); three of four, where the registers allow them, bring more parts than they hide (131071 tokens: 62 and 47).
 template <int NB, int F>
 struct AttnForm {
-  static constexpr int waves = NB == 1 ? W1 : 4;                    // of a workgroup
-  static constexpr int workgroups = NB == 1 ? GRID : 512;          // of a launch; two parts of an item each in the workspace at most
-  static constexpr int tiles = NB > 1 ? 2 : F == 4 ? TL4 : F == 2 ? TL2 : TL1;      // 16-token tiles of a step
+  static constexpr int waves = 4;
+  static constexpr int workgroups = 512;                           // of a launch; two parts of an item each in the workspace at most
+  static constexpr int tiles = F > 1 ? 4 : 2;                      // 16-token tiles of a step (8 at F = 4: 27 us for 22 at 8 x 2048 tokens)
   static constexpr int step = 16 * tiles;                          // tokens of a step
   static constexpr int rows = 16 * NB / F;                         // rows of a block of an item
-  // in steps: what the start and the end of an item cost beside its steps, items that are not shared out, and what a
-  // workgroup gets on average at least
-  static constexpr int over = (NB == 1 ? OVER1 : NB == 2 ? OVER2 : OVER4) / step;
-  static constexpr int whole = WHOLE / step;
-  static_assert(over >= 2 * waves && (NB == 1 ? MIN1 : NB == 2 ? MIN2 : MIN4) / step >= 2 * waves, "no workgroup's share rounds down to nothing");
+  // In steps: what the start and the end of an item cost beside its steps (measured: 3 us and more, of which an item's
+  // steps of 1024 tokens take as much), items that are not shared out, and what a workgroup gets on average at least.
+  static constexpr int over = (NB == 1 ? 1024 : NB == 2 ? 768 : 512) / step;
+  static constexpr int whole = 1024 / step;
+  static constexpr int least = (NB == 1 ? 512 : NB == 2 ? 640 : 1280) / step;
+  static_assert(over >= 2 * waves && least >= 2 * waves, "no workgroup's share rounds down to nothing");
   static_assert(2 * workgroups * sizeof(unsigned) <= kAttnTicketBytes, "two counters for every workgroup");
-  static constexpr int least = (NB == 1 ? MIN1 : NB == 2 ? MIN2 : MIN4) / step;
 };
 
 struct AttnArgs {
@@ -168,7 +141,7 @@ constexpr size_t attn_workspace() {
 // costs a selection and saves (F - 1) / F of the exponentials and all that goes with them; in the second product a
 // column's weights are zero for the tiles of the others.  Each column ends with its own sums, joined like those of the wavefronts.
 template <int D, int NB, int F>
-__global__ __launch_bounds__((64 * AttnForm<NB, F>::waves), NB == 1 ? S1 : 2) void attn_kv4_kernel(AttnArgs p) {
+__global__ __launch_bounds__((64 * AttnForm<NB, F>::waves), 2) void attn_kv4_kernel(AttnArgs p) {
   typedef AttnForm<NB, F> Form;
   constexpr int WAVES = Form::waves, THREADS = 64 * WAVES, TILES = Form::tiles, STEP = Form::step, RB = Form::rows, OVER = Form::over;
   constexpr int NK = D / 32;                  // matrix instructions of a tile of q k^T; words of a lane of a key
@@ -179,8 +152,8 @@ __global__ __launch_bounds__((64 * AttnForm<NB, F>::waves), NB == 1 ? S1 : 2) vo
   constexpr int PITCH = D + 4;                // floats of a row in LDS
   constexpr int LANES = D / 4;                // threads of a row where sums are joined, 4 features each
   constexpr int PART = attn_part_floats(D);
-  constexpr bool Q_LDS = NB >= QL;             // the rows' registers would not leave room for the sums
-  constexpr bool TIGHT = NB == 4 || (T1 && NB == 1);             // registers for the sums and the loads under way, none for widening ahead
+  constexpr bool Q_LDS = NB == 4;             // the rows' registers would not leave room for the sums
+  constexpr bool TIGHT = NB == 4;                        // registers for the sums and the loads under way, none for widening ahead
   constexpr float kNone = -1e30f;             // reference of a row that has seen nothing: below every score
   __shared__ float o_lds[WAVES][COLS][PITCH];
   __shared__ float m_lds[WAVES][COLS], l_lds[WAVES][COLS], c_lds[WAVES][COLS];
@@ -674,7 +647,7 @@ __global__ __launch_bounds__((64 * AttnForm<NB, F>::waves), NB == 1 ? S1 : 2) vo
           v[0] = v[0] * x + a * y; v[1] = v[1] * x + b2 * y; v[2] = v[2] * x + c2 * y; v[3] = v[3] * x + d2 * y;
         };
         if (r < rows) {
-          constexpr int FLY = FLYN;                    // parts on their way together: each is a trip past the caches
+          constexpr int FLY = 4;                       // parts on their way together: each is a trip past the caches (more only lengthen the code)
           for (int i0 = lot; i0 < (int)n; i0 += FLY * lots) {
             float2 ml[FLY], in[FLY][2];
 #pragma unroll
