@@ -10,8 +10,8 @@
 // and not one of 0 to 15: half the error).
 // A masked nibble in the low bits of a half word IS an fp16 number, code * 2^-24 or 16 * code * 2^-24 (subnormal: exact
 // in the matrix unit, which keeps subnormal operands), so widening a word of 8 codes takes 5 bit operations; the
-// factor of 16 is taken out of q (a power of two that q's row is scaled by first, so that nothing is lost) and out of
-// the finished sums.  The token order of the second product is that of the first one's results: p goes from the
+// factor of 16 is taken out of q (a power of two that q's row is scaled by first, so that nothing is lost); the values'
+// codes are shifted to 16 * code * 2^-24 all alike, and the finished sums scaled.  The token order of the second product is that of the first one's results: p goes from the
 // accumulators into the next operand without crossing lanes, and a lane's codes of four tokens are 16 bytes of the
 // cache (kv4.hpp).
 //
@@ -512,9 +512,10 @@ __global__ __launch_bounds__((64 * AttnForm<NB, F>::waves), 2) void attn_kv4_ker
                                  __builtin_amdgcn_perm(d.y, d.x, sel), __builtin_amdgcn_perm(d.w, d.z, sel)};
 #pragma unroll
           for (int n = 0; n < 4; ++n) {
-            const uint32_t mask = n & 1 ? 0x00F000F0u : 0x000F000Fu;
-            const int by = n & 2 ? 8 : 0;
-            const v8h vf = half_frag(x[0] >> by & mask, x[1] >> by & mask, x[2] >> by & mask, x[3] >> by & mask);
+            // nibbles 0 to 3 of the half words, each as 16 * code * 2^-24.  (As code * 2^-24, one shift less, the unit's sums
+            // lose more bits: with 131071 tokens the result is off by 3.3e-4 for 2.9e-4, of which 2.1e-4 is its own rounding.)
+            const auto nibble = [&](uint32_t w) { return (n == 0 ? w << 4 : w >> (n > 0 ? 4 * n - 4 : 0)) & 0x00F000F0u; };
+            const v8h vf = half_frag(nibble(x[0]), nibble(x[1]), nibble(x[2]), nibble(x[3]));
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb) o[nb][v0 + n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, pf[nb], o[nb][v0 + n], 0, 0, 0);
             if (TIGHT) __builtin_amdgcn_sched_barrier(0);
@@ -572,12 +573,12 @@ __global__ __launch_bounds__((64 * AttnForm<NB, F>::waves), 2) void attn_kv4_ker
           if (D == 128) {
             float x[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = o[nb][((e & 1) * 4 + e / 2) % NV][i] * (e & 2 ? 1048576.0f : 16777216.0f);
+            for (int e = 0; e < 8; ++e) x[e] = o[nb][((e & 1) * 4 + e / 2) % NV][i] * 1048576.0f;
             reinterpret_cast<float4*>(dst)[0] = float4{x[0], x[1], x[2], x[3]};
             reinterpret_cast<float4*>(dst)[1] = float4{x[4], x[5], x[6], x[7]};
           } else {
 #pragma unroll
-            for (int n = 0; n < 4; ++n) dst[2 * n + (kb >> 1)] = o[nb][n][i] * (n & 1 ? 1048576.0f : 16777216.0f);
+            for (int n = 0; n < 4; ++n) dst[2 * n + (kb >> 1)] = o[nb][n][i] * 1048576.0f;
           }
         }
       }
