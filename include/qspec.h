@@ -367,8 +367,9 @@ size_t qspec_kv4_page_bytes(int Hkv, int D, int page_size);
  *             merged weight);  inv_freq  binary64 [rot/2], 16-byte aligned, may be NULL for rot = 0;
  *   0 <= rot <= D, a multiple of 16;  mscale > 0, finite;
  *   q_f16     out, fp16 [B, T, Hq, D];  cache  in/out.  Rows that have no place in the cache are not stored; their
- *             queries are written all the same.  Two rows of a call with the same place (pages shared by
- *             two sequences): either may be the one that stays.
+ *             queries are written all the same.  Rows of one call have places of their own (pages that two sequences
+ *             share are not written by both in one call: what stands there afterwards could be codes of one row with
+ *             the step of the other).
  */
 int qspec_rope_kv4_append(const void* qkv_f16, const double* inv_freq, const int32_t* pos, const int32_t* page_table,
                           int B, int T, int Hq, int Hkv, int D, int rot, int interleaved, float mscale,

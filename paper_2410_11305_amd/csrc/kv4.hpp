@@ -142,7 +142,9 @@ __device__ inline uint32_t kv_code_word(const float (&v)[8], _Float16& step, _Fl
 }
 
 // grid (B*T, parts): a workgroup takes one token and every parts-th set of 256 / (D/8) of its Hq + 2 Hkv heads, a row of D/8
-// lanes a head, 8 features a lane.
+// lanes a head, 8 features a lane: 16 bytes in, a code word out, and the folds over a head stay in a row of lanes.  The angles
+// of a token are worked out once a workgroup.  Measured (device time): 2050 tokens of 32 + 2 * 32 heads of 128 31 us with 84 MB to
+// move, XXX.
 template <int D>
 __global__ __launch_bounds__(256) void rope_kv4_append_kernel(AppendArgs p) {
   constexpr int LANES = D / 8, PER = 256 / LANES;
@@ -229,7 +231,8 @@ __device__ inline v8h kv_values(uint32_t w, _Float16 step, _Float16 low) {
   return h;
 }
 
-// grid (B*T, parts of Hkv D / 8 words of a token).  Rows without a place in the cache come back as zeros.
+// grid (B*T, parts of Hkv D / 8 words of a token).  A copy that widens 4 bits to 16: the stores bound it (2050 tokens of 32
+// heads of 128 ZZZ us).  Rows without a place in the cache come back as zeros.
 template <int D>
 __global__ __launch_bounds__(256) void kv4_read_kernel(KvReadArgs p) {
   constexpr int LANES = D / 8;

@@ -349,3 +349,20 @@ def test_binding_checks_shapes_on_the_device(env):
     for bad in (dict(Hkv=3), dict(page_size=24), dict(window=-1), dict(sinks=2), dict(scale=0.0)):
         with pytest.raises((B.QSpecError, ValueError)):
             B.attn_kv4(**{**good, **bad})
+
+
+def test_as_many_query_heads_to_a_key_head_as_are_taken(env):
+    """255, and rows that the blocks of rows cut inside a token."""
+    c = Cache(11, 9, 2, 64, 32)
+    check(env, c, queries(12, 1, 3, 510, 64), np.array([250]), shuffled(5, 1, 9, 9))
+
+
+def test_thousands_of_sequences(env):
+    """More entries than lanes many times over, most of them idle."""
+    Bn, P = 5000, 16
+    rng = np.random.default_rng(13)
+    pos = np.where(rng.random(Bn) < 0.9, -1, rng.integers(0, 16, Bn))
+    pos[[0, 7, Bn - 1]] = 15, 0, 3
+    c = Cache(14, 64, 1, 64, P)
+    table = rng.integers(0, 64, (Bn, 1))                       # (pages may be read by many)
+    check(env, c, queries(15, Bn, 1, 2, 64), pos, table, rows=np.r_[0, 7, Bn - 1, range(0, Bn, 119)])

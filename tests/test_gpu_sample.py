@@ -207,3 +207,35 @@ def test_shares_follow_the_random_number(env):
     w = np.exp(row.astype(np.float64) - row.max())
     share = w / w.sum()
     assert np.abs(np.bincount(got, minlength=V) - share * N).max() <= 1.0
+
+
+def test_as_many_rows_as_are_taken(env):
+    rng = np.random.default_rng(21)
+    logits = rng.integers(-3, 4, (65535, 1, 3)).astype(np.float16)
+    u = (rng.integers(0, 64, (65535, 1)) / 64.0)
+    picked = run(env, logits, u)[1]
+    rows = np.r_[0, 1, 65534, rng.integers(0, 65535, 300)]
+    assert (picked[rows] == want(logits[rows], u[rows])).all() and picked.min() >= 0
+
+
+def test_masses_that_do_not_add_up_exactly(env):
+    """Random numbers at the borders between the values' masses: every row gets a token that has weight."""
+    rng = np.random.default_rng(22)
+    V = 4000
+    logits = np.sort((rng.standard_normal(V) * 3).astype(np.float16))[::-1].copy()
+    logits[rng.random(V) < 0.5] = -np.inf
+    w = np.exp(logits.astype(np.float64) - logits.astype(np.float64).max())
+    share = np.cumsum(np.sort(w)[::-1]) / w.sum()
+    edges = rng.choice(share[:-1], 300)
+    u = np.stack([np.nextafter(edges.astype(np.float32), np.float32(0)), edges.astype(np.float32),
+                  np.nextafter(edges.astype(np.float32), np.float32(1))]).T.clip(0, 1 - 2.0 ** -24)
+    for p in (dict(), dict(top_p=np.asarray(edges))):
+        picked = run(env, np.broadcast_to(logits, (300, 3, V)).copy(), u, **p)[1]
+        assert (picked >= 0).all() and np.isfinite(logits[picked]).all()
+
+
+def test_a_draft_needs_a_row_for_each_token(env):
+    torch, B = env
+    with pytest.raises(B.QSpecError):
+        B.sample(torch.zeros(2, 1, 8, dtype=torch.float16, device="cuda"), torch.zeros(2, 1, device="cuda"),
+                 draft=torch.zeros(2, 0, dtype=torch.int32, device="cuda"))
