@@ -154,6 +154,7 @@ __global__ __launch_bounds__((64 * AttnForm<NB, F>::waves), 2) void attn_kv4_ker
   constexpr int PART = attn_part_floats(D);
   constexpr bool Q_LDS = NB == 4;             // the rows' registers would not leave room for the sums
   constexpr bool TIGHT = NB == 4;                        // registers for the sums and the loads under way, none for widening ahead
+  constexpr bool WHOLE = NB == 4;             // (fewer rows: one block, or a few, a sequence)
   constexpr float kNone = -1e30f;             // reference of a row that has seen nothing: below every score
   __shared__ float o_lds[WAVES][COLS][PITCH];
   __shared__ float m_lds[WAVES][COLS], l_lds[WAVES][COLS], c_lds[WAVES][COLS];
@@ -214,10 +215,40 @@ __global__ __launch_bounds__((64 * AttnForm<NB, F>::waves), 2) void attn_kv4_ker
     const uint32_t each = uniform(n / (uint32_t)Hkv), head = uniform((x - at) / each), in = x - at - head * each;
     return Place{e, (int)head, each <= Form::whole + OVER || in < OVER ? 0 : (int)((in - OVER) & ~(WAVES - 1u)), at + head * each};
   };
-  const Place from = place_of(start_of(me)), to_place = place_of(start_of(me + 1));
-  int entry = from.entry, head = from.head, begin = from.step;
-  const int last_entry = to_place.entry, last_head = to_place.head, last_step = to_place.step;
-  uint32_t item = from.item;                  // where the item starts
+  // Whole items instead, where they come out as even: a prompt's blocks of rows grow by a step or two from one to the next,
+  // so that the longest and the shortest of two rounds of items add up.  Item i of the order by falling block goes to
+  // workgroup i in the first round of items, from the last workgroup backwards in the second, and so on.  A run that begins inside an item
+  // pays one more start and end, which is what the fullest workgroup may have on top of an even share here.
+  const uint32_t items = (uint32_t)(entries * Hkv), abreast = (uint32_t)(p.B * Hkv);
+  const auto dealt = [&](uint32_t round, uint32_t w) { return round * gridDim.x + (round & 1 ? gridDim.x - 1 - w : w); };
+  bool whole_items = false;
+  if (WHOLE && p.blocks > 1 && items > gridDim.x && items <= 8 * gridDim.x) {
+    const int pos = uniform(scalar_load(p.kv.pos, 0));
+    bool alike = true;
+    for (int e = lane; e < p.B; e += 64) alike &= p.kv.pos[e] == pos;
+    // the fullest: one of the ends, or at the end of the last round
+    const uint32_t rest = items % gridDim.x, w = lane == 0 ? 0 : lane == 1 ? gridDim.x - 1 : lane == 2 ? max(rest, 1u) - 1 : gridDim.x - max(rest, 1u);
+    uint32_t load = 0;
+    for (uint32_t round = 0; round * gridDim.x < items; ++round) {
+      const uint32_t i = dealt(round, w);
+      if (i < items) load += (uint32_t)(OVER + attn_span<STEP>(p, pos, p.blocks - 1 - (int)(i / abreast), RB).steps);
+    }
+    whole_items = __builtin_amdgcn_ballot_w64(alike && (lane > 3 || load <= share + OVER)) == ~0ull;
+  }
+  int entry, head, begin = 0, last_entry = entries, last_head = 0, last_step = 0;
+  uint32_t item = 0, round = 0;               // item: where it starts
+  const auto take = [&] {                     // the whole item of a round
+    const uint32_t i = dealt(round, me), from_top = uniform(i / abreast), rest = i - from_top * abreast, b = uniform(rest / (uint32_t)Hkv);
+    entry = i < items ? (int)(b * (uint32_t)p.blocks + (uint32_t)p.blocks - 1 - from_top) : entries;
+    head = (int)(rest - b * (uint32_t)Hkv);
+  };
+  if (WHOLE && whole_items) {
+    take();
+  } else {
+    const Place from = place_of(start_of(me)), to = place_of(start_of(me + 1));
+    entry = from.entry; head = from.head; begin = from.step; item = from.item;
+    last_entry = to.entry; last_head = to.head; last_step = to.step;
+  }
   bool first_run = true;
 
   while (entry < last_entry || (entry == last_entry && (head < last_head || (head == last_head && begin < last_step)))) {
@@ -683,6 +714,11 @@ __global__ __launch_bounds__((64 * AttnForm<NB, F>::waves), 2) void attn_kv4_ker
         }
         __syncthreads();
       }
+    }
+    if (WHOLE && whole_items) {
+      ++round;
+      take();
+      continue;
     }
     item += (uint32_t)(OVER + span.steps);
     begin = 0;

@@ -366,3 +366,18 @@ def test_thousands_of_sequences(env):
     c = Cache(14, 64, 1, 64, P)
     table = rng.integers(0, 64, (Bn, 1))                       # (pages may be read by many)
     check(env, c, queries(15, Bn, 1, 2, 64), pos, table, rows=np.r_[0, 7, Bn - 1, range(0, Bn, 119)])
+
+
+@pytest.mark.parametrize("Bn,T,Hq,Hkv,D,first", [(2, 300, 64, 64, 64, (0, 0)), (2, 300, 64, 64, 64, (0, 9)), (1, 1100, 32, 32, 64, (0,)), (3, 200, 50, 50, 128, (5, 5, 5)),
+                                                (1, 700, 96, 48, 64, (-40,)), (1, 330, 90, 90, 64, (900,)), (4, 1000, 8, 8, 64, (0, 0, 0, 0))])
+def test_prompts_of_more_blocks_than_workgroups(env, Bn, T, Hq, Hkv, D, first):
+    """Blocks of rows that are dealt out whole, and (lengths or histories that differ) ones that are not."""
+    torch, B = env
+    P, n = 64, T + max(first)
+    each = -(-n // P)
+    c = Cache(T, Bn * each, Hkv, D, P)
+    args = (env, c, queries(T, Bn, T, Hq, D), np.array(first), shuffled(T, Bn, each, Bn * each))
+    ws = B.alloc_workspace(B.attn_kv4_workspace_bytes(Bn, T, Hq, Hkv, D))
+    a = check(*args, workspace=ws, rows=[0, Bn - 1])
+    assert torch.equal(a, check(*args, workspace=ws, rows=[0])) and int(ws[:16384].count_nonzero()) == 0
+    check(*args, window=150, sinks=3, workspace=ws, rows=[0])
