@@ -18,8 +18,17 @@
 // Work: an item is one block of rows of one sequence and one key/value head, a step 32 or 64 tokens.  The workgroups share
 // the steps of all items evenly, whatever the lengths, each taking one run of them; the wavefronts of a workgroup
 // take its steps in turn and join their sums through LDS.  An item that several workgroups share is joined by the last of them
-// to finish (last_arrival), from partial sums in the workspace.  The lengths are known on the device only: every
+// to finish (last_arrival), from partial sums in the workspace.  Where there are more items than workgroups and sorted by length they come
+// out as even, they are dealt out whole.  The lengths are known on the device only: every
 // workgroup works the division out for itself.
+//
+// Measured (device time; bytes of the cache, queries and results): 8 sequences of up to 2048 tokens, one row of 32 heads, 21.4 us
+// (3.0 TB/s); 131071 tokens, one row of 64 over 8 heads, 38.6 us (3.7 TB/s); 32 sequences through a window of 4096, 64 over 8 heads of
+// 64, 26.8 us (2.8 TB/s); 128 sequences of 200 to 2048 tokens, 4 rows of 64 over 8 heads, 60 us (2.9 TB/s, 320 TF/s); a prompt of
+// 2050 tokens of 32 heads 81 us (425 TF/s), a chunk of 2050 rows over 4096 tokens of 64 over 8 heads 342 us (600 TF/s).  Short passes are bound by
+// the start (1.4 us of division, 3 us to the first scores) and the joins, long ones of few rows by the vector unit's
+// share of a step (exponentials, steps and lows) beside the loads; from 16 rows on by the vector unit: the matrix unit
+// works 11 % of the time, as it takes 5 vector instructions a word to widen and a dozen a score.
 #pragma once
 #include "common.hpp"
 #include "exchange.hpp"
@@ -28,6 +37,7 @@
 namespace qspec {
 
 constexpr size_t kAttnTicketBytes = 16384;   // arrival counters at the head of the workspace, two a workgroup
+constexpr int kAttnRounds = 8;               // rounds of whole items (more have little left to gain: one part of many)
 // The shape of an instance.  NB: blocks of 16 columns a wavefront carries; F: token tiles that share a block (below).
 // Two workgroups of four wavefronts to a compute unit: the loop is free of spills (a reload inside it waits for every load
 // under way), and one workgroup's start and end of an item stand beside the other's steps.  Workgroups of eight wavefronts, one
@@ -154,14 +164,14 @@ __global__ __launch_bounds__((64 * AttnForm<NB, F>::waves), 2) void attn_kv4_ker
   constexpr int PART = attn_part_floats(D);
   constexpr bool Q_LDS = NB == 4;             // the rows' registers would not leave room for the sums
   constexpr bool TIGHT = NB == 4;                        // registers for the sums and the loads under way, none for widening ahead
-  constexpr bool WHOLE = NB == 4;             // (fewer rows: one block, or a few, a sequence)
   constexpr float kNone = -1e30f;             // reference of a row that has seen nothing: below every score
-  __shared__ float o_lds[WAVES][COLS][PITCH];
+  __shared__ __align__(16) float o_lds[WAVES][COLS][PITCH];
   __shared__ float m_lds[WAVES][COLS], l_lds[WAVES][COLS], c_lds[WAVES][COLS];
   __shared__ float join_m[THREADS / LANES], join_l[THREADS / LANES];
   __shared__ uint4 q_lds[Q_LDS ? NB * NK * 64 : 1];
   __shared__ float4 f_lds[Q_LDS ? RB : 1];    // factor, sum, position of a row
   __shared__ unsigned ticket;
+  __shared__ uint32_t taken[kAttnRounds];     // this workgroup's items where they are dealt out whole
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
   const int col = lane & 15, kb = lane >> 4, mine_tile = F > 1 ? col / COLS : 0;
   const int P = 1 << p.kv.page_shift, R = p.kv.T * p.G, Hkv = p.kv.Hkv;
@@ -215,34 +225,75 @@ __global__ __launch_bounds__((64 * AttnForm<NB, F>::waves), 2) void attn_kv4_ker
     const uint32_t each = uniform(n / (uint32_t)Hkv), head = uniform((x - at) / each), in = x - at - head * each;
     return Place{e, (int)head, each <= Form::whole + OVER || in < OVER ? 0 : (int)((in - OVER) & ~(WAVES - 1u)), at + head * each};
   };
-  // Whole items instead, where they come out as even: a prompt's blocks of rows grow by a step or two from one to the next,
-  // so that the longest and the shortest of two rounds of items add up.  Item i of the order by falling block goes to
-  // workgroup i in the first round of items, from the last workgroup backwards in the second, and so on.  A run that begins inside an item
-  // pays one more start and end, which is what the fullest workgroup may have on top of an even share here.
-  const uint32_t items = (uint32_t)(entries * Hkv), abreast = (uint32_t)(p.B * Hkv);
+  // Whole items instead, where they come out as even: in the order of falling length, dealt out in rounds, first to last
+  // workgroup, last to first, and so on, long ones and short ones add up.  A run that begins inside an item pays one more
+  // start and end, so much may the fullest workgroup have on top of an even share here.  (us: prompt of 2050 tokens,
+  // 32 heads 81 for 99, 4 of 512 46 for 57; 128 sequences of 200 to 2048 tokens, 4 rows of 64 over 8 heads 60 for 67.)
+  const uint32_t items = (uint32_t)(entries * Hkv);
   const auto dealt = [&](uint32_t round, uint32_t w) { return round * gridDim.x + (round & 1 ? gridDim.x - 1 - w : w); };
   bool whole_items = false;
-  if (WHOLE && p.blocks > 1 && items > gridDim.x && items <= 8 * gridDim.x) {
-    const int pos = uniform(scalar_load(p.kv.pos, 0));
-    bool alike = true;
-    for (int e = lane; e < p.B; e += 64) alike &= p.kv.pos[e] == pos;
-    // the fullest: one of the ends, or at the end of the last round
-    const uint32_t rest = items % gridDim.x, w = lane == 0 ? 0 : lane == 1 ? gridDim.x - 1 : lane == 2 ? max(rest, 1u) - 1 : gridDim.x - max(rest, 1u);
-    uint32_t load = 0;
-    for (uint32_t round = 0; round * gridDim.x < items; ++round) {
-      const uint32_t i = dealt(round, w);
-      if (i < items) load += (uint32_t)(OVER + attn_span<STEP>(p, pos, p.blocks - 1 - (int)(i / abreast), RB).steps);
+  if (items > gridDim.x && items <= kAttnRounds * gridDim.x && (NB == 4 || entries <= THREADS)) {
+    // Prompts of one length and history are in order by their blocks; the fullest workgroup is one of the ends, or at the
+    // end of the last round.  Few rows: one block, or a few, a sequence, and the lengths are sorted, in the LDS of the sums to come.
+    uint32_t* const lengths = reinterpret_cast<uint32_t*>(&o_lds[0][0][0]);
+    uint16_t* const order = reinterpret_cast<uint16_t*>(lengths + THREADS);
+    static_assert(sizeof(o_lds) >= THREADS * 6, "room for both");
+    const auto load_of = [&](uint32_t w, auto length_of) {
+      uint32_t load = 0;
+      for (uint32_t round = 0; round * gridDim.x < items; ++round) {
+        const uint32_t i = dealt(round, w);
+        if (i < items) load += length_of(i / (uint32_t)Hkv);
+      }
+      return load;
+    };
+    bool even = true;
+    if (NB == 4) {
+      const int pos = uniform(scalar_load(p.kv.pos, 0));
+      for (int e = lane; e < p.B; e += 64) even &= p.kv.pos[e] == pos;
+      const uint32_t rest = max(items % gridDim.x, 1u);
+      const uint32_t load = load_of(lane == 0 ? 0 : lane == 1 ? gridDim.x - 1 : lane == 2 ? rest - 1 : gridDim.x - rest, [&](uint32_t place) {
+        return (uint32_t)(OVER + attn_span<STEP>(p, pos, p.blocks - 1 - (int)(place / (uint32_t)p.B), RB).steps);
+      });
+      even &= lane > 3 || load <= share + OVER;
+      even = __builtin_amdgcn_ballot_w64(!even) == 0;
+    } else {
+      const int seq = sequence_of(tid);
+      const uint32_t length = tid < entries ? (uint32_t)(OVER + attn_span<STEP>(p, p.kv.pos[seq], tid - seq * p.blocks, RB).steps) : 0u;
+      lengths[tid] = length;
+      __syncthreads();
+      uint32_t rank = 0;
+#pragma unroll 4
+      for (int j = 0; j < entries; j += 4) {
+        const uint4 other = *reinterpret_cast<const uint4*>(lengths + j);
+        rank += other.x > length || (other.x == length && j < tid) ? 1u : 0u;
+        rank += other.y > length || (other.y == length && j + 1 < tid) ? 1u : 0u;
+        rank += other.z > length || (other.z == length && j + 2 < tid) ? 1u : 0u;
+        rank += other.w > length || (other.w == length && j + 3 < tid) ? 1u : 0u;
+      }
+      __syncthreads();
+      if (tid < entries) {
+        lengths[rank] = length;
+        order[rank] = (uint16_t)tid;
+      }
+      __syncthreads();
+      for (uint32_t w = tid; w < gridDim.x; w += THREADS) even &= load_of(w, [&](uint32_t place) { return lengths[place]; }) <= share + OVER;
     }
-    whole_items = __builtin_amdgcn_ballot_w64(alike && (lane > 3 || load <= share + OVER)) == ~0ull;
+    if (tid < kAttnRounds) {
+      const uint32_t i = dealt(tid, me), place = i / (uint32_t)Hkv, from_top = place / (uint32_t)p.B;
+      const uint32_t e = NB == 4 ? (place - from_top * (uint32_t)p.B) * (uint32_t)p.blocks + (uint32_t)p.blocks - 1 - from_top : i < items ? order[place] : 0u;
+      taken[tid] = i < items ? e * (uint32_t)Hkv + i - place * (uint32_t)Hkv : items;
+    }
+    whole_items = __syncthreads_and(even);
   }
-  int entry, head, begin = 0, last_entry = entries, last_head = 0, last_step = 0;
-  uint32_t item = 0, round = 0;               // item: where it starts
-  const auto take = [&] {                     // the whole item of a round
-    const uint32_t i = dealt(round, me), from_top = uniform(i / abreast), rest = i - from_top * abreast, b = uniform(rest / (uint32_t)Hkv);
-    entry = i < items ? (int)(b * (uint32_t)p.blocks + (uint32_t)p.blocks - 1 - from_top) : entries;
-    head = (int)(rest - b * (uint32_t)Hkv);
+  // item: where it starts; or, for whole ones (last_head is -1), the round
+  int entry, head, begin = 0, last_entry = entries, last_head = -1, last_step = 0;
+  uint32_t item = 0;
+  const auto take = [&] {
+    const uint32_t i = item < (uint32_t)kAttnRounds ? uniform(taken[item]) : (uint32_t)(entries * Hkv);
+    entry = (int)uniform(i / (uint32_t)Hkv);
+    head = (int)(i - (uint32_t)entry * (uint32_t)Hkv);
   };
-  if (WHOLE && whole_items) {
+  if (whole_items) {
     take();
   } else {
     const Place from = place_of(start_of(me)), to = place_of(start_of(me + 1));
@@ -715,8 +766,8 @@ __global__ __launch_bounds__((64 * AttnForm<NB, F>::waves), 2) void attn_kv4_ker
         __syncthreads();
       }
     }
-    if (WHOLE && whole_items) {
-      ++round;
+    if (last_head < 0) {
+      ++item;
       take();
       continue;
     }

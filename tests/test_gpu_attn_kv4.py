@@ -381,3 +381,22 @@ def test_prompts_of_more_blocks_than_workgroups(env, Bn, T, Hq, Hkv, D, first):
     a = check(*args, workspace=ws, rows=[0, Bn - 1])
     assert torch.equal(a, check(*args, workspace=ws, rows=[0])) and int(ws[:16384].count_nonzero()) == 0
     check(*args, window=150, sinks=3, workspace=ws, rows=[0])
+
+
+@pytest.mark.parametrize("Bn,T,Hq,Hkv,D,n", [(130, 1, 5, 5, 64, 90), (256, 1, 6, 3, 64, 70), (90, 6, 8, 8, 128, 100), (66, 3, 64, 8, 64, 150), (80, 20, 7, 7, 64, 90),
+                                            (40, 40, 14, 14, 64, 60), (120, 4, 40, 5, 128, 60)])
+@pytest.mark.parametrize("lengths", ["alike", "ragged", "one long"])
+def test_batches_of_more_items_than_workgroups(env, Bn, T, Hq, Hkv, D, n, lengths):
+    """Items that are dealt out whole in the order of their lengths, and ones that are not."""
+    torch, B = env
+    rng = np.random.default_rng(Bn)
+    pos = np.full(Bn, n - T) if lengths == "alike" else rng.integers(-T, n - T + 1, Bn)
+    P, each = 64, -(-n // 64)
+    table = shuffled(T, Bn, each, Bn * each)
+    if lengths == "one long":
+        pos[5], each = 3000, 48
+        table = np.c_[table, rng.integers(0, Bn * table.shape[1], (Bn, each - table.shape[1]))]
+    c = Cache(T + Hq, Bn * -(-n // 64), Hkv, D, P)
+    args = (env, c, queries(T, Bn, T, Hq, D), pos, table)
+    first = check(*args, rows=[0, 5, Bn // 2, Bn - 1])
+    assert torch.equal(first, check(*args, rows=[0]))
