@@ -25,10 +25,11 @@
 // Measured (device time; bytes of the cache, queries and results): 8 sequences of up to 2048 tokens, one row of 32 heads, 21.4 us
 // (3.0 TB/s); 131071 tokens, one row of 64 over 8 heads, 38.6 us (3.7 TB/s); 32 sequences through a window of 4096, 64 over 8 heads of
 // 64, 26.8 us (2.8 TB/s); 128 sequences of 200 to 2048 tokens, 4 rows of 64 over 8 heads, 60 us (2.9 TB/s, 320 TF/s); a prompt of
-// 2050 tokens of 32 heads 81 us (425 TF/s), a chunk of 2050 rows over 4096 tokens of 64 over 8 heads 342 us (600 TF/s).  Short passes are bound by
+// 2050 tokens of 32 heads 77 us (445 TF/s), a chunk of 2050 rows over 4096 tokens of 64 over 8 heads 331 us (620 TF/s).  Short passes are bound by
 // the start (1.4 us of division, 3 us to the first scores) and the joins, long ones of few rows by the vector unit's
-// share of a step (exponentials, steps and lows) beside the loads; from 16 rows on by the vector unit: the matrix unit
-// works 11 % of the time, as it takes 5 vector instructions a word to widen and a dozen a score.
+// share of a step (exponentials, steps and lows) beside the loads.  From 17 rows on the vector unit issues in 54 % of its cycles (32
+// rows), 35 % (64, two wavefronts a SIMD and the LDS reads of q between), the matrix unit works in 12 %: it takes 5 to 7 vector
+// instructions a word to widen and a dozen a score.
 #pragma once
 #include "common.hpp"
 #include "exchange.hpp"
@@ -164,6 +165,7 @@ __global__ __launch_bounds__((64 * AttnForm<NB, F>::waves), 2) void attn_kv4_ker
   constexpr int PART = attn_part_floats(D);
   constexpr bool Q_LDS = NB == 4;             // the rows' registers would not leave room for the sums
   constexpr bool TIGHT = NB == 4;                        // registers for the sums and the loads under way, none for widening ahead
+  constexpr int kPass = 0x108;                // past the fences: matrix instructions and LDS reads (us, prompts: 80 -> 77, 342 -> 331)
   constexpr float kNone = -1e30f;             // reference of a row that has seen nothing: below every score
   __shared__ __align__(16) float o_lds[WAVES][COLS][PITCH];
   __shared__ float m_lds[WAVES][COLS], l_lds[WAVES][COLS], c_lds[WAVES][COLS];
@@ -472,7 +474,7 @@ __global__ __launch_bounds__((64 * AttnForm<NB, F>::waves), 2) void attn_kv4_ker
 #pragma unroll
           for (int i = 0; i < TILES; ++i) sc[nb][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf[i], x, sc[nb][i], 0, 0, 0);
         }
-        if (TIGHT) __builtin_amdgcn_sched_barrier(0);          // (widening ahead would cost the registers of the sums)
+        if (TIGHT) __builtin_amdgcn_sched_barrier(kPass);          // (widening ahead would cost the registers of the sums)
       }
       load_keys(t_next, next);
 
@@ -499,7 +501,6 @@ __global__ __launch_bounds__((64 * AttnForm<NB, F>::waves), 2) void attn_kv4_ker
           for (int i = 1; i < F; ++i) dot = mine_tile == i ? sc[nb][(x >> 2) * F + i][x & 3] : dot;
           sv[nb][x] = fmaf(dot, (float)kp[x].x, (float)kp[x].y * sum_of);
         }
-        if (TIGHT) __builtin_amdgcn_sched_barrier(0);
       }
       if (!whole) {
         uint32_t any = 0;                     // bit x: a row of this lane sees its token x
@@ -572,7 +573,7 @@ __global__ __launch_bounds__((64 * AttnForm<NB, F>::waves), 2) void attn_kv4_ker
           c[nb] = __builtin_amdgcn_fdot2(both, minus8, c[nb], false);
           w[nb][x / 2] = __builtin_bit_cast(uint32_t, both);
         }
-        if (TIGHT) __builtin_amdgcn_sched_barrier(0);
+        if (TIGHT) __builtin_amdgcn_sched_barrier(kPass);
       }
       // values, two tiles at a time: token pairs of one half of the words, nibble by nibble
 #pragma unroll
@@ -600,7 +601,7 @@ __global__ __launch_bounds__((64 * AttnForm<NB, F>::waves), 2) void attn_kv4_ker
             const v8h vf = half_frag(nibble(x[0]), nibble(x[1]), nibble(x[2]), nibble(x[3]));
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb) o[nb][v0 + n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, pf[nb], o[nb][v0 + n], 0, 0, 0);
-            if (TIGHT) __builtin_amdgcn_sched_barrier(0);
+            if (TIGHT) __builtin_amdgcn_sched_barrier(kPass);
           }
         };
         if (D == 128) {
