@@ -11,9 +11,9 @@
 // A masked nibble in the low bits of a half word IS an fp16 number, code * 2^-24 or 16 * code * 2^-24 (subnormal: exact
 // in the matrix unit, which keeps subnormal operands), so widening a word of 8 codes takes 5 bit operations; the
 // factor of 16 is taken out of q (a power of two that q's row is scaled by first, so that nothing is lost); the values'
-// codes are shifted to 16 * code * 2^-24 all alike, and the finished sums scaled.  The token order of the second product is that of the first one's results: p goes from the
-// accumulators into the next operand without crossing lanes, and a lane's codes of four tokens are 16 bytes of the
-// cache (kv4.hpp).
+// codes are shifted to 16 * code * 2^-24 all alike, and the finished sums scaled.  The token order of the second product
+// is that of the first one's results: p goes from the accumulators into the next operand without crossing lanes, and a
+// lane's codes of four tokens are 16 bytes of the cache (kv4.hpp).
 //
 // Work: an item is one block of rows of one sequence and one key/value head, a step 32 or 64 tokens.  The workgroups share
 // the steps of all items evenly, whatever the lengths, each taking one run of them; the wavefronts of a workgroup
