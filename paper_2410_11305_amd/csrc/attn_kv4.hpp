@@ -710,6 +710,9 @@ __global__ __launch_bounds__((64 * AttnForm<NB, F>::waves), 2) void attn_kv4_ker
       if (stage == 0) {
         first = w0 + ((me - w0) & ~7u);
         n = min(8u, w1 + 1 - first);
+        // One on its own has its part in place already.  It must not count: the next item's first eight may begin with this
+        // workgroup, and would count at the same place.  (Sets of two or more begin with a workgroup that is inside their item.)
+        if (n == 1) continue;
         counter = Form::workgroups + first;
       } else if (parts > 16) {
         stride = 8;

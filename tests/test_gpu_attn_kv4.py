@@ -11,6 +11,7 @@ import numpy as np
 import pytest
 
 from oracle import kv4_oracle as kv
+from tests.test_attn_division import NEIGHBOURS
 
 pytestmark = pytest.mark.gpu
 
@@ -400,3 +401,16 @@ def test_batches_of_more_items_than_workgroups(env, Bn, T, Hq, Hkv, D, n, length
     args = (env, c, queries(T, Bn, T, Hq, D), pos, table)
     first = check(*args, rows=[0, 5, Bn // 2, Bn - 1])
     assert torch.equal(first, check(*args, rows=[0]))
+
+
+@pytest.mark.parametrize("T,Hq,Hkv,n", NEIGHBOURS)
+def test_neighbouring_items_of_many_parts_are_joined_apart(env, T, Hq, Hkv, n):
+    """The last workgroup of an item's parts is the first of the next one's (which calls those are: the division's test)."""
+    torch, B = env
+    each, D = -(-n // 256), 64
+    c = Cache(n, each, Hkv, D, 256)
+    ws = B.alloc_workspace(B.attn_kv4_workspace_bytes(1, T, Hq, Hkv, D))
+    args = (env, c, queries(n, 1, T, Hq, D, 2.0), np.array([n - T]), shuffled(3, 1, each, each))
+    first = check(*args, workspace=ws)
+    assert int(ws[:16384].count_nonzero()) == 0
+    assert torch.equal(first, check(*args, workspace=ws)) and int(ws[:16384].count_nonzero()) == 0
