@@ -5,7 +5,7 @@ runs at the length it was trained on.  For contexts `factor` times longer than `
   linear  every frequency divided by factor (positions squeezed into the trained range)
   ntk     theta raised to theta * factor^(rot / (rot - 2)): the slowest pair turns factor times slower, the fastest as before
   yarn    pairs with fewer than `slow` turns over the trained length divided by factor, those with more than `fast` left
-          alone, a linear blend in between (over the index of the pair); queries and keys scaled by 0.1 ln(factor) + 1
+          alone, a linear blend in between (over the index of the pair, from whole index to whole index); queries and keys scaled by 0.1 ln(factor) + 1
 """
 from __future__ import annotations
 
@@ -36,7 +36,8 @@ def frequencies(rot: int, theta: float = 10000.0, scaling: str = None, factor: f
             raise ValueError("yarn scaling needs original >= 1 and fast > slow > 0")
         # index of the pair that makes n turns over the trained length
         index = lambda n: rot * math.log(original / (n * 2.0 * math.pi)) / (2.0 * math.log(theta))
-        low, high = max(math.floor(index(fast)), 0), min(math.ceil(index(slow)), rot // 2 - 1)
+        # (past the last pair, rot / 2 - 1, where all of them make `slow` turns: the line to there is not squeezed)
+        low, high = max(math.floor(index(fast)), 0), min(math.ceil(index(slow)), rot - 1)
         for i in range(rot // 2):
             squeezed = min(max((i - low) / max(high - low, 1e-3), 0.0), 1.0)
             inv[i] = inv[i] * (1.0 - squeezed) + inv[i] / factor * squeezed

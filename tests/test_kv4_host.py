@@ -124,6 +124,21 @@ def test_yarn_frequencies():
     assert torch_all(ratio[1:] <= ratio[:-1])
 
 
+@pytest.mark.parametrize("rot,theta,factor,original", [(128, 10000.0, 8.0, 131072), (16, 10000.0, 4.0, 32768), (64, 10000.0, 32.0, 4096), (128, 500000.0, 8.0, 8192),
+                                                      (64, 500.0, 2.0, 2 ** 20)])
+def test_yarn_blend_where_every_pair_makes_a_turn(rot, theta, factor, original):
+    """The blend is a straight line over the index, also where its end lies past the last pair: what lies before is not squeezed."""
+    f, _ = rope.frequencies(rot, theta, device="cpu")
+    y, _ = rope.frequencies(rot, theta, "yarn", factor, original, device="cpu")
+    index = lambda turns: rot * math.log(original / (turns * 2 * math.pi)) / (2 * math.log(theta))
+    low, high = max(math.floor(index(32.0)), 0), min(math.ceil(index(1.0)), rot - 1)
+    want = [min(max((i - low) / (high - low), 0.0), 1.0) for i in range(rot // 2)]
+    share = (1.0 - (y / f).numpy()) / (1.0 - 1.0 / factor)
+    assert np.abs(share - want).max() < 1e-12
+    turns = (original * f / (2 * math.pi)).numpy()
+    assert (share[turns > theta ** (2 / rot)] < 1.0).all()    # only pairs of about one turn and fewer are divided by the whole factor
+
+
 def torch_all(t):
     return t.numel() > 0 and bool(t.all())
 
