@@ -84,16 +84,20 @@ struct AttnSpan {
   int lo, hi;                // positions of its first and its last row
 };
 
-// pos: position of the sequence's first row.  (Held to +-2^30, far outside of any cache, so that sums stay in 32 bits.)
+// The position that a row of a block's window begins behind.  (A row in front of the sequence sees nothing, whatever its window.)
+__device__ __forceinline__ int behind_window(const AttnArgs& p, int at) { return max(at, 0) - p.window; }
+
+// pos: position of the sequence's first row.  (Held, so that sums stay in 32 bits: from below far in front of the sequence, where rows see nothing,
+// from above to the last positions that there are.)
 template <int STEP>
 __device__ __forceinline__ AttnSpan attn_span(const AttnArgs& p, int pos, int block, int rows_per_block) {
   const int r0 = block * rows_per_block, r1 = min(p.kv.T * p.G, r0 + rows_per_block) - 1;
-  pos = min(max(pos, -(1 << 30)), 1 << 30);
+  pos = min(max(pos, -(1 << 30)), 0x7fffffff - p.kv.T);
   AttnSpan s;
   s.lo = pos + over_group(p, r0);
   s.hi = pos + over_group(p, r1);
   const int end = min(s.hi + 1, p.kv.max_pages << p.kv.page_shift);      // tokens 0 .. end - 1
-  s.first = p.window > 0 ? max(s.lo - p.window + 1, 0) / STEP : 0;
+  s.first = p.window > 0 ? max(behind_window(p, s.lo) + 1, 0) / STEP : 0;
   s.sink_steps = p.window > 0 ? max(min((min(p.sinks, end) + STEP - 1) / STEP, s.first), 0) : 0;
   // at least one: rows that see nothing have their zeros written
   s.steps = max(s.sink_steps + max((end + STEP - 1) / STEP - s.first, 0), 1);
@@ -457,7 +461,7 @@ __global__ __launch_bounds__((64 * AttnForm<NB, F>::waves), 2) void attn_kv4_ker
       }
       const Pages next = pages_of(k);
       // every token of the step in sight of every row
-      const bool whole = pages.there == (1u << TILES) - 1 && t + STEP - 1 <= span.lo && (p.window == 0 || t > span.hi - p.window || t + STEP <= p.sinks);
+      const bool whole = pages.there == (1u << TILES) - 1 && t + STEP - 1 <= span.lo && (p.window == 0 || t > behind_window(p, span.hi) || t + STEP <= p.sinks);
       v4f sc[NB][TILES];
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb)
@@ -506,7 +510,7 @@ __global__ __launch_bounds__((64 * AttnForm<NB, F>::waves), 2) void attn_kv4_ker
         uint32_t any = 0;                     // bit x: a row of this lane sees its token x
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
-          const int at_row = position(nb), behind = p.window > 0 ? at_row - p.window : -0x7fffffff - 1;
+          const int at_row = position(nb), behind = p.window > 0 ? behind_window(p, at_row) : -1;
 #pragma unroll
           for (int x = 0; x < NX; ++x) {
             const int tok = t + ((x >> 2) * F + mine_tile) * 16 + 4 * kb + (x & 3);

@@ -414,3 +414,20 @@ def test_neighbouring_items_of_many_parts_are_joined_apart(env, T, Hq, Hkv, n):
     first = check(*args, workspace=ws)
     assert int(ws[:16384].count_nonzero()) == 0
     assert torch.equal(first, check(*args, workspace=ws)) and int(ws[:16384].count_nonzero()) == 0
+
+
+@pytest.mark.parametrize("window,sinks", [(2 ** 31 - 1, 0), (2 ** 31 - 1, 3), (2 ** 30 + 7, 1)])
+@pytest.mark.parametrize("T,G,D", [(6, 1, 64), (20, 2, 128), (70, 1, 64)])
+def test_windows_as_large_as_they_come(env, window, sinks, T, G, D):
+    """No token is behind them, also where a block begins with rows in front of the sequence."""
+    c = Cache(31, 12, 1, D, 32)
+    check(env, c, queries(32, 4, T, G, D), np.array([-5, 1 - T, 0, 90]), shuffled(8, 4, 3, 12)[:, [0, 1, 2, 2, 2, 2]], window=window, sinks=sinks)
+
+
+def test_windows_of_rows_far_past_the_cache(env):
+    """A window that still reaches the cache from there."""
+    T = 4
+    for pos in (2 ** 30 + 5, 2 ** 31 - 2 ** 20, 2 ** 31 - 1 - T):
+        c = Cache(33, 4, 2, 64, 64)
+        got = check(env, c, queries(34, 1, T, 4, 64), np.array([pos]), np.arange(4).reshape(1, 4), window=pos - 150, sinks=5)
+        assert (got != 0).all()
