@@ -384,8 +384,9 @@ int qspec_kv4_read(const void* cache, const int32_t* pos, const int32_t* page_ta
  * Attention over the 4-bit cache, on the values it stands for:
  *   out[b, j, h] = sum_t softmax_t(scale * q[b, j, h] . k[b, t, h / G]) v[b, t, h / G],   G = Hq / Hkv,
  * over the tokens t that are in the cache with t <= p = pos[b] + j and, if window > 0, t > p - window or t < sinks (the
- * window counts p itself).  A row that sees nothing gets zeros.  What stands in rows that no row of
- * the same sequence sees does not matter.  fp32 sums; the weights enter the second product in fp16.
+ * window counts p itself).  A row that sees nothing gets zeros, whatever its query.  What stands in rows that no row of
+ * the same sequence sees does not matter.  A row whose query holds a NaN or an infinity, or that sees a key or value with NaN for
+ * step or low, gets NaN.  fp32 sums; the weights enter the second product in fp16.
  *   q_f16   fp16 [B, T, Hq, D], e.g. from qspec_rope_kv4_append, whose rows of the same call are seen;
  *   1e-10 <= scale <= 1e10;  window >= 0 (0: none);  sinks >= 0 (0 without a window);
  *   out_f16 out, fp16 [B, T, Hq, D];

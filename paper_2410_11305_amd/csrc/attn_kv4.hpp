@@ -396,6 +396,7 @@ __global__ __launch_bounds__((64 * AttnForm<NB, F>::waves), 2) void attn_kv4_ker
       }
       top = column_max(top);
       sum = column_sum(sum);
+      sum += sum - sum;                       // no number if one of the features is none, and then no score is
       const int ex = top > 0.0f ? __builtin_amdgcn_frexp_expf(top) : 0;
       const float up = __builtin_amdgcn_ldexpf(1.0f, 14 - ex);
 #pragma unroll
@@ -625,11 +626,11 @@ __global__ __launch_bounds__((64 * AttnForm<NB, F>::waves), 2) void attn_kv4_ker
     const uint32_t w0 = shared ? group_of(item + OVER + WAVES - 1) : me, w1 = shared ? group_of(item + OVER + span.steps - 1) : me;   // the workgroups that hold a part of it
     const auto write_row = [&](int r, const float (&v)[4], float sum) {
       const int j = over_group(p, r), g = r - j * p.G;
-      const float by = sum > 0.0f ? 1.0f / sum : 0.0f;
+      const float by = 1.0f / sum;            // (0: a row that saw nothing, and no other)
       typedef _Float16 v4h __attribute__((ext_vector_type(4)));
       v4h h;
 #pragma unroll
-      for (int x = 0; x < 4; ++x) h[x] = (_Float16)(sum > 0.0f ? fminf(fmaxf(v[x] * by, -65504.0f), 65504.0f) : 0.0f);   // (a 15th code may lie past fp16's end)
+      for (int x = 0; x < 4; ++x) h[x] = sum == 0.0f ? (_Float16)0.0f : held_to_half(v[x] * by);
       *reinterpret_cast<v4h*>(p.out + (((size_t)b * p.kv.T + j) * p.Hq + (size_t)head * p.G + g) * D + own) = h;
     };
     const auto write_part = [&](uint32_t slot, int r, float ref, float sum, const float (&v)[4]) {

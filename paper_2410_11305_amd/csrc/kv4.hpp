@@ -48,6 +48,12 @@ __device__ inline _Float16 half_of_f64(double v) {
   return (_Float16)__builtin_bit_cast(float, (high & 0x80000000u) | (uint32_t)magnitude << 3);
 }
 
+// A value in fp16.  A step that was rounded up can carry the 15th code of a row that fills fp16's range past its end: the largest finite
+// value then.  What is no number, or infinite, stays so.
+__device__ __forceinline__ _Float16 held_to_half(float x) {
+  return (_Float16)(fabsf(x) < __builtin_inff() ? fminf(fmaxf(x, -65504.0f), 65504.0f) : x);
+}
+
 // cos and sin of `turns` whole turns, to a few units in the last place of binary64: the nearest quarter turn off, then
 // the Taylor series on +-pi/4 (the first terms left out are below 2^-58).
 __device__ inline void cos_sin_turns(double turns, double& c, double& s) {

@@ -431,3 +431,51 @@ def test_windows_of_rows_far_past_the_cache(env):
         c = Cache(33, 4, 2, 64, 64)
         got = check(env, c, queries(34, 1, T, 4, 64), np.array([pos]), np.arange(4).reshape(1, 4), window=pos - 150, sinks=5)
         assert (got != 0).all()
+
+
+@pytest.mark.parametrize("T,G,n", [(1, 1, 100), (1, 8, 3000), (4, 4, 700), (20, 1, 5000), (70, 1, 400), (3, 1, 20000)])
+@pytest.mark.parametrize("what", ["key", "value"])
+def test_a_token_that_is_no_number_shows(env, T, G, n, what):
+    """NaN for step and low of a token that every row sees: NaN, in the sums of one workgroup and in joined ones; the other head keeps its result."""
+    torch, B = env
+    P, D, Hkv = 64, 64, 2
+    each = -(-n // P)
+    c = Cache(37, each, Hkv, D, P)
+    q, pos, table = dev(torch, queries(38, 1, T, G * Hkv, D)), torch.tensor([n - T], dtype=torch.int32, device="cuda"), torch.arange(each, dtype=torch.int32, device="cuda").view(1, -1)
+    want = B.attn_kv4(q, dev(torch, c.bytes()), pos, Hkv, P, table)
+    for at in (0, n // 3, n - T):
+        d = Cache(37, each, Hkv, D, P)
+        for a in (d.ks, d.kl) if what == "key" else (d.vs, d.vl):
+            a[at // P, 0, at % P] = np.nan
+        got = B.attn_kv4(q, dev(torch, d.bytes()), pos, Hkv, P, table)
+        assert got[:, :, :G].isnan().all() and torch.equal(got[:, :, G:], want[:, :, G:]), at
+
+
+@pytest.mark.parametrize("T,G,n", [(1, 1, 1), (1, 8, 3000), (4, 4, 700), (20, 1, 5000), (70, 1, 400)])
+def test_a_query_that_is_no_number_shows(env, T, G, n):
+    """A NaN or an infinity in one feature of one row: NaN there, the other rows and heads keep their results."""
+    torch, B = env
+    P, D, Hkv = 64, 128, 2
+    each = -(-n // P)
+    c = Cache(39, each, Hkv, D, P)
+    c.kl[:] = 0.5                                             # all keys positive: a negative infinity would weigh every token with zero
+    q = queries(40, 1, T, G * Hkv, D)
+    cache, pos, table = dev(torch, c.bytes()), torch.tensor([n - T], dtype=torch.int32, device="cuda"), torch.arange(each, dtype=torch.int32, device="cuda").view(1, -1)
+    want = B.attn_kv4(dev(torch, q), cache, pos, Hkv, P, table).cpu().numpy()
+    j, h = T // 2, G * Hkv - 1
+    for bad in (np.nan, np.inf, -np.inf):
+        for d in (0, 70, D - 1):
+            p = q.copy()
+            p[0, j, h, d] = bad
+            got = B.attn_kv4(dev(torch, p), cache, pos, Hkv, P, table).cpu().numpy()
+            assert np.isnan(got[0, j, h]).all(), (bad, d)
+            got[0, j, h] = want[0, j, h]
+            compare(got.astype(np.float64), c, q, np.array([n - T]), np.arange(each).reshape(1, each), None, 0, 0)
+
+
+def test_rows_that_see_nothing_stay_zero_whatever_the_query(env):
+    torch, B = env
+    c = Cache(41, 2, 1, 64, 16)
+    q = np.full((2, 3, 2, 64), np.nan, np.float16)
+    got = B.attn_kv4(dev(torch, q), dev(torch, c.bytes()), torch.tensor([-3, -2], dtype=torch.int32, device="cuda"), 1, 16, torch.tensor([[0], [1]], dtype=torch.int32, device="cuda"))
+    assert (got[0] == 0).all() and (got[1, :2] == 0).all() and got[1, 2].isnan().all()
