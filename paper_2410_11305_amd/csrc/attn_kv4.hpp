@@ -624,13 +624,15 @@ __global__ __launch_bounds__((64 * AttnForm<NB, F>::waves), 2) void attn_kv4_ker
     // ---- the wavefronts' sums, a block of columns at a time
     const bool shared = begin > 0 || stop < span.steps;
     const uint32_t w0 = shared ? group_of(item + OVER + WAVES - 1) : me, w1 = shared ? group_of(item + OVER + span.steps - 1) : me;   // the workgroups that hold a part of it
-    const auto write_row = [&](int r, const float (&v)[4], float sum) {
+    const auto write_row = [&](int r, const float (&v)[4], float sum, float ref) {
       const int j = over_group(p, r), g = r - j * p.G;
-      const float by = 1.0f / sum;            // (0: a row that saw nothing, and no other)
+      // From 2^28 on a reference can be too far off to keep the weights inside fp16's range, down to all of them zero or infinite.
+      const bool none = sum == 0.0f && ref == kNone;
+      const float by = fabsf(ref) < 134217728.0f ? 1.0f / sum : __builtin_nanf("");
       typedef _Float16 v4h __attribute__((ext_vector_type(4)));
       v4h h;
 #pragma unroll
-      for (int x = 0; x < 4; ++x) h[x] = sum == 0.0f ? (_Float16)0.0f : held_to_half(v[x] * by);
+      for (int x = 0; x < 4; ++x) h[x] = none ? (_Float16)0.0f : held_to_half(v[x] * by);
       *reinterpret_cast<v4h*>(p.out + (((size_t)b * p.kv.T + j) * p.Hq + (size_t)head * p.G + g) * D + own) = h;
     };
     const auto write_part = [&](uint32_t slot, int r, float ref, float sum, const float (&v)[4]) {
@@ -697,7 +699,7 @@ __global__ __launch_bounds__((64 * AttnForm<NB, F>::waves), 2) void attn_kv4_ker
 #pragma unroll
         for (int x = 0; x < 4; ++x) v[x] += total_c;
         if (!shared) {
-          write_row(block * RB + r, v, total_l);
+          write_row(block * RB + r, v, total_l, ref);
         } else {
           write_part(2 * me + (first_run ? 0 : 1), r, ref, total_l, v);
         }
@@ -769,7 +771,7 @@ __global__ __launch_bounds__((64 * AttnForm<NB, F>::waves), 2) void attn_kv4_ker
           }
         }
         if (lot == 0 && r < rows) {
-          if (stage == 1) write_row(block * RB + r, v, sum);
+          if (stage == 1) write_row(block * RB + r, v, sum, ref);
           else write_part(slot_of(first), r, ref, sum, v);
         }
         __syncthreads();

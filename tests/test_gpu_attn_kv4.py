@@ -479,3 +479,29 @@ def test_rows_that_see_nothing_stay_zero_whatever_the_query(env):
     q = np.full((2, 3, 2, 64), np.nan, np.float16)
     got = B.attn_kv4(dev(torch, q), dev(torch, c.bytes()), torch.tensor([-3, -2], dtype=torch.int32, device="cuda"), 1, 16, torch.tensor([[0], [1]], dtype=torch.int32, device="cuda"))
     assert (got[0] == 0).all() and (got[1, :2] == 0).all() and got[1, 2].isnan().all()
+
+
+@pytest.mark.parametrize("T,G,first", [(1, 1, 89), (4, 2, 2996), (20, 1, 1980), (70, 1, 230), (70, 1, -3)])
+def test_scores_past_what_is_told_apart(env, T, G, first):
+    """Scores of up to 2^26: the token with the largest weighs everything, where it leads by more than their rounding.  Past 2^27 a row is no
+    number, but for rows that see nothing."""
+    torch, B = env
+    P, D = 64, 64
+    each = -(-(first + T) // P)
+    c, table, pos = Cache(43, each, 1, D, P), np.arange(each).reshape(1, each), np.array([first])
+    q = queries(44, 1, T, G, D)
+    k, v, _, step = c.sequence(table[0], first + T)
+    s = q[0].astype(np.float64) @ k[:, 0].T                   # [T, G, tokens]
+    s[np.broadcast_to(np.arange(first + T) > first + np.arange(T)[:, None, None], s.shape)] = -np.inf
+    sees = np.arange(T) + first >= 0
+    fits = float(np.float32(2.0 ** 26 / np.abs(s[np.isfinite(s)]).max()))
+    got = check(env, c, q, pos, table, scale=fits).cpu().numpy()[0].astype(np.float64)
+    with np.errstate(invalid="ignore"):
+        lead = np.sort(s, -1)[..., -1] - (np.sort(s, -1)[..., -2] if first + T > 1 else -np.inf)
+    rounding = (D + 12) * 2.0 ** -24 * np.abs(q[0].astype(np.float64)).sum(-1) * np.abs(k).max() * 4
+    for j, h in np.argwhere((lead > rounding + 64 / fits) & sees[:, None]):
+        want = v[s[j, h].argmax(), 0]
+        assert (np.abs(got[j, h] - want) <= 2.0 ** -11 * np.abs(want) + 2.0 ** -11 * 8 * step.max()).all(), (j, h)
+    for scale in (float(2.0 ** 27 / np.abs(s.max(-1)[sees]).min()), 1e10):
+        out = B.attn_kv4(dev(torch, q), dev(torch, c.bytes()), dev(torch, pos.astype(np.int32)), 1, P, dev(torch, table.astype(np.int32)), scale).cpu().numpy()[0]
+        assert np.isnan(out[sees]).all() and (out[~sees] == 0).all()
