@@ -388,8 +388,8 @@ int qspec_kv4_read(const void* cache, const int32_t* pos, const int32_t* page_ta
  * the same sequence sees does not matter.  A row whose query holds a NaN or an infinity, or that sees a key or value with NaN for
  * step or low, gets NaN.  fp32 sums; the weights enter the second product in fp16.
  *   q_f16   fp16 [B, T, Hq, D], e.g. from qspec_rope_kv4_append, whose rows of the same call are seen;
- *   1e-10 <= scale <= 1e10, with scores, scale * q . k, within +-2^26 (binary32 tells
- *           numbers of that size 4 apart, past it too few: a row may be NaN then, and is where its largest score passes 2^27);  window >= 0 (0: none);  sinks >= 0 (0 without a window);
+ *   1e-10 <= scale <= 1e10, with scores, scale * q . k, within +-2^26 (binary32 tells numbers of that size 4 apart; past it a row
+ *           may be NaN, and is where its largest score passes 2^27);  window >= 0 (0: none);  sinks >= 0 (0 without a window);
  *   out_f16 out, fp16 [B, T, Hq, D];
  *   workspace  qspec_attn_kv4_workspace_bytes(...) bytes; the workspace rule at qspec_workspace_bytes holds, and one
  *           workspace may serve these calls and the products in turn.

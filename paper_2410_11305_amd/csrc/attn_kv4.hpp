@@ -523,6 +523,22 @@ __global__ __launch_bounds__((64 * AttnForm<NB, F>::waves), 2) void attn_kv4_ker
         // whatever stands in rows that nobody sees (infinities, NaN) must not meet a weight, not even one of zero
 #pragma unroll
         for (int x = 0; x < NX; ++x) vp[x] = any >> x & 1u ? vp[x] : v2h{(_Float16)0.0f, (_Float16)0.0f};
+        if (NB > 1) {
+          // nor, in a token that only some of the lane's rows see, the weights of zero of the others: it is taken out, and its NaN left with the rows that see it
+          const v2h zero = {(_Float16)0.0f, (_Float16)0.0f};
+          v2h odd = vp[0] * zero;
+#pragma unroll
+          for (int x = 1; x < NX; ++x) odd += vp[x] * zero;
+          if (__builtin_amdgcn_ballot_w64(!((float)odd.x + (float)odd.y == 0.0f)) != 0) {
+#pragma unroll
+            for (int x = 0; x < NX; ++x) {
+              const float none = (float)vp[x].x * 0.0f + (float)vp[x].y * 0.0f;
+#pragma unroll
+              for (int nb = 0; nb < NB; ++nb) c[nb] += sv[nb][x] == -__builtin_inff() ? 0.0f : none;
+              vp[x] = none == 0.0f ? vp[x] : zero;
+            }
+          }
+        }
       }
       // The reference: 2^(s - m) times the value steps has to stay inside fp16's range, with its largest terms well above its
       // smallest numbers, so m is the largest score less 8, plus the exponent of the largest value step.  It moves

@@ -505,3 +505,27 @@ def test_scores_past_what_is_told_apart(env, T, G, first):
     for scale in (float(2.0 ** 27 / np.abs(s.max(-1)[sees]).min()), 1e10):
         out = B.attn_kv4(dev(torch, q), dev(torch, c.bytes()), dev(torch, pos.astype(np.int32)), 1, P, dev(torch, table.astype(np.int32)), scale).cpu().numpy()[0]
         assert np.isnan(out[sees]).all() and (out[~sees] == 0).all()
+
+
+@pytest.mark.parametrize("T,G,D,window", [(3, 1, 64, 0), (9, 1, 128, 4), (20, 1, 64, 0), (40, 1, 64, 0), (70, 1, 128, 0), (100, 2, 64, 0), (70, 1, 128, 9), (20, 1, 128, 6)])
+@pytest.mark.parametrize("bad", [(np.nan, np.nan, np.nan, np.nan), (0.25, -2.0, np.inf, 0.0), (0.25, -2.0, 0.25, -np.inf), (0.25, -2.0, np.nan, 0.0)])
+def test_what_later_rows_see_does_not_reach_earlier_ones(env, T, G, D, window, bad):
+    """A token of the call whose step or low is not finite: rows before it (and rows whose window has passed it) are as if it were not there, the rows
+    that see it are not finite."""
+    torch, B = env
+    first, P, Hkv = 35, 32, 2
+    at = first + T // 2
+    each = -(-(first + T) // P)
+    c, table = Cache(35, each, Hkv, D, P), np.arange(each).reshape(1, each)
+    q, pos = queries(36, 1, T, G * Hkv, D), np.array([first])
+    clean = c.bytes()
+    for a, x in zip((c.ks, c.kl, c.vs, c.vl), bad):
+        a[at // P, 1, at % P] = x                             # the second head's alone
+    call = lambda raw: B.attn_kv4(dev(torch, q), dev(torch, raw), dev(torch, pos.astype(np.int32)), Hkv, P, dev(torch, table.astype(np.int32)), window=window).cpu().numpy()[0]
+    got = call(c.bytes())
+    sees = np.array([kv.visible(first + j, each * P, window, 0)[at] for j in range(T)])
+    assert sees.any() and not sees.all()
+    assert not np.isfinite(got[sees, G:]).any()
+    want = Cache(35, each, Hkv, D, P)
+    got[sees, G:] = call(clean)[sees, G:]
+    compare(got[None].astype(np.float64), want, q, pos, table, None, window, 0)
