@@ -37,7 +37,7 @@ __device__ __forceinline__ int kv_page(const KvShape& s, int b, long long at) {
   return page >= 0 && page < s.n_pages ? page : -1;
 }
 
-// A finite binary64 value to fp16 in one rounding: cut to 20 bits of significand with a last bit that remembers what was
+// A binary64 value (NaN: an infinity) to fp16 in one rounding: cut to 20 bits of significand with a last bit that remembers what was
 // cut off (9 bits more than fp16 has; round to odd), put together as binary32, then to nearest even.  Whole-number operations: the
 // conversions from and to binary64 take four times as long as any of them.
 __device__ inline _Float16 half_of_f64(double v) {
@@ -198,6 +198,19 @@ __global__ __launch_bounds__(256) void rope_kv4_append_kernel(AppendArgs p) {
           const double a = (double)(float)x[e], c = (double)(float)z[e];
           h[e] = half_of_f64(a * t.x + (upper ? c : -c) * t.y);
         }
+      }
+    }
+    // What is no finite number: a lane that has any, of the whole wavefront.  Rare, so what has to be done about it stands apart.
+    const v2h nothing = {(_Float16)0.0f, (_Float16)0.0f};
+    const v2h odd = v2h{h[0], h[1]} * nothing + v2h{h[2], h[3]} * nothing + (v2h{h[4], h[5]} * nothing + v2h{h[6], h[7]} * nothing);
+    const uint64_t odd_lanes = __builtin_amdgcn_ballot_w64(!((float)odd.x + (float)odd.y == 0.0f));
+    if (odd_lanes != 0 && in_rot && now < p.Hq + p.kv.Hkv) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {                         // (rounding has made infinities of the NaN among them)
+        const double2 t = turn[p.interleaved ? 4 * l + e / 2 : 8 * l + e - (upper ? half : 0)];
+        const double a = (double)(float)x[e], c = (double)(float)(p.interleaved ? x[e ^ 1] : z[e]);
+        const double r = a * t.x + ((p.interleaved ? (e & 1) != 0 : upper) ? c : -c) * t.y;
+        h[e] = r == r ? h[e] : (_Float16)__builtin_nanf("");
       }
     }
     if (now < p.Hq) p.q[((size_t)token * p.Hq + now) * LANES + l] = __builtin_bit_cast(uint4, h);

@@ -184,3 +184,19 @@ def test_binding_checks_shapes_on_the_device(env):
         B.kv4_read(cache, pos, 2, 2, 64, 16, k=torch.empty((2, 1, 2, 64), dtype=torch.float16, device="cuda"))
     with pytest.raises(B.QSpecError):
         B.kv4_read(cache, pos, 0, 2, 64, 16)
+
+
+@pytest.mark.parametrize("rot,interleaved", [(64, False), (64, True), (32, False), (16, True)])
+def test_rotated_queries_keep_what_is_no_number(env, rot, interleaved):
+    """NaN stays NaN and infinities what the rotation makes of them: infinite, or NaN beside another one or at an angle of zero."""
+    torch, B = env
+    rng, Hq, T, D = np.random.default_rng(50), 5, 9, 64
+    x = rng.standard_normal((T, Hq + 2, D)).astype(np.float16)
+    bad = rng.random((T, Hq, D)) < 0.1
+    x[:, :Hq][bad] = rng.choice([np.nan, np.inf, -np.inf], bad.sum())
+    cache, pos = B.alloc_kv4_cache(1, 1, D, 16), torch.zeros(1, dtype=torch.int32, device="cuda")
+    q = B.rope_kv4_append(dev(torch, x.reshape(1, T, -1)), dev(torch, FREQ(rot)), pos, cache, Hq, 1, 16, interleaved=interleaved)[0].cpu().numpy()
+    with np.errstate(invalid="ignore"):
+        want = kv.rotate(x[:, :Hq], np.arange(T), FREQ(rot), interleaved)
+    np.testing.assert_array_equal(q, want)
+    assert np.isnan(want).any() and np.isinf(want).any()
