@@ -336,7 +336,8 @@ int qspec_kv_overwrite(const void* kv_verify_f16, const int32_t* n_accept, const
  * fp16 scales; the paper keeps the cache itself in fp16, this form is the library's).  A token's key (after rotation)
  * or value of one head, x[0 .. D-1] in fp16, is stored as
  *   low = min x (a zero is +0),  step = fp16((max x - low) / 15),  code = clamp(rne((x - low) / step), 0, 15)   (step 0: codes 0)
- * with the quotient decided exactly; it stands for code * step + low.  step and low are fp16.
+ * with the quotient decided exactly; it stands for code * step + low.  step and low are fp16.  A row that holds a NaN or an
+ * infinity is stored with NaN for step and low and codes 0: all of it reads as NaN.
  *   cache   n_pages pages of qspec_kv4_page_bytes bytes.  A page holds page_size tokens (a power of two, 16 or more)
  *           of every key/value head; per head, page_size * (D + 8) bytes:
  *             page_size rows of D/2 bytes       key codes, 32-bit word w of a row: features 8w .. 8w+7
@@ -376,7 +377,7 @@ int qspec_rope_kv4_append(const void* qkv_f16, const double* inv_freq, const int
                           int page_size, int max_pages, int n_pages, void* q_f16, void* cache, void* stream);
 
 /* Values of rows pos[b] .. pos[b] + T - 1 of the cache: k_f16, v_f16 out, fp16 [B, T, Hkv, D] (code * step + low in
- * binary32, then rounded and held to fp16's finite range); zeros for rows that have no place in it. */
+ * binary32, then rounded, finite ones held to fp16's finite range); zeros for rows that have no place in it. */
 int qspec_kv4_read(const void* cache, const int32_t* pos, const int32_t* page_table, int B, int T, int Hkv, int D,
                    int page_size, int max_pages, int n_pages, void* k_f16, void* v_f16, void* stream);
 

@@ -8,7 +8,8 @@ pass's entries, Sec. 3.1; the 4-bit form is this library's):
   rotation   pair (a, b) at position p: mscale (a cos t - b sin t), mscale (b cos t + a sin t), t = p inv_freq[i],
              rounded once to fp16; pairs (i, i + rot/2) or (2i, 2i + 1)
   codes      per token and head: low = min x, step = fp16((max x - low) / 15), code = clamp(rne((x - low) / step), 0, 15)
-             with the quotient in rational arithmetic (half way: to even); step 0: code 0
+             with the quotient in rational arithmetic (half way: to even); step 0: code 0.  A row with a NaN or an infinity:
+             step and low NaN, codes 0
   attention  softmax(scale q k) v over the tokens in the cache at t <= p, inside the window or among the sinks; a row
              that sees nothing gives zeros
 
@@ -37,13 +38,14 @@ def rotate(x: np.ndarray, positions: np.ndarray, inv_freq: np.ndarray, interleav
 
 def quantise(x: np.ndarray):
     """x fp16 [..., D] -> (codes uint8 [..., D], step fp16 [...], low fp16 [...])."""
-    y = x.astype(np.float64)
+    number = np.isfinite(x).all(-1)
+    y = np.where(number[..., None], x.astype(np.float64), 0.0)
     low = y.min(-1) + 0.0                                     # a zero is +0
     step = ((y.max(-1) + 0.0 - low) / 15.0).astype(np.float16)
     s = step.astype(np.float64)[..., None]
     quotient = (y - low[..., None]) / np.where(s > 0, s, 1.0)
     codes = np.where(s > 0, np.clip(np.rint(quotient), 0, 15), 0).astype(np.uint8)
-    return codes, step, low.astype(np.float16)
+    return codes, np.where(number, step, np.float16(np.nan)), np.where(number, low.astype(np.float16), np.float16(np.nan))
 
 
 def quantise_exactly(x) -> list:

@@ -3,7 +3,7 @@
 // Quantisation, per token and head over its D features (asymmetric: the rotated keys of a token are far from
 // symmetric, and the extra fp16 per row is 3 % of it), everything that decides a code exact:
 //   low = min x, step = fp16((max x - low) / 15), code = clamp(rne((x - low) / step), 0, 15); step 0 gives codes 0
-// A value is code * step + low.
+// A value is code * step + low.  A row that holds a NaN or an infinity has NaN for step and low and codes 0: none of its values is a number.
 //
 // A page holds P tokens of every key/value head; per head, one region of P (D + 8) bytes:
 //   keys    P rows of D/2 bytes, word w holding features 8w .. 8w+7
@@ -219,7 +219,11 @@ __global__ __launch_bounds__(256) void rope_kv4_append_kernel(AppendArgs p) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[e] = (float)h[e];
       _Float16 step, low;
-      const uint32_t word = kv_code_word<LANES>(v, step, low);
+      uint32_t word = kv_code_word<LANES>(v, step, low);
+      if (odd_lanes != 0 && (odd_lanes >> (threadIdx.x & 63 & ~(LANES - 1)) & ((1u << LANES) - 1)) != 0) {      // in one of the row's lanes
+        word = 0u;
+        step = low = __builtin_bit_cast(_Float16, (uint16_t)0x7E00);
+      }
       if (page >= 0) {
         const bool value = now >= p.Hq + p.kv.Hkv;
         uint8_t* const region = regions + (size_t)(now - p.Hq - (value ? p.kv.Hkv : 0)) * ((size_t)P * (D + 8));
@@ -239,14 +243,12 @@ struct KvReadArgs {
   uint4* v;
 };
 
-// 8 codes of a word times step plus low, each rounded once to binary32 and once to fp16.  (A step that was rounded up can
-// carry the 15th code of a row that fills fp16's range past its end: the largest finite value then.)
+// 8 codes of a word times step plus low, each rounded once to binary32 and once to fp16.
 __device__ inline v8h kv_values(uint32_t w, _Float16 step, _Float16 low) {
   v8h h;
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
-    const float x = rounded_f32(fmaf((float)((w >> (4 * nibble_pos(e))) & 15u), (float)step, (float)low));
-    h[e] = (_Float16)fminf(fmaxf(x, -65504.0f), 65504.0f);
+    h[e] = held_to_half(rounded_f32(fmaf((float)((w >> (4 * nibble_pos(e))) & 15u), (float)step, (float)low)));
   }
   return h;
 }

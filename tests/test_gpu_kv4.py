@@ -200,3 +200,58 @@ def test_rotated_queries_keep_what_is_no_number(env, rot, interleaved):
         want = kv.rotate(x[:, :Hq], np.arange(T), FREQ(rot), interleaved)
     np.testing.assert_array_equal(q, want)
     assert np.isnan(want).any() and np.isinf(want).any()
+
+
+def run_without_numbers(env, x, freq, pos, table, n_pages, Hq, Hkv, P, interleaved=False):
+    """run_append for heads x fp16 [T, Hq + 2 Hkv, D] of one sequence that hold infinities and NaN: a NaN is a NaN, whatever its bits, but in the cache."""
+    torch, B = env
+    T, heads, D = x.shape
+    plain, cache = Plain(n_pages, Hkv, D, P), B.alloc_kv4_cache(n_pages, Hkv, D, P)
+    at, tab = dev(torch, np.array([pos], dtype=np.int32)), dev(torch, table.astype(np.int32))
+    q = B.rope_kv4_append(dev(torch, x.reshape(1, T, -1)), None if freq is None else dev(torch, freq), at, cache, Hq, Hkv, P, tab, interleaved=interleaved)
+    k, v = B.kv4_read(cache, at, T, Hkv, D, P, tab)
+    with np.errstate(over="ignore", invalid="ignore"):
+        turned = x[:, :Hq + Hkv] if freq is None else kv.rotate(x[:, :Hq + Hkv], pos + np.arange(T), freq, interleaved)
+    np.testing.assert_array_equal(q[0].cpu().numpy(), turned[:, :Hq])
+    for j in range(T):
+        plain.put(*place(table, 0, pos + j, P, n_pages), turned[j, Hq:], x[j, Hq + Hkv:])
+    assert (cache.cpu().numpy() == plain.bytes()).all()
+    for got, rows in ((k, turned[:, Hq:]), (v, x[:, Hq + Hkv:])):
+        assert (got[0].isnan().cpu().numpy() == ~np.isfinite(rows).all(-1, keepdims=True)).all()
+    return turned
+
+
+@pytest.mark.parametrize("D,rot,interleaved", [(64, 64, False), (128, 64, True), (128, 128, False), (64, 0, False)])
+def test_values_that_are_no_numbers(env, D, rot, interleaved):
+    """A query keeps NaN and infinities where the rotation leaves them; a key or value row that has one is stored with NaN for step and low and codes
+    of zero, and reads back as NaN; the rows beside it are what they were."""
+    rng = np.random.default_rng(51)
+    Hq, Hkv, T = 3, 2, 24
+    x = rng.standard_normal((T, Hq + 2 * Hkv, D)).astype(np.float16)
+    for j, bad in enumerate((np.nan, np.inf, -np.inf) * 7):
+        for h in range(j % 3, Hq + 2 * Hkv, 3):
+            x[j, h, rng.integers(0, D)] = bad
+    x[22, :, 5], x[22, :, 7] = np.inf, -np.inf                # both
+    x[23] = np.nan
+    turned = run_without_numbers(env, x, FREQ(rot) if rot else None, 13, np.array([[1, 2, 0]]), 3, Hq, Hkv, 16, interleaved)
+    assert np.isnan(turned).any() and np.isinf(turned).any() and np.isfinite(turned).all(-1).any()
+
+
+def test_rotation_past_the_largest_number(env):
+    """A rotated key that leaves fp16's range is an infinity: its row has no numbers either."""
+    x = np.full((2, 3, 64), 1.0, np.float16)
+    x[1, :2, 0] = x[1, :2, 32] = 60000.0
+    turned = run_without_numbers(env, x, FREQ(64), 40, np.array([[0, 1, 2]]), 3, 1, 1, 16)
+    assert np.isinf(turned[1]).any() and np.isfinite(turned[0]).all()
+
+
+def test_steps_and_lows_that_are_no_numbers_read_back_as_such(env):
+    torch, B = env
+    plain = Plain(1, 1, 64, 16)
+    plain.k[:], plain.v[:] = 3, 15
+    plain.ks[:], plain.kl[:], plain.vs[:], plain.vl[:] = 1.0, 2.0, 8737.6, -65504.0
+    for slot, (step, low) in enumerate(((np.nan, np.nan), (np.inf, 0.0), (0.0, -np.inf), (1.0, np.nan))):
+        plain.ks[0, 0, slot], plain.kl[0, 0, slot], plain.vs[0, 0, slot], plain.vl[0, 0, slot] = step, low, step, low
+    k, v = B.kv4_read(dev(torch, plain.bytes()), torch.zeros(1, dtype=torch.int32, device="cuda"), 5, 1, 64, 16)
+    np.testing.assert_array_equal(k[0, :, 0, 0].cpu().numpy(), [np.nan, np.inf, -np.inf, np.nan, 5.0])
+    np.testing.assert_array_equal(v[0, :, 0, 0].cpu().numpy(), [np.nan, np.inf, -np.inf, np.nan, 65504.0])    # (15 * 8736 - 65504 = 65536, a finite value: held)

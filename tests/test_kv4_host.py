@@ -164,6 +164,15 @@ def test_oracle_quantiser_decides_in_rational_arithmetic():
             assert np.abs(kv.values(codes, step, low) - x.astype(np.float64)).max() <= float(step) * (0.5 + 15 * 2.0 ** -11)
 
 
+def test_oracle_rows_that_hold_no_number():
+    x = np.zeros((4, 64), np.float16)
+    x[0, 3], x[1, 63], x[2, 0], x[3, 7] = np.nan, np.inf, -np.inf, 15.0
+    codes, step, low = kv.quantise(x)
+    assert step.view(np.uint16)[:3].tolist() == low.view(np.uint16)[:3].tolist() == [0x7E00] * 3 and not codes[:3].any()
+    assert step[3] == 1.0 and low[3] == 0.0 and codes[3].tolist() == [15 if i == 7 else 0 for i in range(64)]
+    assert np.isnan(kv.values(codes, step, low)[:3]).all()
+
+
 def test_oracle_rotation_keeps_lengths_and_differences_of_positions():
     rng = np.random.default_rng(2)
     f = 10000.0 ** (-np.arange(0, 32, 2) / 32.0)
