@@ -382,8 +382,11 @@ __global__ __launch_bounds__(kSampleThreads) void sample_kernel(SampleArgs p) {
   const uint64_t hit = __builtin_amdgcn_ballot_w64(x.n && x.upto > target), have = __builtin_amdgcn_ballot_w64(x.n && x.weight > 0.0);
   const int at = hit ? __builtin_ctzll(hit) : 63 - __builtin_clzll(have | 1ull);
   const double into = fmax(target - (x.upto - (double)x.n * x.weight), 0.0) / x.weight;
-  const uint32_t key = (uint32_t)__builtin_amdgcn_readlane((int)x.key, at);
-  const uint32_t rank = (uint32_t)__builtin_amdgcn_readlane((int)(x.n ? min((uint32_t)fmin(into, 4e9), x.n - 1) : 0u), at);
+  // (none: a block whose weights are below binary64 one by one, though not in the polynomial, and which the scans' rounding gave the target.  The
+  // largest value then: every value that is looked for below has a token.)
+  const bool some = (hit | have) != 0;
+  const uint32_t key = some ? (uint32_t)__builtin_amdgcn_readlane((int)x.key, at) : top;
+  const uint32_t rank = some ? (uint32_t)__builtin_amdgcn_readlane((int)(x.n ? min((uint32_t)fmin(into, 4e9), x.n - 1) : 0u), at) : 0u;
 
   // ---- which of the tokens of that value: matches of every wavefront and trip, in the order of the indices
   __syncthreads();
