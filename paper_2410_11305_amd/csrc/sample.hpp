@@ -43,11 +43,12 @@ struct SampleArgs {
 };
 
 // exp(x) for x <= 0 in binary64, to about a unit in the last place: n ln 2 off in two parts, the Taylor polynomial of
-// degree 13 on +-ln 2 / 2 (the next term is below 2^-57).
+// degree 13 on +-ln 2 / 2 (the next term is below 2^-57).  The parts: ln 2 cut to 40 bits, which n (11 bits) multiplies exactly, and what is left of it.
 __device__ inline double exp_negative(double x) {
   x = fmax(x, -800.0);
   const double n = rint(x * 1.44269504088896340736);
-  const double r = fma(n, -1.90821492927058770002e-10, fma(n, -6.93147180369123816490e-01, x));
+  const double ln2 = 0x1.62e42fefa2p-1, ln2_rest = 0x1.9ef35793c7673p-41;
+  const double r = fma(n, -ln2_rest, fma(n, -ln2, x));
   double e = 1.0 / 6227020800.0;
   e = fma(e, r, 1.0 / 479001600.0);
   e = fma(e, r, 1.0 / 39916800.0);

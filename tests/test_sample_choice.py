@@ -1,7 +1,9 @@
-"""The last step of sampling looks for one token of the chosen value and goes to the place where it found it: the value has to have one.
+"""What the sampling kernel rests on and no call shows.  The last step of sampling looks for one token of the chosen value and goes to the place where it found it: the value has to have one.
 The choice inside a block is restated here, with what the source does where no value of the block has weight.  Needs no GPU."""
 import os
 import re
+from decimal import Decimal, getcontext
+from fractions import Fraction
 
 import pytest
 
@@ -32,3 +34,11 @@ def test_the_chosen_value_has_a_token(tokens, weight):
 def test_the_choice_is_the_sources():
     assert "const int at = hit ? __builtin_ctzll(hit) : 63 - __builtin_clzll(have | 1ull);" in DRAW
     assert "ballot_w64(x.n && x.upto > target), have = __builtin_amdgcn_ballot_w64(x.n && x.weight > 0.0);" in DRAW
+
+
+def test_the_two_parts_of_ln_2():
+    """The first has few enough bits for an exact product with any exponent; both together are ln 2 to 2^-93."""
+    getcontext().prec = 50
+    whole, rest = (Fraction(float.fromhex(x)) for x in re.search(r"ln2 = ([^,]*), ln2_rest = ([^;]*);", SOURCE).groups())
+    assert (whole * 2 ** 40).denominator == 1 and 800 / 0.693 < 2 ** 11
+    assert abs(whole + rest - Fraction(Decimal(2).ln())) < Fraction(1, 2 ** 93)
