@@ -202,8 +202,10 @@ __global__ __launch_bounds__(256) void rope_kv4_append_kernel(AppendArgs p) {
     }
     // What is no finite number: a lane that has any, of the whole wavefront.  Rare, so what has to be done about it stands apart.
     const v2h nothing = {(_Float16)0.0f, (_Float16)0.0f};
-    const v2h odd = v2h{h[0], h[1]} * nothing + v2h{h[2], h[3]} * nothing + (v2h{h[4], h[5]} * nothing + v2h{h[6], h[7]} * nothing);
-    const uint64_t odd_lanes = __builtin_amdgcn_ballot_w64(!((float)odd.x + (float)odd.y == 0.0f));
+    float odd = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 8; e += 2) odd = __builtin_amdgcn_fdot2(v2h{h[e], h[e + 1]}, nothing, odd, false);
+    const uint64_t odd_lanes = __builtin_amdgcn_ballot_w64(!(odd == 0.0f));
     if (odd_lanes != 0 && in_rot && now < p.Hq + p.kv.Hkv) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) {                         // (rounding has made infinities of the NaN among them)
