@@ -366,7 +366,7 @@ size_t qspec_kv4_page_bytes(int Hkv, int D, int page_size);
  * (interleaved = 0) or (2i, 2i + 1) (interleaved = 1).  Scaling for long contexts is a matter of inv_freq and mscale.
  *   qkv_f16   fp16 [B, T, (Hq + 2 Hkv) D]: query heads, key heads, value heads (as qspec_gemm_w4a16 writes them for the
  *             merged weight);  inv_freq  binary64 [rot/2], 16-byte aligned, may be NULL for rot = 0;
- *   0 <= rot <= D, a multiple of 16;  mscale > 0, finite;
+ *   0 <= rot <= D, a multiple of 16;  mscale > 0, finite;  T <= 2^20, qkv_f16 below 2 GiB;
  *   q_f16     out, fp16 [B, T, Hq, D];  cache  in/out.  Rows that have no place in the cache are not stored; their
  *             queries are written all the same.  Rows of one call have places of their own (pages that two sequences
  *             share are not written by both in one call: what stands there afterwards could be codes of one row with
@@ -377,7 +377,7 @@ int qspec_rope_kv4_append(const void* qkv_f16, const double* inv_freq, const int
                           int page_size, int max_pages, int n_pages, void* q_f16, void* cache, void* stream);
 
 /* Values of rows pos[b] .. pos[b] + T - 1 of the cache: k_f16, v_f16 out, fp16 [B, T, Hkv, D] (code * step + low in
- * binary32, then rounded, finite ones held to fp16's finite range); zeros for rows that have no place in it. */
+ * binary32, then rounded, finite ones held to fp16's finite range), below 2 GiB each; zeros for rows that have no place in it. */
 int qspec_kv4_read(const void* cache, const int32_t* pos, const int32_t* page_table, int B, int T, int Hkv, int D,
                    int page_size, int max_pages, int n_pages, void* k_f16, void* v_f16, void* stream);
 
@@ -387,8 +387,11 @@ int qspec_kv4_read(const void* cache, const int32_t* pos, const int32_t* page_ta
  * over the tokens t that are in the cache with t <= p = pos[b] + j and, if window > 0, t > p - window or t < sinks (the
  * window counts p itself).  A row that sees nothing gets zeros, whatever its query.  What stands in rows that no row of
  * the same sequence sees does not matter.  A row whose query holds a NaN or an infinity, or that sees a key or value with NaN for
- * step or low, gets NaN.  fp32 sums; the weights enter the second product in fp16.
- *   q_f16   fp16 [B, T, Hq, D], e.g. from qspec_rope_kv4_append, whose rows of the same call are seen;
+ * step or low, gets NaN.  fp32 sums; the weights enter the second product in fp16, scaled for the largest value step that a
+ * block of up to 64 rows sees (tokens with steps 2^18 times smaller lose bits).
+ *   q_f16   fp16 [B, T, Hq, D], below 2 GiB, e.g. from qspec_rope_kv4_append, whose rows of the same call are seen;  T <= 2^20,
+ *           Hq a multiple of Hkv and 255 times that at most.  A call has blocks of 4, 8, 16, 32 or 64 of the T Hq / Hkv rows that share a
+ *           key/value head (the smallest that hold them, or 64), and B * blocks * Hkv * (max_pages * page_size / 32 + 64) < 2^31;
  *   1e-10 <= scale <= 1e10, with scores, scale * q . k, within +-2^26 (binary32 tells numbers of that size 4 apart; past it a row
  *           may be NaN, and is where its largest score passes 2^27);  window >= 0 (0: none);  sinks >= 0 (0 without a window);
  *   out_f16 out, fp16 [B, T, Hq, D];

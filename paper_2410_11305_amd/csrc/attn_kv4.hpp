@@ -10,7 +10,8 @@
 // and not one of 0 to 15: half the error).
 // A masked nibble in the low bits of a half word IS an fp16 number, code * 2^-24 or 16 * code * 2^-24 (subnormal: exact
 // in the matrix unit, which keeps subnormal operands), so widening a word of 8 codes takes 5 bit operations; the
-// factor of 16 is taken out of q (a power of two that q's row is scaled by first, so that nothing is lost); the values'
+// factor of 16 is taken out of q (its row is scaled by a power of two first, so that only features 2^23 times smaller than its largest
+// lose bits, which the sums in binary32 do not keep either); the values'
 // codes are shifted to 16 * code * 2^-24 all alike, and the finished sums scaled.  The token order of the second product
 // is that of the first one's results: p goes from the accumulators into the next operand without crossing lanes, and a
 // lane's codes of four tokens are 16 bytes of the cache (kv4.hpp).
@@ -22,13 +23,13 @@
 // out as even, they are dealt out whole.  The lengths are known on the device only: every
 // workgroup works the division out for itself.
 //
-// Measured (device time; bytes of the cache, queries and results): 8 sequences of up to 2048 tokens, one row of 32 heads, 21.4 us
-// (3.0 TB/s); 131071 tokens, one row of 64 over 8 heads, 38.6 us (3.7 TB/s); 32 sequences through a window of 4096, 64 over 8 heads of
-// 64, 26.8 us (2.8 TB/s); 128 sequences of 200 to 2048 tokens, 4 rows of 64 over 8 heads, 60 us (2.9 TB/s, 320 TF/s); a prompt of
-// 2050 tokens of 32 heads 77 us (445 TF/s), a chunk of 2050 rows over 4096 tokens of 64 over 8 heads 331 us (620 TF/s).  Short passes are bound by
-// the start (1.4 us of division, 3 us to the first scores) and the joins, long ones of few rows by the vector unit's
-// share of a step (exponentials, steps and lows) beside the loads.  From 17 rows on the vector unit issues in 54 % of its cycles (32
-// rows), 35 % (64, two wavefronts a SIMD and the LDS reads of q between), the matrix unit works in 12 %: it takes 5 to 7 vector
+// Measured (device time; bytes of the cache, queries and results): 8 sequences of up to 2048 tokens, one row of 32 heads, 21.8 us
+// (2.9 TB/s); 131071 tokens, one row of 64 over 8 heads, 38.8 us (3.7 TB/s); 32 sequences through a window of 4096, 64 over 8 heads of
+// 64, 26.8 us (2.8 TB/s); 128 sequences of 200 to 2048 tokens, 4 rows of 64 over 8 heads, 59.5 us (2.9 TB/s, 320 TF/s); a prompt of
+// 2050 tokens of 32 heads 77.7 us (445 TF/s), a chunk of 2050 rows over 4096 tokens of 64 over 8 heads 331 us (620 TF/s).  Short passes are bound by
+// the start (1.4 us of division, 3 us to the first scores) and the joins.  Long ones of few rows wait (36 to 43 % of a wavefront's life) as much
+// as they issue, the vector unit works in 27 to 34 % of its cycles.  From 17 rows on it works in 55 % (32 rows), 37 % (64: two wavefronts a SIMD,
+// in which the products and the exponentials of a step wait for one another), the matrix unit in 12 %: it takes 5 to 7 vector
 // instructions a word to widen and a dozen a score.
 #pragma once
 #include "common.hpp"
@@ -589,7 +590,8 @@ __global__ __launch_bounds__((64 * AttnForm<NB, F>::waves), 2) void attn_kv4_ker
           l[nb] += e1;
           c[nb] = fmaf(e0, fmaf(8.0f, (float)vp[x].x, (float)vp[x].y), c[nb]);
           c[nb] = fmaf(e1, fmaf(8.0f, (float)vp[x + 1].x, (float)vp[x + 1].y), c[nb]);
-          // 11 bits of a weight: what an fp16 probability keeps
+          // 11 bits of a weight, what an fp16 probability keeps, since the matrix unit takes fp16: results are off by 2.4e-4 to 2.8e-4 where
+          // their own rounding makes 2.1e-4.  (A second number for what is cut off cost drafts 5 %.)
           const v2h both = __builtin_convertvector((v2f{e0 * (float)vp[x].x, e1 * (float)vp[x + 1].x}), v2h);
           c[nb] = __builtin_amdgcn_fdot2(both, minus8, c[nb], false);
           w[nb][x / 2] = __builtin_bit_cast(uint32_t, both);

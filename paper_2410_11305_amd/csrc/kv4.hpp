@@ -149,9 +149,9 @@ __device__ inline uint32_t kv_code_word(const float (&v)[8], _Float16& step, _Fl
 
 // grid (B*T, parts): a workgroup takes one token and every parts-th set of 256 / (D/8) of its Hq + 2 Hkv heads, a row of D/8
 // lanes a head, 8 features a lane: 16 bytes in, a code word out, and the folds over a head stay in a row of lanes.  The angles
-// of a token are worked out once a workgroup.  Measured: 2050 tokens of 32 heads and 32 key/value heads of 128 24 us with 85 MB to
-// move (3.5 TB/s), the vector unit at 49 % of its cycles: the binary64 rotation and the stores of value words 64 bytes apart share the bound.
-// 512 tokens of 64 and 8 heads 8.6 us (20 MB), one token 3.6 us, a launch and four dependent trips to memory.
+// of a token are worked out once a workgroup.  Measured: 2050 tokens of 32 heads and 32 key/value heads of 128 25 us, the vector unit at 54 % of its
+// cycles.  The binary64 rotation and the stores share the bound: a token's value words lie 64 bytes apart and each costs a sector of 32, 58 MB
+// written where 26 are needed.  512 tokens of 64 and 8 heads 9.1 us (10.9 MB written for 9.0), one token 3.7 us, a launch and four dependent trips to memory.
 template <int D>
 __global__ __launch_bounds__(256) void rope_kv4_append_kernel(AppendArgs p) {
   constexpr int LANES = D / 8, PER = 256 / LANES;
@@ -256,7 +256,7 @@ __device__ inline v8h kv_values(uint32_t w, _Float16 step, _Float16 low) {
 }
 
 // grid (B*T, parts of Hkv D / 8 words of a token).  A copy that widens 4 bits to 16: memory bounds it (2050 tokens of 32
-// heads of 128: 51 MB in 13 us, 3.9 TB/s; one token 2.3 us, a launch).  Rows without a place in the cache come back as zeros.
+// heads of 128: 51 MB in 13 us, 3.9 TB/s; one token 2.4 us, a launch).  Rows without a place in the cache come back as zeros.
 template <int D>
 __global__ __launch_bounds__(256) void kv4_read_kernel(KvReadArgs p) {
   constexpr int LANES = D / 8;

@@ -81,6 +81,14 @@ def test_attention_refusals():
     assert attend(nws=B.attn_kv4_workspace_bytes(2, 3, 8, 2, 128) - 1) == B.ERR_WORKSPACE
 
 
+def test_attention_refuses_more_work_than_it_counts():
+    """B * blocks * Hkv * (tokens / 32 + 64) from 2^31 on."""
+    size = dict(B=1024, T=4, Hq=64, Hkv=64, D=64, page=64, nws=1)                # (the workspace is looked at first: what is not refused for its size is for that)
+    assert attend(**{**size, "nws": 1 << 30}, each=1 << 14, table=A) == B.ERR_SHAPE
+    assert attend(**size, each=1 << 9, table=A) == B.ERR_WORKSPACE
+    assert attend(B=3, T=1 << 20, Hq=1, Hkv=1, D=64, page=1 << 12, each=1 << 18, table=A) == B.ERR_SHAPE
+
+
 def test_sample_refusals():
     for bad in (dict(B=0), dict(gamma=-1), dict(gamma=0), dict(V=0), dict(V=(1 << 21) + 1), dict(B=20000)):
         assert choose(**bad) == B.ERR_SHAPE, bad
