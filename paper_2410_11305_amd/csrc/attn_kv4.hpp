@@ -644,7 +644,7 @@ __global__ __launch_bounds__((64 * AttnForm<NB, F>::waves), 2) void attn_kv4_ker
     const uint32_t w0 = shared ? group_of(item + OVER + WAVES - 1) : me, w1 = shared ? group_of(item + OVER + span.steps - 1) : me;   // the workgroups that hold a part of it
     const auto write_row = [&](int r, const float (&v)[4], float sum, float ref) {
       const int j = over_group(p, r), g = r - j * p.G;
-      // From 2^28 on a reference can be too far off to keep the weights inside fp16's range, down to all of them zero or infinite.
+      // From 2^27 on, where binary32 goes by 16, a reference can be 8 off and the largest weight past fp16's range; further on all weights zero or infinite.
       const bool none = sum == 0.0f && ref == kNone;
       const float by = fabsf(ref) < 134217728.0f ? 1.0f / sum : __builtin_nanf("");
       typedef _Float16 v4h __attribute__((ext_vector_type(4)));
