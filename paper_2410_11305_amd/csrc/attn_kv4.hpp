@@ -336,7 +336,12 @@ __global__ __launch_bounds__((64 * AttnForm<NB, F>::waves), 2) void attn_kv4_ker
       g.there = 0;
 #pragma unroll
       for (int i = 0; i < TILES; ++i) {
-        const int page = i > 0 && P >= STEP ? g.page[0] : __builtin_amdgcn_readlane(known, k * TILES + i);
+        if (i > 0 && P >= STEP) {             // the same page, there or not
+          g.page[i] = g.page[0];
+          g.there |= (g.there & 1u) << i;
+          continue;
+        }
+        const int page = __builtin_amdgcn_readlane(known, k * TILES + i);
         const bool there = page >= 0 && page < p.kv.n_pages;
         g.page[i] = there ? page : 0;
         g.there |= there ? 1u << i : 0u;
