@@ -405,6 +405,78 @@ int qspec_attn_kv4(const void* q_f16, const void* cache, const int32_t* pos, con
                    void* workspace, size_t workspace_bytes, void* stream);
 
 /*
+ * Attention for sequences that share the beginnings of their contexts (a system prompt, several samples of one prompt): what
+ * qspec_attn_kv4 gives without a window, with the shared tokens read and multiplied once for all of a group.
+ * The B sequences are `groups` sets of B / groups neighbours.  Token t < shared[g] of every sequence of group g is read through the
+ * page table's row of the group's first sequence, the others through the sequence's own row: the rows
+ * may name the same pages (a sequence's own page in which the shared tokens end may hold anything in their places), or only the first
+ * may have them.  Rows at positions before shared[g] see the shared tokens up to their own.
+ *   shared  int32 [groups], device memory; 0 or less: none.  Held to max_pages * page_size.
+ *   (B / groups) * T <= 2^20, and the count of work at qspec_attn_kv4 holds for the groups as sequences of (B / groups) * T rows too.
+ *   A row in front of its sequence gets zeros.  Everything else, NaN and limits of scale and scores included, as in qspec_attn_kv4;
+ *   two launches, partial sums of the shared tokens in binary32.
+ *   workspace  qspec_attn_kv4_shared_workspace_bytes(...) bytes; the workspace rule at qspec_workspace_bytes holds.
+ */
+size_t qspec_attn_kv4_shared_workspace_bytes(int B, int T, int Hq, int Hkv, int D, int groups);
+int qspec_attn_kv4_shared(const void* q_f16, const void* cache, const int32_t* pos, const int32_t* page_table, const int32_t* shared,
+                          int B, int T, int Hq, int Hkv, int D, int groups, int page_size, int max_pages, int n_pages,
+                          float scale, void* out_f16, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Sparse attention over a long context: each row reads some pages of the cache only, chosen by bounds of what their keys can
+ * score.  page_size >= 64 in these calls.
+ *
+ * Bounds.  For the keys of a page's tokens and one key/value head, the largest and smallest value of each feature (code * step + low in
+ * binary32), rounded outward to whole numbers of a grid, the smallest power of two with all of them within +-127 (1 where all are zero).
+ *   bounds  n_pages pages of qspec_kv4_bounds_bytes(Hkv, D) bytes, one for each page of the cache.  A page holds, per head, D upper and
+ *           D lower codes (int8), then the heads' grids (binary32), and is filled up to a multiple of 16 bytes.  A page with a key that
+ *           is stored as NaN has codes 0 and NaN for its grid.
+ * qspec_kv4_bounds writes them for the pages that rows pos[b] .. pos[b] + T - 1 lie in, from the tokens of these pages up to the
+ * last of the rows: call it behind each append, with the same arguments.  (Rows rejected after a verify pass leave their page's bounds when the next
+ * call writes it.)  Pages that two sequences share are not written by both in one call.
+ * B * ((T - 1) / page_size + 2) <= 2^23, Hkv <= 65535.
+ */
+size_t qspec_kv4_bounds_bytes(int Hkv, int D);
+int qspec_kv4_bounds(const void* cache, const int32_t* pos, const int32_t* page_table, int B, int T, int Hkv, int D,
+                     int page_size, int max_pages, int n_pages, void* bounds, void* stream);
+
+/* Bounds of the pages that rows pos[b] .. pos[b] + T - 1 lie in, as numbers: upper, lower out, fp32 [B, (T - 1) / page_size + 2, Hkv, D],
+ * 16-byte aligned, below 2 GiB each; zeros behind the last of these pages and for pages that are not there. */
+int qspec_kv4_bounds_read(const void* bounds, const int32_t* pos, const int32_t* page_table, int B, int T, int Hkv, int D,
+                          int page_size, int max_pages, int n_pages, float* upper, float* lower, void* stream);
+
+/*
+ * The choice of pages.  The row at position p = pos[b] + j sees pages 0 .. n - 1, n = min(p / page_size + 1, max_pages) (0 for p < 0).  Of these the
+ * first `first` and the last `last` are taken, and of the others the best by
+ *   score[i] = grid[i] max_g sum_d max(c[g][d] upper[i][d], c[g][d] lower[i][d])          over the row's heads g of the key/value head,
+ * c the queries rounded to nearest even whole numbers of their own grid, the smallest power of two with all features of these heads within
+ * +-127: whole numbers but for powers of two, so the choice is exact.  The lower page among equals.  A page whose grid is NaN comes
+ * before all others, a page that is not there after them; a row with a NaN or an infinity has zeros for c.
+ *   pages  out, int32 [B, T, Hkv, count], below 2 GiB: `count` of them in ascending order, -1 behind the last where n < count.
+ *   first, last >= 0, first + last <= count;  max_pages <= 2^24;
+ *   workspace  qspec_kv4_select_workspace_bytes(...) bytes of scratch, 16-byte aligned, nothing to clear.
+ */
+size_t qspec_kv4_select_workspace_bytes(int B, int T, int Hq, int Hkv, int max_pages);
+int qspec_kv4_select(const void* q_f16, const void* bounds, const int32_t* pos, const int32_t* page_table, int B, int T, int Hq, int Hkv, int D,
+                     int page_size, int max_pages, int n_pages, int first, int last, int count, int32_t* pages,
+                     void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Attention over chosen pages: row j of sequence b and its heads of key/value head h see the tokens t <= pos[b] + j of the pages that
+ * pages[b][j][h] names, and no others.  A list is read from its start, min(count, n) entries of it (n as above); an entry that
+ * is negative, not larger than the one before it, or at or past max_pages is left out, so ascending lists with -1 at their end, as qspec_kv4_select
+ * writes them, are taken whole.  A row that sees nothing gets zeros.
+ *   pages  int32 [B, T, Hkv, count], count >= 1, below 2 GiB;
+ *   B * T * Hkv * blocks * (min(count, max_pages) * page_size / 32 + 64) < 2^31, blocks of 4, 8, 16, 32 or 64 of the Hq / Hkv heads as in qspec_attn_kv4,
+ *   with which everything else, the values of NaN and the limits of scale and scores, agrees;
+ *   workspace  qspec_attn_kv4_blocks_workspace_bytes(...) bytes; the workspace rule at qspec_workspace_bytes holds.
+ */
+size_t qspec_attn_kv4_blocks_workspace_bytes(int B, int T, int Hq, int Hkv, int D);
+int qspec_attn_kv4_blocks(const void* q_f16, const void* cache, const int32_t* pos, const int32_t* page_table, const int32_t* pages,
+                          int B, int T, int Hq, int Hkv, int D, int count, int page_size, int max_pages, int n_pages,
+                          float scale, void* out_f16, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
  * Sampling from given random numbers, for decoding that is not greedy (paper Sec. 3.1 decodes greedily; the walk over
  * the drafts is the same).  The tokens of a row are ordered by falling logit, the lowest id first among equals, and
  * weigh w = exp((logit - max) / temperature), in binary64.  top_k keeps the first top_k of them, min_p those with w >=

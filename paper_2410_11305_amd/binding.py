@@ -26,6 +26,8 @@ EXPORTS = (
     "qspec_w4a4_takes_wide", "qspec_quant_act_wide", "qspec_gemm_w4a4_wide",
     "qspec_kv4_page_bytes", "qspec_rope_kv4_append", "qspec_kv4_read", "qspec_attn_kv4_workspace_bytes", "qspec_attn_kv4",
     "qspec_sample_workspace_bytes", "qspec_sample",
+    "qspec_attn_kv4_shared_workspace_bytes", "qspec_attn_kv4_shared", "qspec_kv4_bounds_bytes", "qspec_kv4_bounds", "qspec_kv4_bounds_read",
+    "qspec_kv4_select_workspace_bytes", "qspec_kv4_select", "qspec_attn_kv4_blocks_workspace_bytes", "qspec_attn_kv4_blocks",
 )
 
 
@@ -107,6 +109,24 @@ def lib() -> ctypes.CDLL:
     L.qspec_attn_kv4_workspace_bytes.argtypes = [ci, ci, ci, ci, ci]
     L.qspec_attn_kv4.restype = ci
     L.qspec_attn_kv4.argtypes = [vp, vp, vp, vp, ci, ci, ci, ci, ci, ci, ci, ci, ctypes.c_float, ci, ci, vp, vp, sz, vp]
+    L.qspec_attn_kv4_shared_workspace_bytes.restype = sz
+    L.qspec_attn_kv4_shared_workspace_bytes.argtypes = [ci, ci, ci, ci, ci, ci]
+    L.qspec_attn_kv4_shared.restype = ci
+    L.qspec_attn_kv4_shared.argtypes = [vp, vp, vp, vp, vp, ci, ci, ci, ci, ci, ci, ci, ci, ci, ctypes.c_float, vp, vp, sz, vp]
+    L.qspec_kv4_bounds_bytes.restype = sz
+    L.qspec_kv4_bounds_bytes.argtypes = [ci, ci]
+    L.qspec_kv4_bounds.restype = ci
+    L.qspec_kv4_bounds.argtypes = [vp, vp, vp, ci, ci, ci, ci, ci, ci, ci, vp, vp]
+    L.qspec_kv4_bounds_read.restype = ci
+    L.qspec_kv4_bounds_read.argtypes = [vp, vp, vp, ci, ci, ci, ci, ci, ci, ci, vp, vp, vp]
+    L.qspec_kv4_select_workspace_bytes.restype = sz
+    L.qspec_kv4_select_workspace_bytes.argtypes = [ci, ci, ci, ci, ci]
+    L.qspec_kv4_select.restype = ci
+    L.qspec_kv4_select.argtypes = [vp, vp, vp, vp, ci, ci, ci, ci, ci, ci, ci, ci, ci, ci, ci, vp, vp, sz, vp]
+    L.qspec_attn_kv4_blocks_workspace_bytes.restype = sz
+    L.qspec_attn_kv4_blocks_workspace_bytes.argtypes = [ci, ci, ci, ci, ci]
+    L.qspec_attn_kv4_blocks.restype = ci
+    L.qspec_attn_kv4_blocks.argtypes = [vp, vp, vp, vp, vp, ci, ci, ci, ci, ci, ci, ci, ci, ci, ctypes.c_float, vp, vp, sz, vp]
     L.qspec_sample_workspace_bytes.restype = sz
     L.qspec_sample_workspace_bytes.argtypes = [ci, ci, ci]
     L.qspec_sample.restype = ci
@@ -569,6 +589,131 @@ def attn_kv4(q: torch.Tensor, cache: torch.Tensor, pos: torch.Tensor, Hkv: int, 
                                 window, sinks, _shaped(out, torch.float16, q.shape, device, "out"),
                                 _shaped(workspace, torch.uint8, (workspace.numel(),), device, "workspace"), workspace.numel(), _stream()),
            "qspec_attn_kv4")
+    return out
+
+
+def attn_kv4_shared_workspace_bytes(B: int, T: int, Hq: int, Hkv: int, D: int, groups: int) -> int:
+    return lib().qspec_attn_kv4_shared_workspace_bytes(B, T, Hq, Hkv, D, groups)
+
+
+def attn_kv4_shared(q: torch.Tensor, cache: torch.Tensor, pos: torch.Tensor, shared: torch.Tensor, Hkv: int, page_size: int,
+                    page_table: torch.Tensor = None, scale: float = None, out: torch.Tensor = None,
+                    workspace: torch.Tensor = None) -> torch.Tensor:
+    """attn_kv4 for sequences that share beginnings: shared int32 [groups], the B sequences being that many sets of neighbours; the
+    first shared[g] tokens of a set are read once, through the page table's row of its first sequence.  Hot loops pass out and a workspace."""
+    B, T, Hq, D = q.shape
+    groups = shared.shape[0]
+    device, c, at, table, Bp, max_pages, n_pages = _kv4(cache, pos, page_table, Hkv, D, page_size, "qspec_attn_kv4_shared")
+    x = _shaped(q, torch.float16, (Bp, T, Hq, D), device, "q")
+    if out is None:
+        out = torch.empty_like(q)
+    if workspace is None:
+        workspace = alloc_workspace(attn_kv4_shared_workspace_bytes(B, T, Hq, Hkv, D, groups))
+    _check(lib().qspec_attn_kv4_shared(x, c, at, table, _shaped(shared, torch.int32, (groups,), device, "shared"), B, T, Hq, Hkv, D, groups, page_size,
+                                       max_pages, n_pages, D ** -0.5 if scale is None else scale, _shaped(out, torch.float16, q.shape, device, "out"),
+                                       _shaped(workspace, torch.uint8, (workspace.numel(),), device, "workspace"), workspace.numel(), _stream()),
+           "qspec_attn_kv4_shared")
+    return out
+
+
+def kv4_bounds_bytes(Hkv: int, D: int) -> int:
+    return lib().qspec_kv4_bounds_bytes(Hkv, D)
+
+
+def alloc_kv4_bounds(n_pages: int, Hkv: int, D: int) -> torch.Tensor:
+    """Bounds for a cache of n_pages pages: uint8 [n_pages, kv4_bounds_bytes], zeroed."""
+    nbytes = kv4_bounds_bytes(Hkv, D)
+    if nbytes == 0:
+        raise QSpecError(ERR_SHAPE, "qspec_kv4_bounds_bytes")
+    return torch.zeros((n_pages, nbytes), dtype=torch.uint8, device="cuda")
+
+
+def kv4_bounds(cache: torch.Tensor, pos: torch.Tensor, T: int, bounds: torch.Tensor, Hkv: int, D: int, page_size: int,
+               page_table: torch.Tensor = None) -> torch.Tensor:
+    """Bounds of the keys in the pages that rows pos[b] .. pos[b] + T - 1 lie in, from the tokens up to the last of them: bounds uint8 [pages,
+    kv4_bounds_bytes], updated in place.  To be called behind each rope_kv4_append."""
+    device, c, at, table, B, max_pages, n_pages = _kv4(cache, pos, page_table, Hkv, D, page_size, "qspec_kv4_bounds")
+    _check(lib().qspec_kv4_bounds(c, at, table, B, T, Hkv, D, page_size, max_pages, n_pages,
+                                  _shaped(bounds, torch.uint8, (n_pages, kv4_bounds_bytes(Hkv, D)), device, "bounds"), _stream()), "qspec_kv4_bounds")
+    return bounds
+
+
+def _kv4_bounds(bounds, pos, page_table, Hkv, D, where):
+    """(device number, bounds, pos, table pointers, B, max_pages, n_pages) of a call that reads bounds."""
+    n_pages, B = bounds.shape[0], pos.shape[0]
+    nbytes = kv4_bounds_bytes(Hkv, D)
+    if B == 0 or n_pages == 0 or nbytes == 0:
+        raise QSpecError(ERR_SHAPE, where)
+    device = _here(bounds, "bounds")
+    table, max_pages = None, n_pages // B
+    if page_table is not None:
+        max_pages = page_table.shape[-1]
+        table = _shaped(page_table, torch.int32, (B, max_pages), device, "page_table")
+    return (device, _shaped(bounds, torch.uint8, (n_pages, nbytes), device, "bounds"), _shaped(pos, torch.int32, (B,), device, "pos"),
+            table, B, max_pages, n_pages)
+
+
+def kv4_bounds_read(bounds: torch.Tensor, pos: torch.Tensor, T: int, Hkv: int, D: int, page_size: int, page_table: torch.Tensor = None,
+                    upper: torch.Tensor = None, lower: torch.Tensor = None):
+    """Bounds of the pages that rows pos[b] .. pos[b] + T - 1 lie in, as numbers: (upper, lower), fp32 [B, (T - 1) // page_size + 2, Hkv, D];
+    zeros behind the last of them."""
+    device, c, at, table, B, max_pages, n_pages = _kv4_bounds(bounds, pos, page_table, Hkv, D, "qspec_kv4_bounds_read")
+    if T < 1 or page_size < 1:
+        raise QSpecError(ERR_SHAPE, "qspec_kv4_bounds_read")
+    shape = (B, (T - 1) // page_size + 2, Hkv, D)
+    upper = torch.empty(shape, dtype=torch.float32, device=bounds.device) if upper is None else upper
+    lower = torch.empty(shape, dtype=torch.float32, device=bounds.device) if lower is None else lower
+    _check(lib().qspec_kv4_bounds_read(c, at, table, B, T, Hkv, D, page_size, max_pages, n_pages, _shaped(upper, torch.float32, shape, device, "upper"),
+                                       _shaped(lower, torch.float32, shape, device, "lower"), _stream()), "qspec_kv4_bounds_read")
+    return upper, lower
+
+
+def kv4_select_workspace_bytes(B: int, T: int, Hq: int, Hkv: int, max_pages: int) -> int:
+    return lib().qspec_kv4_select_workspace_bytes(B, T, Hq, Hkv, max_pages)
+
+
+def kv4_select(q: torch.Tensor, bounds: torch.Tensor, pos: torch.Tensor, Hkv: int, page_size: int, count: int, page_table: torch.Tensor = None,
+               first: int = 1, last: int = 1, blocks: torch.Tensor = None, workspace: torch.Tensor = None) -> torch.Tensor:
+    """For every row of q fp16 [B, T, Hq, D] and key/value head the `count` pages that its attention is to read, int32 [B, T, Hkv, count] in
+    ascending order (-1 behind the last): the first `first`, the last `last`, and the best of the others by their bounds."""
+    B, T, Hq, D = q.shape
+    device, c, at, table, Bp, max_pages, n_pages = _kv4_bounds(bounds, pos, page_table, Hkv, D, "qspec_kv4_select")
+    x = _shaped(q, torch.float16, (Bp, T, Hq, D), device, "q")
+    if count < 1:
+        raise QSpecError(ERR_SHAPE, "qspec_kv4_select")
+    if blocks is None:
+        blocks = torch.empty((B, T, Hkv, count), dtype=torch.int32, device=q.device)
+    if workspace is None:
+        workspace = torch.empty(max(kv4_select_workspace_bytes(B, T, Hq, Hkv, max_pages), 16), dtype=torch.uint8, device=q.device)
+    _check(lib().qspec_kv4_select(x, c, at, table, B, T, Hq, Hkv, D, page_size, max_pages, n_pages, first, last, count,
+                                  _shaped(blocks, torch.int32, (B, T, Hkv, count), device, "blocks"),
+                                  _shaped(workspace, torch.uint8, (workspace.numel(),), device, "workspace"), workspace.numel(), _stream()),
+           "qspec_kv4_select")
+    return blocks
+
+
+def attn_kv4_blocks_workspace_bytes(B: int, T: int, Hq: int, Hkv: int, D: int) -> int:
+    return lib().qspec_attn_kv4_blocks_workspace_bytes(B, T, Hq, Hkv, D)
+
+
+def attn_kv4_blocks(q: torch.Tensor, cache: torch.Tensor, pos: torch.Tensor, blocks: torch.Tensor, Hkv: int, page_size: int,
+                    page_table: torch.Tensor = None, scale: float = None, out: torch.Tensor = None,
+                    workspace: torch.Tensor = None) -> torch.Tensor:
+    """attn_kv4 over the pages that blocks int32 [B, T, Hkv, count] names for every row and key/value head (kv4_select writes
+    such lists).  Hot loops pass out and a workspace."""
+    B, T, Hq, D = q.shape
+    device, c, at, table, Bp, max_pages, n_pages = _kv4(cache, pos, page_table, Hkv, D, page_size, "qspec_attn_kv4_blocks")
+    x = _shaped(q, torch.float16, (Bp, T, Hq, D), device, "q")
+    count = blocks.shape[-1]
+    if out is None:
+        out = torch.empty_like(q)
+    if workspace is None:
+        workspace = alloc_workspace(attn_kv4_blocks_workspace_bytes(B, T, Hq, Hkv, D))
+    _check(lib().qspec_attn_kv4_blocks(x, c, at, table, _shaped(blocks, torch.int32, (B, T, Hkv, count), device, "blocks"), B, T, Hq, Hkv, D, count,
+                                       page_size, max_pages, n_pages, D ** -0.5 if scale is None else scale,
+                                       _shaped(out, torch.float16, q.shape, device, "out"),
+                                       _shaped(workspace, torch.uint8, (workspace.numel(),), device, "workspace"), workspace.numel(), _stream()),
+           "qspec_attn_kv4_blocks")
     return out
 
 

@@ -74,6 +74,21 @@ struct AttnArgs {
   float scale_log2;          // scale * log2(e)
 };
 
+// What a launch reads and what becomes of its sums.  kAttnWhole: every token in sight, results.  kAttnPrefix: the tokens that the sequences of a
+// group share, as partial sums of every row; kAttnRest: those behind them, joined with these sums, results.  kAttnPages: the pages
+// that a list names for each row, results.
+enum { kAttnWhole, kAttnPrefix, kAttnRest, kAttnPages };
+
+struct AttnPartArgs : AttnArgs {
+  // kAttnPrefix: kv.T and B are the rows of a group and the groups;  kAttnPages: one row each and all rows
+  int rows;                  // rows of a sequence (T of the call)
+  int group;                 // sequences of a group
+  const int32_t* shared;     // [groups]: tokens that they share
+  float* joint;              // [B * rows * Hq]: partial sums of the shared tokens, attn_part_floats each
+  const int32_t* list;       // [B * rows][Hkv][count]
+  int count;
+};
+
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 __device__ __forceinline__ uint32_t uniform(uint32_t v) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)v); }
 
@@ -85,21 +100,49 @@ struct AttnSpan {
   int lo, hi;                // positions of its first and its last row
 };
 
+__device__ __forceinline__ int row_group(const AttnArgs&) { return 1; }
+__device__ __forceinline__ int row_group(const AttnPartArgs& p) { return p.group; }
+__device__ __forceinline__ int row_count(const AttnArgs&) { return 1; }
+__device__ __forceinline__ int row_count(const AttnPartArgs& p) { return p.rows; }
+
+// Where a sequence stands.  at: position of its first row (kAttnPrefix: how many tokens the group shares);  from: its first token (kAttnRest).
+struct AttnWhere {
+  int at, from;
+};
+
 // The position that a row of a block's window begins behind.  (A row in front of the sequence sees nothing, whatever its window.)
 __device__ __forceinline__ int behind_window(const AttnArgs& p, int at) { return max(at, 0) - p.window; }
 
-// pos: position of the sequence's first row.  (Held, so that sums stay in 32 bits: from below far in front of the sequence, where rows see nothing,
-// from above to the last positions that there are.)
-template <int STEP>
-__device__ __forceinline__ AttnSpan attn_span(const AttnArgs& p, int pos, int block, int rows_per_block) {
+// Position of the first of T rows, held so that sums stay in 32 bits: from below far in front of the sequence, where rows see nothing,
+// from above to the last positions that there are.
+__device__ __forceinline__ int held_position(int pos, int T) { return min(max(pos, -(1 << 30)), 0x7fffffff - T); }
+
+template <int STEP, int MODE = kAttnWhole, class Args = AttnArgs>
+__device__ __forceinline__ AttnSpan attn_span(const Args& p, AttnWhere w, int block, int rows_per_block) {
   const int r0 = block * rows_per_block, r1 = min(p.kv.T * p.G, r0 + rows_per_block) - 1;
-  pos = min(max(pos, -(1 << 30)), 0x7fffffff - p.kv.T);
+  const int last = p.kv.max_pages << p.kv.page_shift;
   AttnSpan s;
+  s.first = s.sink_steps = 0;
+  if constexpr (MODE == kAttnPrefix) {
+    s.lo = s.hi = min(w.at, last) - 1;        // (of the rows that see them all)
+    s.steps = max((s.hi + STEP) / STEP, 1);
+    return s;
+  }
+  const int pos = held_position(w.at, p.kv.T);
   s.lo = pos + over_group(p, r0);
   s.hi = pos + over_group(p, r1);
-  const int end = min(s.hi + 1, p.kv.max_pages << p.kv.page_shift);      // tokens 0 .. end - 1
-  s.first = p.window > 0 ? max(behind_window(p, s.lo) + 1, 0) / STEP : 0;
-  s.sink_steps = p.window > 0 ? max(min((min(p.sinks, end) + STEP - 1) / STEP, s.first), 0) : 0;
+  const int end = min(s.hi + 1, last);        // tokens 0 .. end - 1
+  if constexpr (MODE == kAttnPages) {
+    const int pages = end > 0 ? ((end - 1) >> p.kv.page_shift) + 1 : 0;
+    s.steps = max(min(p.count, pages) * ((1 << p.kv.page_shift) / STEP), 1);
+    return s;
+  }
+  if constexpr (MODE == kAttnRest) {
+    s.first = w.from / STEP;
+  } else {
+    s.first = p.window > 0 ? max(behind_window(p, s.lo) + 1, 0) / STEP : 0;
+    s.sink_steps = p.window > 0 ? max(min((min(p.sinks, end) + STEP - 1) / STEP, s.first), 0) : 0;
+  }
   // at least one: rows that see nothing have their zeros written
   s.steps = max(s.sink_steps + max((end + STEP - 1) / STEP - s.first, 0), 1);
   return s;
@@ -156,8 +199,8 @@ constexpr size_t attn_workspace() {
 // c / (16 / F) of a step only: the scores of the F tiles are computed for all columns and each column keeps its own, which
 // costs a selection and saves (F - 1) / F of the exponentials and all that goes with them; in the second product a
 // column's weights are zero for the tiles of the others.  Each column ends with its own sums, joined like those of the wavefronts.
-template <int D, int NB, int F>
-__global__ __launch_bounds__((64 * AttnForm<NB, F>::waves), 2) void attn_kv4_kernel(AttnArgs p) {
+template <int D, int NB, int F, int MODE, class Args>
+__device__ __forceinline__ void attn_kv4_work(const Args& p) {
   typedef AttnForm<NB, F> Form;
   constexpr int WAVES = Form::waves, THREADS = 64 * WAVES, TILES = Form::tiles, STEP = Form::step, RB = Form::rows, OVER = Form::over;
   constexpr int NK = D / 32;                  // matrix instructions of a tile of q k^T; words of a lane of a key
@@ -185,16 +228,32 @@ __global__ __launch_bounds__((64 * AttnForm<NB, F>::waves), 2) void attn_kv4_ker
   const uint32_t region_bytes = (uint32_t)P * (D + 8);
   const int row_of = tid / LANES, own = (tid & (LANES - 1)) * 4;       // join: row, first feature
   const auto sequence_of = [&](int e) { return p.blocks == 1 ? e : e / p.blocks; };
+  const auto where_is = [&](int seq, auto load) {        // load(array, index)
+    if constexpr (MODE == kAttnPrefix) {
+      return AttnWhere{max(load(p.shared, seq), 0), 0};
+    } else if constexpr (MODE == kAttnRest) {
+      return AttnWhere{load(p.kv.pos, seq), min(max(load(p.shared, seq / p.group), 0), p.kv.max_pages << p.kv.page_shift)};
+    } else if constexpr (MODE == kAttnPages) {
+      const int b = p.rows == 1 ? seq : seq / p.rows;
+      return AttnWhere{held_position(load(p.kv.pos, b), p.rows) + (seq - b * p.rows), 0};
+    } else {
+      return AttnWhere{load(p.kv.pos, seq), 0};
+    }
+  };
+  const auto where = [&](int seq) { return where_is(seq, [](const int32_t* a, int i) { return a[i]; }); };
+  const auto where_scalar = [&](int seq) { return where_is(seq, [](const int32_t* a, int i) { return scalar_load(a, i); }); };
+  // the sequence whose pages are read
+  const auto table_row = [&](int seq) { return MODE == kAttnPrefix ? seq * row_group(p) : MODE == kAttnPages ? seq / row_count(p) : seq; };
 
   // ---- the division of the work: entries are (sequence, block of rows), each of Hkv items of equal size, OVER + steps.
   // Every wavefront works it out by itself, a run of entries to a lane: no barrier stands before the first loads.
   const int entries = p.B * p.blocks;
   const int per = (entries + 63) / 64;
-  const auto size_of = [&](int e, int pos) {
-    return (uint32_t)(OVER + attn_span<STEP>(p, pos, e - sequence_of(e) * p.blocks, RB).steps) * (uint32_t)Hkv;
+  const auto size_of = [&](int e, AttnWhere at) {
+    return (uint32_t)(OVER + attn_span<STEP, MODE>(p, at, e - sequence_of(e) * p.blocks, RB).steps) * (uint32_t)Hkv;
   };
   uint32_t mine = 0;
-  for (int e = lane * per; e < min(entries, (lane + 1) * per); ++e) mine += size_of(e, p.kv.pos[sequence_of(e)]);
+  for (int e = lane * per; e < min(entries, (lane + 1) * per); ++e) mine += size_of(e, where(sequence_of(e)));
   uint32_t upto = mine;                       // of the entries up to this lane's
 #define QSPEC_DPP_ADD(ctrl, rows) upto += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)upto, ctrl, rows, 0xf, false)
   QSPEC_DPP_ADD(0x111, 0xf);                  // row_shr 1, 2, 4, 8: sums inside a row of 16
@@ -224,7 +283,7 @@ __global__ __launch_bounds__((64 * AttnForm<NB, F>::waves), 2) void attn_kv4_ker
     int e = owner * per;
     if (per > 1) {
       for (;; ++e) {
-        n = uniform(size_of(e, uniform(scalar_load(p.kv.pos, sequence_of(e)))));
+        n = uniform(size_of(e, where_scalar(sequence_of(uniform(e)))));
         if (x - at < n) break;
         at += n;
       }
@@ -255,17 +314,20 @@ __global__ __launch_bounds__((64 * AttnForm<NB, F>::waves), 2) void attn_kv4_ker
     };
     bool even = true;
     if (NB == 4) {
-      const int pos = uniform(scalar_load(p.kv.pos, 0));
-      for (int e = lane; e < p.B; e += 64) even &= p.kv.pos[e] == pos;
+      const AttnWhere at = where_scalar(0);
+      for (int e = lane; e < p.B; e += 64) {
+        const AttnWhere other = where(e);
+        even &= other.at == at.at && other.from == at.from;
+      }
       const uint32_t rest = max(items % gridDim.x, 1u);
       const uint32_t load = load_of(lane == 0 ? 0 : lane == 1 ? gridDim.x - 1 : lane == 2 ? rest - 1 : gridDim.x - rest, [&](uint32_t place) {
-        return (uint32_t)(OVER + attn_span<STEP>(p, pos, p.blocks - 1 - (int)(place / (uint32_t)p.B), RB).steps);
+        return (uint32_t)(OVER + attn_span<STEP, MODE>(p, at, p.blocks - 1 - (int)(place / (uint32_t)p.B), RB).steps);
       });
       even &= lane > 3 || load <= share + OVER;
       even = __builtin_amdgcn_ballot_w64(!even) == 0;
     } else {
       const int seq = sequence_of(tid);
-      const uint32_t length = tid < entries ? (uint32_t)(OVER + attn_span<STEP>(p, p.kv.pos[seq], tid - seq * p.blocks, RB).steps) : 0u;
+      const uint32_t length = tid < entries ? (uint32_t)(OVER + attn_span<STEP, MODE>(p, where(seq), tid - seq * p.blocks, RB).steps) : 0u;
       lengths[tid] = length;
       __syncthreads();
       uint32_t rank = 0;
@@ -311,7 +373,9 @@ __global__ __launch_bounds__((64 * AttnForm<NB, F>::waves), 2) void attn_kv4_ker
 
   while (entry < last_entry || (entry == last_entry && (head < last_head || (head == last_head && begin < last_step)))) {
     const int b = uniform(sequence_of(entry)), block = entry - b * p.blocks;
-    AttnSpan span = attn_span<STEP>(p, uniform(scalar_load(p.kv.pos, b)), block, RB);
+    AttnWhere here = where_scalar(b);
+    here.at = uniform(here.at); here.from = uniform(here.from);
+    AttnSpan span = attn_span<STEP, MODE>(p, here, block, RB);
     span.steps = uniform(span.steps); span.sink_steps = uniform(span.sink_steps); span.first = uniform(span.first);
     span.lo = uniform(span.lo); span.hi = uniform(span.hi);
     const int stop = entry == last_entry && head == last_head ? last_step : span.steps;
@@ -324,24 +388,33 @@ __global__ __launch_bounds__((64 * AttnForm<NB, F>::waves), 2) void attn_kv4_ker
     const auto first_token = [&](int s) { return STEP * (s < span.sink_steps ? s : s - span.sink_steps + span.first); };
     // Pages of the next 64 tiles of this wavefront, BATCH steps, a tile to a lane: they are looked up a batch ahead.
     constexpr int BATCH = 64 / TILES;
+    struct Tile { int page, token; };         // (token: of the step, where a list says it)
     const auto look_up = [&](int s) {
+      if constexpr (MODE == kAttnPages) {
+        const int step = min(s + lane / TILES * WAVES, span.steps - 1), shift = p.kv.page_shift - (STEP == 64 ? 6 : 5), at = step >> shift;
+        const int32_t* const mine = p.list + ((size_t)b * Hkv + head) * p.count + at;
+        const int entry = mine[0], before = at > 0 ? mine[-1] : -1;
+        if (entry < 0 || entry <= before || entry >= p.kv.max_pages) return Tile{-1, 0};
+        const size_t at_page = (size_t)table_row(b) * p.kv.max_pages + entry;
+        return Tile{p.kv.table != nullptr ? p.kv.table[at_page] : (int)at_page, (entry << p.kv.page_shift) + (step - (at << shift)) * STEP};
+      }
       const int i = (first_token(min(s + lane / TILES * WAVES, span.steps - 1)) + lane % TILES * 16) >> p.kv.page_shift;
-      if (i >= p.kv.max_pages) return -1;
-      const size_t at_page = (size_t)b * p.kv.max_pages + i;
-      return p.kv.table != nullptr ? p.kv.table[at_page] : (int)at_page;
+      if (i >= p.kv.max_pages) return Tile{-1, 0};
+      const size_t at_page = (size_t)table_row(b) * p.kv.max_pages + i;
+      return Tile{p.kv.table != nullptr ? p.kv.table[at_page] : (int)at_page, 0};
     };
-    int known = look_up(begin + wave), ahead = -1;
+    Tile known = look_up(begin + wave), ahead = Tile{-1, 0};
     const auto pages_of = [&](int k) {        // of the batch's step k
       Pages g;
       g.there = 0;
 #pragma unroll
       for (int i = 0; i < TILES; ++i) {
-        if (i > 0 && P >= STEP) {             // the same page, there or not
+        if (i > 0 && (MODE == kAttnPages || P >= STEP)) {             // the same page, there or not
           g.page[i] = g.page[0];
           g.there |= (g.there & 1u) << i;
           continue;
         }
-        const int page = __builtin_amdgcn_readlane(known, k * TILES + i);
+        const int page = __builtin_amdgcn_readlane(known.page, k * TILES + i);
         const bool there = page >= 0 && page < p.kv.n_pages;
         g.page[i] = there ? page : 0;
         g.there |= there ? 1u << i : 0u;
@@ -368,10 +441,10 @@ __global__ __launch_bounds__((64 * AttnForm<NB, F>::waves), 2) void attn_kv4_ker
 #pragma unroll
       for (int i = 0; i < NP; ++i) {                   // its tiles: i * F + mine_tile
         const uint8_t* par;
-        if (F == 1 || P >= STEP) {
+        if (F == 1 || MODE == kAttnPages || P >= STEP) {
           par = region_of(g.page[i * F]) + (uint32_t)P * D + (uint32_t)((t + 16 * F * i) & (P - 1)) * 8 + (par_off + (uint32_t)mine_tile * 128);
         } else {                                     // pages that end inside a step: a lane's tile has a region of its own
-          const int page = __shfl(known, k * TILES + i * F + mine_tile);
+          const int page = __shfl(known.page, k * TILES + i * F + mine_tile);
           par = region_of(page >= 0 && page < p.kv.n_pages ? page : 0) + (uint32_t)P * D + (uint32_t)((t + 16 * (i * F + mine_tile)) & (P - 1)) * 8 + par_off;
         }
         raw.par[i][0] = reinterpret_cast<const uint4*>(par)[0];
@@ -412,15 +485,24 @@ __global__ __launch_bounds__((64 * AttnForm<NB, F>::waves), 2) void attn_kv4_ker
       factor_of = p.scale_log2 * __builtin_amdgcn_ldexpf(1.0f, ex + 10);
       sum_of = sum * __builtin_amdgcn_ldexpf(1.0f, -ex - 10);
     };
-    const auto position_of = [&](int nb) { return span.lo + over_group(p, row_of_column(nb)) - over_group(p, block * RB); };
+    const auto position_of = [&](int nb) {
+      const int j = over_group(p, row_of_column(nb));
+      if constexpr (MODE == kAttnPrefix) {
+        // (what a row in front of its sequence collects here is not used)
+        const int seq = p.rows == 1 ? j : j / p.rows, at = held_position(p.kv.pos[b * p.group + seq], p.rows) + (j - seq * p.rows);
+        return at < 0 ? span.hi : min(at, span.hi);
+      }
+      return span.lo + j - over_group(p, block * RB);
+    };
     if (!Q_LDS) {
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) load_row(nb, qf[Q_LDS ? 0 : nb]);
     }
     int s = begin + wave, t = 0;
     Pages pages;
+    const auto token_of = [&](int s, int k) { return MODE == kAttnPages ? __builtin_amdgcn_readlane(known.token, k * TILES) : first_token(min(s, span.steps - 1)); };
     if (s < stop) {
-      t = first_token(s);
+      t = token_of(s, 0);
       pages = pages_of(0);
       load_keys(t, pages);
       load_rest(t, pages, 0);
@@ -456,19 +538,28 @@ __global__ __launch_bounds__((64 * AttnForm<NB, F>::waves), 2) void attn_kv4_ker
     const auto factor = [&](int nb) { return Q_LDS ? f_lds[nb * 16 + col].x : f_own[Q_LDS ? 0 : nb]; };
     const auto shift = [&](int nb) { return Q_LDS ? f_lds[nb * 16 + col].y : shift_own[Q_LDS ? 0 : nb]; };
     const auto position = [&](int nb) { return Q_LDS ? __builtin_bit_cast(int, f_lds[nb * 16 + col].z) : pos_own[Q_LDS ? 0 : nb]; };
+    if constexpr (MODE == kAttnPrefix) {      // the first of the rows' last tokens
+      int least = Q_LDS ? __builtin_bit_cast(int, f_lds[Q_LDS ? lane & (RB - 1) : 0].z) : pos_own[0];
+#pragma unroll
+      for (int nb = 1; nb < (Q_LDS ? 1 : NB); ++nb) least = min(least, pos_own[nb]);
+#pragma unroll
+      for (int d = 1; d < 64; d <<= 1) least = min(least, __shfl_xor(least, d));
+      span.lo = uniform(least);
+    }
     int vexp = -30;                           // exponent of the largest value step so far
 
     // ---- the steps of this wavefront
     for (int k = 1; s < stop; s += WAVES, ++k) {
-      const int t_next = first_token(min(s + WAVES, span.steps - 1));       // (the last one's loads repeat a step)
       if (k == BATCH) {
         k = 0;
         known = ahead;
         ahead = look_up(s + (BATCH + 1) * WAVES);
       }
+      const int t_next = token_of(s + WAVES, k);       // (the last one's loads repeat a step)
       const Pages next = pages_of(k);
       // every token of the step in sight of every row
-      const bool whole = pages.there == (1u << TILES) - 1 && t + STEP - 1 <= span.lo && (p.window == 0 || t > behind_window(p, span.hi) || t + STEP <= p.sinks);
+      const bool whole = pages.there == (1u << TILES) - 1 && t + STEP - 1 <= span.lo &&
+                         (MODE == kAttnRest ? t >= here.from : MODE != kAttnWhole || p.window == 0 || t > behind_window(p, span.hi) || t + STEP <= p.sinks);
       v4f sc[NB][TILES];
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb)
@@ -517,11 +608,11 @@ __global__ __launch_bounds__((64 * AttnForm<NB, F>::waves), 2) void attn_kv4_ker
         uint32_t any = 0;                     // bit x: a row of this lane sees its token x
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
-          const int at_row = position(nb), behind = p.window > 0 ? behind_window(p, at_row) : -1;
+          const int at_row = position(nb), behind = MODE == kAttnRest ? here.from - 1 : MODE == kAttnWhole && p.window > 0 ? behind_window(p, at_row) : -1;
 #pragma unroll
           for (int x = 0; x < NX; ++x) {
             const int tok = t + ((x >> 2) * F + mine_tile) * 16 + 4 * kb + (x & 3);
-            const bool in = ((pages.there >> ((x >> 2) * F + mine_tile) & 1u) != 0) & (tok <= at_row) & ((tok > behind) | (tok < p.sinks));
+            const bool in = ((pages.there >> ((x >> 2) * F + mine_tile) & 1u) != 0) & (tok <= at_row) & ((tok > behind) | (MODE == kAttnWhole && tok < p.sinks));
             any |= in ? 1u << x : 0u;
             sv[nb][x] = in ? sv[nb][x] : -__builtin_inff();
           }
@@ -647,8 +738,26 @@ __global__ __launch_bounds__((64 * AttnForm<NB, F>::waves), 2) void attn_kv4_ker
     // ---- the wavefronts' sums, a block of columns at a time
     const bool shared = begin > 0 || stop < span.steps;
     const uint32_t w0 = shared ? group_of(item + OVER + WAVES - 1) : me, w1 = shared ? group_of(item + OVER + span.steps - 1) : me;   // the workgroups that hold a part of it
-    const auto write_row = [&](int r, const float (&v)[4], float sum, float ref) {
+    const auto write_row = [&](int r, float (&v)[4], float sum, float ref) {
       const int j = over_group(p, r), g = r - j * p.G;
+      const size_t row = ((size_t)b * p.kv.T + j) * p.Hq + (size_t)head * p.G + g;
+      if constexpr (MODE == kAttnPrefix) {
+        float* const part = p.joint + row * PART;
+        if (own == 0) *reinterpret_cast<float2*>(part) = float2{ref, sum};
+        *reinterpret_cast<float4*>(part + 4 + own) = float4{v[0], v[1], v[2], v[3]};
+        return;
+      }
+      if constexpr (MODE == kAttnRest) {
+        const float* const part = p.joint + row * PART;
+        const float2 ml = *reinterpret_cast<const float2*>(part);
+        const float4 a = *reinterpret_cast<const float4*>(part + 4 + own);
+        if (span.lo + j - over_group(p, block * RB) >= 0) {        // (a row in front of its sequence has seen nothing)
+          const float to = fmaxf(ref, ml.x), x = __builtin_amdgcn_exp2f(ref - to), y = __builtin_amdgcn_exp2f(ml.x - to);
+          ref = to;
+          sum = sum * x + ml.y * y;
+          v[0] = v[0] * x + a.x * y; v[1] = v[1] * x + a.y * y; v[2] = v[2] * x + a.z * y; v[3] = v[3] * x + a.w * y;
+        }
+      }
       // From 2^27 on, where binary32 goes by 16, a reference can be 8 off and the largest weight past fp16's range; further on all weights zero or infinite.
       const bool none = sum == 0.0f && ref == kNone;
       const float by = fabsf(ref) < 134217728.0f ? 1.0f / sum : __builtin_nanf("");
@@ -656,7 +765,7 @@ __global__ __launch_bounds__((64 * AttnForm<NB, F>::waves), 2) void attn_kv4_ker
       v4h h;
 #pragma unroll
       for (int x = 0; x < 4; ++x) h[x] = none ? (_Float16)0.0f : held_to_half(v[x] * by);
-      *reinterpret_cast<v4h*>(p.out + (((size_t)b * p.kv.T + j) * p.Hq + (size_t)head * p.G + g) * D + own) = h;
+      *reinterpret_cast<v4h*>(p.out + row * D + own) = h;
     };
     const auto write_part = [&](uint32_t slot, int r, float ref, float sum, const float (&v)[4]) {
       float* const part = p.parts + ((size_t)slot * RB + r) * PART;
@@ -810,6 +919,16 @@ __global__ __launch_bounds__((64 * AttnForm<NB, F>::waves), 2) void attn_kv4_ker
     first_run = false;
     if (++head == Hkv) { head = 0; ++entry; }
   }
+}
+
+template <int D, int NB, int F>
+__global__ __launch_bounds__((64 * AttnForm<NB, F>::waves), 2) void attn_kv4_kernel(AttnArgs p) {
+  attn_kv4_work<D, NB, F, kAttnWhole>(p);
+}
+
+template <int D, int NB, int F, int MODE>
+__global__ __launch_bounds__((64 * AttnForm<NB, F>::waves), 2) void attn_kv4_part_kernel(AttnPartArgs p) {
+  attn_kv4_work<D, NB, F, MODE>(p);
 }
 
 }  // namespace qspec

@@ -19,6 +19,7 @@
 #include "gemm_tile16w2.hpp"
 #include "gemm_tile4.hpp"
 #include "kv4.hpp"
+#include "kv4_pages.hpp"
 #include "mlp_chain.hpp"
 #include "pack.hpp"
 #include "producers.hpp"
@@ -874,6 +875,50 @@ void launch_attn(const AttnArgs& a, AttnPlan plan, hipStream_t s) {
   else launch_attn_inst<D, 4, 1>(a, s);
 }
 
+template <int D, int MODE>
+void launch_attn_part(const AttnPartArgs& a, AttnPlan plan, hipStream_t s) {
+  const dim3 grid(AttnForm<1, 1>::workgroups), threads(64 * AttnForm<1, 1>::waves);
+  if (plan.f == 4) launch_kernel((attn_kv4_part_kernel<D, 1, 4, MODE>), grid, threads, 0, s, a);
+  else if (plan.f == 2) launch_kernel((attn_kv4_part_kernel<D, 1, 2, MODE>), grid, threads, 0, s, a);
+  else if (plan.nb == 1) launch_kernel((attn_kv4_part_kernel<D, 1, 1, MODE>), grid, threads, 0, s, a);
+  else if (plan.nb == 2) launch_kernel((attn_kv4_part_kernel<D, 2, 1, MODE>), grid, threads, 0, s, a);
+  else launch_kernel((attn_kv4_part_kernel<D, 4, 1, MODE>), grid, threads, 0, s, a);
+}
+
+// What every call of the attention has.
+AttnArgs attn_args(const KvShape& kv, const void* q_f16, const void* cache, void* out_f16, void* workspace, int B, int Hq, AttnPlan plan, float scale,
+                   int window, int sinks) {
+  const int G = Hq / kv.Hkv, rows = 16 * plan.nb / plan.f;
+  return AttnArgs{kv, static_cast<const uint16_t*>(q_f16), static_cast<const uint8_t*>(cache), static_cast<uint16_t*>(out_f16),
+                  static_cast<unsigned*>(workspace), reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + kAttnTicketBytes), B, Hq, G,
+                  (int)(((long long)kv.T * G + rows - 1) / rows), G > 1 ? (uint32_t)(((1ULL << 32) + G - 1) / G) : 0u, window, sinks, scale * 1.44269504f};
+}
+
+// The kernel counts the steps of the call in 32 bits (32 tokens and a few dozen for each item at most).
+bool attn_counts(const AttnArgs& a, long long tokens) { return (long long)a.B * a.blocks * a.kv.Hkv <= 0x7fffffffLL / (tokens / 32 + 64); }
+
+// (the bounds of the scale keep every score inside binary32, and off the reference of a row that has seen nothing)
+inline bool scale_fits(float scale) { return scale >= 1e-10f && scale <= 1e10f; }
+
+// Bytes of a call's workspace in front of the partial sums of the shared tokens.
+size_t attn_shared_base_bytes(int T, int group, int G, int D) {
+  const size_t a = attn_workspace_bytes(T * group, G, D), b = attn_workspace_bytes(T, G, D);
+  return ((a > b ? a : b) + 255) & ~(size_t)255;
+}
+int check_attn_shared(int B, int T, int Hq, int Hkv, int D, int groups) {
+  if (int st = check_attn(B, T, Hq, Hkv, D)) return st;
+  if (groups < 1 || B % groups != 0 || (long long)(B / groups) * T > (1 << 20)) return QSPEC_ERR_SHAPE;
+  return QSPEC_OK;
+}
+// ---------------------------------------------------------------- bounds of pages, and the choice of pages by them
+inline bool page_is_block(int page_size) { return page_size >= kBlockTokens; }
+
+int check_select(int B, int T, int Hq, int Hkv, int max_pages) {
+  if (B < 1 || T < 1 || T > (1 << 20) || Hkv < 1 || Hq < Hkv || Hq % Hkv != 0 || Hq / Hkv > 255 || max_pages < 1 || max_pages > (1 << 24)) return QSPEC_ERR_SHAPE;
+  if ((long long)B * T * Hkv > 0x7fffffffLL) return QSPEC_ERR_SHAPE;
+  return QSPEC_OK;
+}
+
 int check_sample_shape(int B, int gamma, int V) {
   if (B < 1 || gamma < 0 || V < 1 || V > kSampleMaxV) return QSPEC_ERR_SHAPE;
   if ((long long)B * ((long long)gamma + 1) > 65535) return QSPEC_ERR_SHAPE;
@@ -1293,24 +1338,143 @@ int qspec_attn_kv4(const void* q_f16, const void* cache, const int32_t* pos, con
   if (!q_f16 || !cache || !pos || !out_f16 || !workspace) return QSPEC_ERR_NULL;
   if (int st = check_attn(B, T, Hq, Hkv, D)) return st;
   if (int st = check_kv(page_table, B, T, Hkv, D, page_size, max_pages, n_pages)) return st;
-  // (the bounds of the scale keep every score inside binary32, and off the reference of a row that has seen nothing)
-  if (!(scale >= 1e-10f) || !(scale <= 1e10f) || window < 0 || sinks < 0 || (window == 0 && sinks > 0)) return QSPEC_ERR_SHAPE;
+  if (!scale_fits(scale) || window < 0 || sinks < 0 || (window == 0 && sinks > 0)) return QSPEC_ERR_SHAPE;
   if (misaligned(q_f16) || misaligned(cache) || misaligned(out_f16) || misaligned(workspace) || misaligned4(pos) || misaligned4(page_table))
     return QSPEC_ERR_ALIGN;
   const int G = Hq / Hkv;
   const AttnPlan plan = attn_plan(T, G);
-  const int rows = 16 * plan.nb / plan.f;
   if (workspace_bytes < attn_workspace_bytes(T, G, D)) return QSPEC_ERR_WORKSPACE;
-  const long long blocks = ((long long)T * G + rows - 1) / rows;
-  // the kernel counts the steps of the call in 32 bits (32 tokens and a few dozen for each item at most)
-  if (B * blocks * Hkv > 0x7fffffffLL / ((long long)max_pages * page_size / 32 + 64)) return QSPEC_ERR_SHAPE;
+  const AttnArgs a = attn_args(kv_shape(pos, page_table, T, Hkv, page_size, max_pages, n_pages), q_f16, cache, out_f16, workspace, B, Hq, plan, scale, window, sinks);
+  if (!attn_counts(a, (long long)max_pages * page_size)) return QSPEC_ERR_SHAPE;
   if (int st = check_device()) return st;
-  AttnArgs a{kv_shape(pos, page_table, T, Hkv, page_size, max_pages, n_pages), static_cast<const uint16_t*>(q_f16),
-             static_cast<const uint8_t*>(cache), static_cast<uint16_t*>(out_f16), static_cast<unsigned*>(workspace),
-             reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + kAttnTicketBytes), B, Hq, G, (int)blocks,
-             G > 1 ? (uint32_t)(((1ULL << 32) + G - 1) / G) : 0u, window, sinks, scale * 1.44269504f};
   if (D == 128) launch_attn<128>(a, plan, static_cast<hipStream_t>(stream));
   else launch_attn<64>(a, plan, static_cast<hipStream_t>(stream));
+  return launch_status();
+}
+
+size_t qspec_attn_kv4_shared_workspace_bytes(int B, int T, int Hq, int Hkv, int D, int groups) {
+  if (check_attn_shared(B, T, Hq, Hkv, D, groups) != QSPEC_OK) return 0;
+  return attn_shared_base_bytes(T, B / groups, Hq / Hkv, D) + (size_t)B * T * Hq * attn_part_floats(D) * sizeof(float);
+}
+
+int qspec_attn_kv4_shared(const void* q_f16, const void* cache, const int32_t* pos, const int32_t* page_table, const int32_t* shared,
+                          int B, int T, int Hq, int Hkv, int D, int groups, int page_size, int max_pages, int n_pages,
+                          float scale, void* out_f16, void* workspace, size_t workspace_bytes, void* stream) {
+  if (!q_f16 || !cache || !pos || !shared || !out_f16 || !workspace) return QSPEC_ERR_NULL;
+  if (int st = check_attn_shared(B, T, Hq, Hkv, D, groups)) return st;
+  if (int st = check_kv(page_table, B, T, Hkv, D, page_size, max_pages, n_pages)) return st;
+  if (!scale_fits(scale)) return QSPEC_ERR_SHAPE;
+  if (misaligned(q_f16) || misaligned(cache) || misaligned(out_f16) || misaligned(workspace) || misaligned4(pos) || misaligned4(page_table) || misaligned4(shared))
+    return QSPEC_ERR_ALIGN;
+  const int G = Hq / Hkv, group = B / groups;
+  if (workspace_bytes < qspec_attn_kv4_shared_workspace_bytes(B, T, Hq, Hkv, D, groups)) return QSPEC_ERR_WORKSPACE;
+  const AttnPlan plan = attn_plan(T * group, G), rest_plan = attn_plan(T, G);
+  KvShape kv = kv_shape(pos, page_table, T * group, Hkv, page_size, max_pages, n_pages);
+  AttnPartArgs first{attn_args(kv, q_f16, cache, out_f16, workspace, groups, Hq, plan, scale, 0, 0), T, group, shared,
+                     reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + attn_shared_base_bytes(T, group, G, D)), nullptr, 0};
+  kv.T = T;
+  AttnPartArgs rest = first;
+  static_cast<AttnArgs&>(rest) = attn_args(kv, q_f16, cache, out_f16, workspace, B, Hq, rest_plan, scale, 0, 0);
+  const long long tokens = (long long)max_pages * page_size;
+  if (!attn_counts(first, tokens) || !attn_counts(rest, tokens)) return QSPEC_ERR_SHAPE;
+  if (int st = check_device()) return st;
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  if (D == 128) {
+    launch_attn_part<128, kAttnPrefix>(first, plan, s);
+    launch_attn_part<128, kAttnRest>(rest, rest_plan, s);
+  } else {
+    launch_attn_part<64, kAttnPrefix>(first, plan, s);
+    launch_attn_part<64, kAttnRest>(rest, rest_plan, s);
+  }
+  return launch_status();
+}
+
+size_t qspec_attn_kv4_blocks_workspace_bytes(int B, int T, int Hq, int Hkv, int D) {
+  return check_attn(B, T, Hq, Hkv, D) == QSPEC_OK ? attn_workspace_bytes(1, Hq / Hkv, D) : 0;
+}
+
+int qspec_attn_kv4_blocks(const void* q_f16, const void* cache, const int32_t* pos, const int32_t* page_table, const int32_t* pages,
+                          int B, int T, int Hq, int Hkv, int D, int count, int page_size, int max_pages, int n_pages,
+                          float scale, void* out_f16, void* workspace, size_t workspace_bytes, void* stream) {
+  if (!q_f16 || !cache || !pos || !pages || !out_f16 || !workspace) return QSPEC_ERR_NULL;
+  if (int st = check_attn(B, T, Hq, Hkv, D)) return st;
+  if (int st = check_kv(page_table, B, T, Hkv, D, page_size, max_pages, n_pages)) return st;
+  if (!page_is_block(page_size) || !scale_fits(scale) || count < 1) return QSPEC_ERR_SHAPE;
+  if ((long long)B * T * Hkv * count * 4 >= 0x7fffffffLL) return QSPEC_ERR_SHAPE;
+  if (misaligned(q_f16) || misaligned(cache) || misaligned(out_f16) || misaligned(workspace) || misaligned4(pos) || misaligned4(page_table) || misaligned4(pages))
+    return QSPEC_ERR_ALIGN;
+  const AttnPlan plan = attn_plan(1, Hq / Hkv);
+  if (workspace_bytes < attn_workspace_bytes(1, Hq / Hkv, D)) return QSPEC_ERR_WORKSPACE;
+  const AttnPartArgs a{attn_args(kv_shape(pos, page_table, 1, Hkv, page_size, max_pages, n_pages), q_f16, cache, out_f16, workspace, B * T, Hq, plan, scale, 0, 0),
+                       T, 1, nullptr, nullptr, pages, count};
+  if (!attn_counts(a, (long long)(count < max_pages ? count : max_pages) * page_size)) return QSPEC_ERR_SHAPE;
+  if (int st = check_device()) return st;
+  if (D == 128) launch_attn_part<128, kAttnPages>(a, plan, static_cast<hipStream_t>(stream));
+  else launch_attn_part<64, kAttnPages>(a, plan, static_cast<hipStream_t>(stream));
+  return launch_status();
+}
+
+size_t qspec_kv4_bounds_bytes(int Hkv, int D) { return check_kv_cache(Hkv, D, kBlockTokens) == QSPEC_OK ? bounds_page_bytes(Hkv, D) : 0; }
+
+int qspec_kv4_bounds(const void* cache, const int32_t* pos, const int32_t* page_table, int B, int T, int Hkv, int D,
+                     int page_size, int max_pages, int n_pages, void* bounds, void* stream) {
+  if (!cache || !pos || !bounds) return QSPEC_ERR_NULL;
+  if (int st = check_kv(page_table, B, T, Hkv, D, page_size, max_pages, n_pages)) return st;
+  if (!page_is_block(page_size) || Hkv > 65535) return QSPEC_ERR_SHAPE;
+  const int touched = (T - 1) / page_size + 2;
+  if ((long long)B * touched > (1 << 23)) return QSPEC_ERR_SHAPE;        // (threads of a launch: below 2^32)
+  if (misaligned(cache) || misaligned(bounds) || misaligned4(pos) || misaligned4(page_table)) return QSPEC_ERR_ALIGN;
+  if (int st = check_device()) return st;
+  const BoundsArgs a{kv_shape(pos, page_table, T, Hkv, page_size, max_pages, n_pages), static_cast<const uint8_t*>(cache), static_cast<uint8_t*>(bounds), touched};
+  const dim3 grid(B * touched, Hkv);
+  if (D == 128) launch_kernel(kv4_bounds_kernel<128>, grid, dim3(256), 0, static_cast<hipStream_t>(stream), a);
+  else launch_kernel(kv4_bounds_kernel<64>, grid, dim3(256), 0, static_cast<hipStream_t>(stream), a);
+  return launch_status();
+}
+
+int qspec_kv4_bounds_read(const void* bounds, const int32_t* pos, const int32_t* page_table, int B, int T, int Hkv, int D,
+                          int page_size, int max_pages, int n_pages, float* upper, float* lower, void* stream) {
+  if (!bounds || !pos || !upper || !lower) return QSPEC_ERR_NULL;
+  if (int st = check_kv(page_table, B, T, Hkv, D, page_size, max_pages, n_pages)) return st;
+  const int touched = page_size >= kBlockTokens ? (T - 1) / page_size + 2 : 0;
+  if (touched == 0 || (long long)B * touched > (1 << 23) || (long long)B * touched * Hkv * D * 4 >= 0x7fffffffLL) return QSPEC_ERR_SHAPE;
+  if (misaligned(bounds) || misaligned(upper) || misaligned(lower) || misaligned4(pos) || misaligned4(page_table)) return QSPEC_ERR_ALIGN;
+  if (int st = check_device()) return st;
+  const BoundsReadArgs a{kv_shape(pos, page_table, T, Hkv, page_size, max_pages, n_pages), static_cast<const uint8_t*>(bounds),
+                         reinterpret_cast<float4*>(upper), reinterpret_cast<float4*>(lower), touched};
+  const dim3 grid(B * touched, blocks_for((size_t)Hkv * (D / 4), 256));
+  if (D == 128) launch_kernel(kv4_bounds_read_kernel<128>, grid, dim3(256), 0, static_cast<hipStream_t>(stream), a);
+  else launch_kernel(kv4_bounds_read_kernel<64>, grid, dim3(256), 0, static_cast<hipStream_t>(stream), a);
+  return launch_status();
+}
+
+size_t qspec_kv4_select_workspace_bytes(int B, int T, int Hq, int Hkv, int max_pages) {
+  return check_select(B, T, Hq, Hkv, max_pages) == QSPEC_OK ? (size_t)B * T * Hkv * select_row_keys(max_pages) * sizeof(uint32_t) : 0;
+}
+
+int qspec_kv4_select(const void* q_f16, const void* bounds, const int32_t* pos, const int32_t* page_table, int B, int T, int Hq, int Hkv, int D,
+                     int page_size, int max_pages, int n_pages, int first, int last, int count, int32_t* pages,
+                     void* workspace, size_t workspace_bytes, void* stream) {
+  if (!q_f16 || !bounds || !pos || !pages || !workspace) return QSPEC_ERR_NULL;
+  if (int st = check_attn(B, T, Hq, Hkv, D)) return st;
+  if (int st = check_kv(page_table, B, T, Hkv, D, page_size, max_pages, n_pages)) return st;
+  if (int st = check_select(B, T, Hq, Hkv, max_pages)) return st;
+  if (!page_is_block(page_size) || count < 1 || first < 0 || last < 0 || (long long)first + last > count) return QSPEC_ERR_SHAPE;
+  if ((long long)B * T * Hkv * count * 4 >= 0x7fffffffLL) return QSPEC_ERR_SHAPE;
+  if (misaligned(q_f16) || misaligned(bounds) || misaligned(workspace) || misaligned4(pos) || misaligned4(page_table) || misaligned4(pages)) return QSPEC_ERR_ALIGN;
+  if (workspace_bytes < qspec_kv4_select_workspace_bytes(B, T, Hq, Hkv, max_pages)) return QSPEC_ERR_WORKSPACE;
+  const int G = Hq / Hkv, queries = G > 16 ? 1 : 16 / G;        // of a block of columns
+  const long long sets = (long long)B * ((T + queries - 1) / queries);
+  if (sets * Hkv > 0x7fffffffLL) return QSPEC_ERR_SHAPE;
+  if (int st = check_device()) return st;
+  SelectArgs a{kv_shape(pos, page_table, T, Hkv, page_size, max_pages, n_pages), static_cast<const uint16_t*>(q_f16), static_cast<const uint8_t*>(bounds),
+               static_cast<uint32_t*>(workspace), pages, Hq, G, queries, (T + queries - 1) / queries, first, last, count, select_row_keys(max_pages)};
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  const unsigned chunks = blocks_for((size_t)max_pages, 64);
+  const dim3 grid((unsigned)(sets * Hkv), chunks < 65535u ? chunks : 65535u);
+  if (D == 128) launch_kernel(kv4_score_kernel<128>, grid, dim3(256), 0, s, a);
+  else launch_kernel(kv4_score_kernel<64>, grid, dim3(256), 0, s, a);
+  launch_kernel(kv4_choose_kernel, dim3((unsigned)(B * T * Hkv)), dim3(kChooseThreads), 0, s, a);
   return launch_status();
 }
 
