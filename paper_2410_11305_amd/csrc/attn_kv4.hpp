@@ -84,9 +84,15 @@ struct AttnPartArgs : AttnArgs {
   int rows;                  // rows of a sequence (T of the call)
   int group;                 // sequences of a group
   const int32_t* shared;     // [groups]: tokens that they share
-  float* joint;              // [B * rows * Hq]: partial sums of the shared tokens, attn_part_floats each
+  // Partial sums of the shared tokens, attn_part_floats a row: in `joint` [B * rows * Hq], or in several parts, for an item that several
+  // workgroups hold.  (They stay as they are: the launch that reads them has the rows of an item in many workgroups.)
+  float* joint;
+  float* first_parts;        // [places][1 << first_shift]
+  int2* first_items;         // per item: place of its first part, how many there are
+  int first_shift, first_blocks;      // rows of a block of an item (a power of two), blocks of a group
   const int32_t* list;       // [B * rows][Hkv][count]
   int count;
+  int split;                 // log2 of the parts of an item
 };
 
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
@@ -199,10 +205,12 @@ constexpr size_t attn_workspace() {
 // c / (16 / F) of a step only: the scores of the F tiles are computed for all columns and each column keeps its own, which
 // costs a selection and saves (F - 1) / F of the exponentials and all that goes with them; in the second product a
 // column's weights are zero for the tiles of the others.  Each column ends with its own sums, joined like those of the wavefronts.
-template <int D, int NB, int F, int MODE, class Args>
+template <int D, int NB, int F, int MODE, int W, class Args>
 __device__ __forceinline__ void attn_kv4_work(const Args& p) {
   typedef AttnForm<NB, F> Form;
-  constexpr int WAVES = Form::waves, THREADS = 64 * WAVES, TILES = Form::tiles, STEP = Form::step, RB = Form::rows, OVER = Form::over;
+  constexpr int WAVES = W, THREADS = 64 * WAVES, TILES = Form::tiles, STEP = Form::step, RB = Form::rows, OVER = Form::over;
+  // (sums that are not joined in this launch cost less: 2048 shared tokens of 1024 rows over 8 heads 39 us for 55)
+  constexpr int LEAST = MODE == kAttnWhole || F > 1 ? Form::least : (NB == 4 ? 512 : 256) / STEP;
   constexpr int NK = D / 32;                  // matrix instructions of a tile of q k^T; words of a lane of a key
   constexpr int NV = D / 16;                  // matrix instructions of two tiles of p v
   constexpr int COLS = 16 / F;                // rows of a block of columns
@@ -253,7 +261,7 @@ __device__ __forceinline__ void attn_kv4_work(const Args& p) {
     return (uint32_t)(OVER + attn_span<STEP, MODE>(p, at, e - sequence_of(e) * p.blocks, RB).steps) * (uint32_t)Hkv;
   };
   uint32_t mine = 0;
-  for (int e = lane * per; e < min(entries, (lane + 1) * per); ++e) mine += size_of(e, where(sequence_of(e)));
+  for (int e = lane * per; MODE != kAttnPages && e < min(entries, (lane + 1) * per); ++e) mine += size_of(e, where(sequence_of(e)));
   uint32_t upto = mine;                       // of the entries up to this lane's
 #define QSPEC_DPP_ADD(ctrl, rows) upto += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)upto, ctrl, rows, 0xf, false)
   QSPEC_DPP_ADD(0x111, 0xf);                  // row_shr 1, 2, 4, 8: sums inside a row of 16
@@ -264,9 +272,9 @@ __device__ __forceinline__ void attn_kv4_work(const Args& p) {
   QSPEC_DPP_ADD(0x143, 0xc);                  // row_bcast 31 into rows 2 and 3
 #undef QSPEC_DPP_ADD
   const uint32_t total = (uint32_t)__builtin_amdgcn_readlane((int)upto, 63);
-  const uint32_t groups = uniform(min((uint32_t)gridDim.x, max((uint32_t)(entries * Hkv), (total - (uint32_t)(entries * Hkv) * OVER) / Form::least)));
+  const uint32_t groups = uniform(min((uint32_t)gridDim.x, max((uint32_t)(entries * Hkv), (total - (uint32_t)(entries * Hkv) * OVER) / LEAST)));
   const uint32_t me = blockIdx.x;
-  if (me >= groups) return;
+  if (MODE != kAttnPages && me >= groups) return;
   // workgroup w begins at w * share, and the first `more` of them take one more each; inside an item it begins a whole
   // number of rounds of its wavefronts in, or with the item in one that is not shared out
   const uint32_t share = uniform(total / groups), more = total - share * groups;
@@ -298,7 +306,7 @@ __device__ __forceinline__ void attn_kv4_work(const Args& p) {
   const uint32_t items = (uint32_t)(entries * Hkv);
   const auto dealt = [&](uint32_t round, uint32_t w) { return round * gridDim.x + (round & 1 ? gridDim.x - 1 - w : w); };
   bool whole_items = false;
-  if (items > gridDim.x && items <= kAttnRounds * gridDim.x && (NB == 4 || entries <= THREADS)) {
+  if (MODE != kAttnPages && items > gridDim.x && items <= kAttnRounds * gridDim.x && (NB == 4 || entries <= THREADS)) {
     // Prompts of one length and history are in order by their blocks; the fullest workgroup is one of the ends, or at the
     // end of the last round.  Few rows: one block, or a few, a sequence, and the lengths are sorted, in the LDS of the sums to come.
     uint32_t* const lengths = reinterpret_cast<uint32_t*>(&o_lds[0][0][0]);
@@ -362,7 +370,11 @@ __device__ __forceinline__ void attn_kv4_work(const Args& p) {
     entry = (int)uniform(i / (uint32_t)Hkv);
     head = (int)(i - (uint32_t)entry * (uint32_t)Hkv);
   };
-  if (whole_items) {
+  if constexpr (MODE == kAttnPages) {         // lists have a length that the host knows: a workgroup for each part of each item
+    item = me >> p.split;
+    entry = (int)uniform(item / (uint32_t)Hkv);
+    head = (int)(item - (uint32_t)entry * (uint32_t)Hkv);
+  } else if (whole_items) {
     take();
   } else {
     const Place from = place_of(start_of(me)), to = place_of(start_of(me + 1));
@@ -378,7 +390,15 @@ __device__ __forceinline__ void attn_kv4_work(const Args& p) {
     AttnSpan span = attn_span<STEP, MODE>(p, here, block, RB);
     span.steps = uniform(span.steps); span.sink_steps = uniform(span.sink_steps); span.first = uniform(span.first);
     span.lo = uniform(span.lo); span.hi = uniform(span.hi);
-    const int stop = entry == last_entry && head == last_head ? last_step : span.steps;
+    int stop = entry == last_entry && head == last_head ? last_step : span.steps;
+    int page_parts = 1;
+    if constexpr (MODE == kAttnPages) {
+      const int rounds = (span.steps + WAVES - 1) / WAVES, each = (rounds + (1 << p.split) - 1) >> p.split;
+      begin = (int)(me - (item << p.split)) * each * WAVES;
+      if (begin >= span.steps) return;
+      stop = min(span.steps, begin + each * WAVES);
+      page_parts = (span.steps + each * WAVES - 1) / (each * WAVES);
+    }
     const int rows = min(RB, R - block * RB);
 
     // ---- loads of a step: keys and values of its tiles, steps and lows of this lane's tiles
@@ -737,7 +757,14 @@ __device__ __forceinline__ void attn_kv4_work(const Args& p) {
 
     // ---- the wavefronts' sums, a block of columns at a time
     const bool shared = begin > 0 || stop < span.steps;
-    const uint32_t w0 = shared ? group_of(item + OVER + WAVES - 1) : me, w1 = shared ? group_of(item + OVER + span.steps - 1) : me;   // the workgroups that hold a part of it
+    uint32_t w0 = me, w1 = me;                // the workgroups that hold a part of it
+    if constexpr (MODE == kAttnPages) {
+      w0 = item << p.split;
+      w1 = w0 + (uint32_t)page_parts - 1;
+    } else if (shared) {
+      w0 = group_of(item + OVER + WAVES - 1);
+      w1 = group_of(item + OVER + span.steps - 1);
+    }
     const auto write_row = [&](int r, float (&v)[4], float sum, float ref) {
       const int j = over_group(p, r), g = r - j * p.G;
       const size_t row = ((size_t)b * p.kv.T + j) * p.Hq + (size_t)head * p.G + g;
@@ -748,14 +775,28 @@ __device__ __forceinline__ void attn_kv4_work(const Args& p) {
         return;
       }
       if constexpr (MODE == kAttnRest) {
-        const float* const part = p.joint + row * PART;
-        const float2 ml = *reinterpret_cast<const float2*>(part);
-        const float4 a = *reinterpret_cast<const float4*>(part + 4 + own);
-        if (span.lo + j - over_group(p, block * RB) >= 0) {        // (a row in front of its sequence has seen nothing)
-          const float to = fmaxf(ref, ml.x), x = __builtin_amdgcn_exp2f(ref - to), y = __builtin_amdgcn_exp2f(ml.x - to);
-          ref = to;
-          sum = sum * x + ml.y * y;
-          v[0] = v[0] * x + a.x * y; v[1] = v[1] * x + a.y * y; v[2] = v[2] * x + a.z * y; v[3] = v[3] * x + a.w * y;
+        const int set = b / p.group, in_set = ((b - set * p.group) * p.rows + j) * p.G + g;
+        const int2 item_of = p.first_items[(size_t)(set * p.first_blocks + (in_set >> p.first_shift)) * Hkv + head];
+        const int n = span.lo + j - over_group(p, block * RB) < 0 ? 0 : item_of.y;      // (a row in front of its sequence has seen nothing)
+        constexpr int FLY = 4;
+        for (int i0 = 0; i0 < n; i0 += FLY) {
+          float2 ml[FLY];
+          float4 a[FLY];
+#pragma unroll
+          for (int y = 0; y < FLY; ++y) {
+            const int i = min(i0 + y, n - 1), place = i == 0 ? item_of.x : (item_of.x & ~1) + 2 * i;
+            const float* const part = n == 1 ? p.joint + row * PART : p.first_parts + (((size_t)place << p.first_shift) + (in_set & ((1 << p.first_shift) - 1))) * PART;
+            ml[y] = *reinterpret_cast<const float2*>(part);
+            a[y] = *reinterpret_cast<const float4*>(part + 4 + own);
+          }
+#pragma unroll
+          for (int y = 0; y < FLY; ++y) {
+            if (i0 + y >= n) break;
+            const float to = fmaxf(ref, ml[y].x), w = __builtin_amdgcn_exp2f(ref - to), z = __builtin_amdgcn_exp2f(ml[y].x - to);
+            ref = to;
+            sum = sum * w + ml[y].y * z;
+            v[0] = v[0] * w + a[y].x * z; v[1] = v[1] * w + a[y].y * z; v[2] = v[2] * w + a[y].z * z; v[3] = v[3] * w + a[y].w * z;
+          }
         }
       }
       // From 2^27 on, where binary32 goes by 16, a reference can be 8 off and the largest weight past fp16's range; further on all weights zero or infinite.
@@ -769,6 +810,11 @@ __device__ __forceinline__ void attn_kv4_work(const Args& p) {
     };
     const auto write_part = [&](uint32_t slot, int r, float ref, float sum, const float (&v)[4]) {
       float* const part = p.parts + ((size_t)slot * RB + r) * PART;
+      if constexpr (MODE == kAttnPrefix) {
+        if (own == 0) *reinterpret_cast<float2*>(part) = float2{ref, sum};
+        *reinterpret_cast<float4*>(part + 4 + own) = float4{v[0], v[1], v[2], v[3]};
+        return;
+      }
       if (own == 0) store_shared_f2(part, ref, sum);
       store_shared_f2(part + 4 + own, v[0], v[1]);
       store_shared_f2(part + 6 + own, v[2], v[3]);
@@ -805,6 +851,9 @@ __device__ __forceinline__ void attn_kv4_work(const Args& p) {
         }
       }
     };
+    if constexpr (MODE == kAttnPrefix) {
+      if (begin == 0 && tid == 0) p.first_items[(size_t)entry * Hkv + head] = shared ? int2{(int)(2 * me + (first_run ? 0 : 1)), (int)(w1 - w0 + 1)} : int2{0, 1};
+    }
 #pragma unroll 1
     for (int nb = 0; nb < NB && nb * COLS < rows; ++nb) {
       if (NB == 1 || nb == 0) hand_over(0);
@@ -833,7 +882,7 @@ __device__ __forceinline__ void attn_kv4_work(const Args& p) {
         if (!shared) {
           write_row(block * RB + r, v, total_l, ref);
         } else {
-          write_part(2 * me + (first_run ? 0 : 1), r, ref, total_l, v);
+          write_part(MODE == kAttnPages ? me : 2 * me + (first_run ? 0 : 1), r, ref, total_l, v);
         }
       }
       __syncthreads();
@@ -842,9 +891,10 @@ __device__ __forceinline__ void attn_kv4_work(const Args& p) {
     // ---- the last of the item's workgroups joins their parts; of many parts, the last of each eight theirs first (a
     // workgroup reads parts past the caches at tens of GB/s: 64 parts of 8 rows in one go take 14 us)
     const uint32_t parts = w1 - w0 + 1;
-    const auto slot_of = [&](uint32_t w) { return w == w0 ? 2 * w0 + (start_of(w0) < item ? 1 : 0) : 2 * w; };
+    const auto slot_of = [&](uint32_t w) { return MODE == kAttnPages ? w : w == w0 ? 2 * w0 + (start_of(w0) < item ? 1 : 0) : 2 * w; };
 #pragma unroll 1
     for (int stage = parts > 16 ? 0 : 1; shared && stage < 2; ++stage) {
+      if constexpr (MODE == kAttnPrefix) break;
       uint32_t first = w0, stride = 1, n = parts, counter = w0;
       if (stage == 0) {
         first = w0 + ((me - w0) & ~7u);
@@ -909,6 +959,7 @@ __device__ __forceinline__ void attn_kv4_work(const Args& p) {
         __syncthreads();
       }
     }
+    if constexpr (MODE == kAttnPages) return;
     if (last_head < 0) {
       ++item;
       take();
@@ -923,12 +974,12 @@ __device__ __forceinline__ void attn_kv4_work(const Args& p) {
 
 template <int D, int NB, int F>
 __global__ __launch_bounds__((64 * AttnForm<NB, F>::waves), 2) void attn_kv4_kernel(AttnArgs p) {
-  attn_kv4_work<D, NB, F, kAttnWhole>(p);
+  attn_kv4_work<D, NB, F, kAttnWhole, AttnForm<NB, F>::waves>(p);
 }
 
-template <int D, int NB, int F, int MODE>
-__global__ __launch_bounds__((64 * AttnForm<NB, F>::waves), 2) void attn_kv4_part_kernel(AttnPartArgs p) {
-  attn_kv4_work<D, NB, F, MODE>(p);
+template <int D, int NB, int F, int MODE, int W = AttnForm<NB, F>::waves>
+__global__ __launch_bounds__((64 * W), 2) void attn_kv4_part_kernel(AttnPartArgs p) {
+  attn_kv4_work<D, NB, F, MODE, W>(p);
 }
 
 }  // namespace qspec

@@ -876,13 +876,23 @@ void launch_attn(const AttnArgs& a, AttnPlan plan, hipStream_t s) {
 }
 
 template <int D, int MODE>
-void launch_attn_part(const AttnPartArgs& a, AttnPlan plan, hipStream_t s) {
-  const dim3 grid(AttnForm<1, 1>::workgroups), threads(64 * AttnForm<1, 1>::waves);
+void launch_attn_part(const AttnPartArgs& a, AttnPlan plan, hipStream_t s, unsigned workgroups = AttnForm<1, 1>::workgroups) {
+  const dim3 grid(workgroups), threads(64 * AttnForm<1, 1>::waves);
   if (plan.f == 4) launch_kernel((attn_kv4_part_kernel<D, 1, 4, MODE>), grid, threads, 0, s, a);
   else if (plan.f == 2) launch_kernel((attn_kv4_part_kernel<D, 1, 2, MODE>), grid, threads, 0, s, a);
   else if (plan.nb == 1) launch_kernel((attn_kv4_part_kernel<D, 1, 1, MODE>), grid, threads, 0, s, a);
   else if (plan.nb == 2) launch_kernel((attn_kv4_part_kernel<D, 2, 1, MODE>), grid, threads, 0, s, a);
   else launch_kernel((attn_kv4_part_kernel<D, 4, 1, MODE>), grid, threads, 0, s, a);
+}
+
+// The same with workgroups of one wavefront, up to two blocks of columns.
+template <int D, int MODE>
+void launch_attn_waves(const AttnPartArgs& a, AttnPlan plan, hipStream_t s, unsigned workgroups) {
+  const dim3 grid(workgroups), threads(64);
+  if (plan.f == 4) launch_kernel((attn_kv4_part_kernel<D, 1, 4, MODE, 1>), grid, threads, 0, s, a);
+  else if (plan.f == 2) launch_kernel((attn_kv4_part_kernel<D, 1, 2, MODE, 1>), grid, threads, 0, s, a);
+  else if (plan.nb == 1) launch_kernel((attn_kv4_part_kernel<D, 1, 1, MODE, 1>), grid, threads, 0, s, a);
+  else launch_kernel((attn_kv4_part_kernel<D, 2, 1, MODE, 1>), grid, threads, 0, s, a);
 }
 
 // What every call of the attention has.
@@ -900,10 +910,20 @@ bool attn_counts(const AttnArgs& a, long long tokens) { return (long long)a.B * 
 // (the bounds of the scale keep every score inside binary32, and off the reference of a row that has seen nothing)
 inline bool scale_fits(float scale) { return scale >= 1e-10f && scale <= 1e10f; }
 
-// Bytes of a call's workspace in front of the partial sums of the shared tokens.
-size_t attn_shared_base_bytes(int T, int group, int G, int D) {
-  const size_t a = attn_workspace_bytes(T * group, G, D), b = attn_workspace_bytes(T, G, D);
-  return ((a > b ? a : b) + 255) & ~(size_t)255;
+// A call's workspace: what the second launch has for itself, then the first one's partial sums, their directory, and those that are whole.
+struct SharedWorkspace { size_t parts, items, joint, bytes; };
+SharedWorkspace attn_shared_workspace(int B, int T, int Hq, int Hkv, int D, int groups) {
+  const int G = Hq / Hkv, rows = B / groups * T;
+  const AttnPlan plan = attn_plan(rows, G);
+  const int block = 16 * plan.nb / plan.f;
+  const size_t items = (size_t)groups * (((size_t)rows * G + block - 1) / block) * Hkv;
+  const auto up = [](size_t n) { return (n + 255) & ~(size_t)255; };
+  SharedWorkspace w;
+  w.parts = up(attn_workspace_bytes(T, G, D));
+  w.items = w.parts + up(attn_workspace_bytes(rows, G, D) - kAttnTicketBytes);
+  w.joint = w.items + up(items * sizeof(int2));
+  w.bytes = w.joint + (size_t)B * T * Hq * attn_part_floats(D) * sizeof(float);
+  return w;
 }
 int check_attn_shared(int B, int T, int Hq, int Hkv, int D, int groups) {
   if (int st = check_attn(B, T, Hq, Hkv, D)) return st;
@@ -1354,7 +1374,7 @@ int qspec_attn_kv4(const void* q_f16, const void* cache, const int32_t* pos, con
 
 size_t qspec_attn_kv4_shared_workspace_bytes(int B, int T, int Hq, int Hkv, int D, int groups) {
   if (check_attn_shared(B, T, Hq, Hkv, D, groups) != QSPEC_OK) return 0;
-  return attn_shared_base_bytes(T, B / groups, Hq / Hkv, D) + (size_t)B * T * Hq * attn_part_floats(D) * sizeof(float);
+  return attn_shared_workspace(B, T, Hq, Hkv, D, groups).bytes;
 }
 
 int qspec_attn_kv4_shared(const void* q_f16, const void* cache, const int32_t* pos, const int32_t* page_table, const int32_t* shared,
@@ -1367,11 +1387,16 @@ int qspec_attn_kv4_shared(const void* q_f16, const void* cache, const int32_t* p
   if (misaligned(q_f16) || misaligned(cache) || misaligned(out_f16) || misaligned(workspace) || misaligned4(pos) || misaligned4(page_table) || misaligned4(shared))
     return QSPEC_ERR_ALIGN;
   const int G = Hq / Hkv, group = B / groups;
-  if (workspace_bytes < qspec_attn_kv4_shared_workspace_bytes(B, T, Hq, Hkv, D, groups)) return QSPEC_ERR_WORKSPACE;
+  const SharedWorkspace w = attn_shared_workspace(B, T, Hq, Hkv, D, groups);
+  if (workspace_bytes < w.bytes) return QSPEC_ERR_WORKSPACE;
+  uint8_t* const base = static_cast<uint8_t*>(workspace);
   const AttnPlan plan = attn_plan(T * group, G), rest_plan = attn_plan(T, G);
   KvShape kv = kv_shape(pos, page_table, T * group, Hkv, page_size, max_pages, n_pages);
   AttnPartArgs first{attn_args(kv, q_f16, cache, out_f16, workspace, groups, Hq, plan, scale, 0, 0), T, group, shared,
-                     reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + attn_shared_base_bytes(T, group, G, D)), nullptr, 0};
+                     reinterpret_cast<float*>(base + w.joint), reinterpret_cast<float*>(base + w.parts), reinterpret_cast<int2*>(base + w.items),
+                     log2_exact(16 * plan.nb / plan.f), 0, nullptr, 0, 0};
+  first.first_blocks = first.blocks;
+  first.parts = first.first_parts;
   kv.T = T;
   AttnPartArgs rest = first;
   static_cast<AttnArgs&>(rest) = attn_args(kv, q_f16, cache, out_f16, workspace, B, Hq, rest_plan, scale, 0, 0);
@@ -1405,12 +1430,24 @@ int qspec_attn_kv4_blocks(const void* q_f16, const void* cache, const int32_t* p
     return QSPEC_ERR_ALIGN;
   const AttnPlan plan = attn_plan(1, Hq / Hkv);
   if (workspace_bytes < attn_workspace_bytes(1, Hq / Hkv, D)) return QSPEC_ERR_WORKSPACE;
-  const AttnPartArgs a{attn_args(kv_shape(pos, page_table, 1, Hkv, page_size, max_pages, n_pages), q_f16, cache, out_f16, workspace, B * T, Hq, plan, scale, 0, 0),
-                       T, 1, nullptr, nullptr, pages, count};
-  if (!attn_counts(a, (long long)(count < max_pages ? count : max_pages) * page_size)) return QSPEC_ERR_SHAPE;
+  const AttnArgs common = attn_args(kv_shape(pos, page_table, 1, Hkv, page_size, max_pages, n_pages), q_f16, cache, out_f16, workspace, B * T, Hq, plan, scale, 0, 0);
+  const long long tokens = (long long)(count < max_pages ? count : max_pages) * page_size, items = (long long)B * T * common.blocks * Hkv;
+  if (!attn_counts(common, tokens)) return QSPEC_ERR_SHAPE;
+  const int steps = (int)(tokens / (plan.f > 1 ? 64 : 32));
+  // A wavefront to an item where there are enough of them (us, 228 rows of 32 heads and 1 page: 16 for 33; 512 rows of 8 heads and 16 pages: 62 for 75;
+  // 128 rows of 8 heads and 32 pages: 33 for 28).  Four to a workgroup otherwise, which share the items out among the compute units, a step
+  // to a wavefront at least (64 items of 32 pages: 11 in 256 workgroups, 15 in 512).
+  const bool single = plan.nb < 4 && (items >= 2048 || (items >= 1024 && steps <= 8));
+  int split = 0;
+  while (!single && split < 4 && items << (split + 1) <= 256 && steps >> (split + 1) >= 4) ++split;
+  const AttnPartArgs a{common, T, 1, nullptr, nullptr, nullptr, nullptr, 0, 0, pages, count, split};
   if (int st = check_device()) return st;
-  if (D == 128) launch_attn_part<128, kAttnPages>(a, plan, static_cast<hipStream_t>(stream));
-  else launch_attn_part<64, kAttnPages>(a, plan, static_cast<hipStream_t>(stream));
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  const unsigned workgroups = (unsigned)(items << split);
+  if (single && D == 128) launch_attn_waves<128, kAttnPages>(a, plan, s, workgroups);
+  else if (single) launch_attn_waves<64, kAttnPages>(a, plan, s, workgroups);
+  else if (D == 128) launch_attn_part<128, kAttnPages>(a, plan, s, workgroups);
+  else launch_attn_part<64, kAttnPages>(a, plan, s, workgroups);
   return launch_status();
 }
 
