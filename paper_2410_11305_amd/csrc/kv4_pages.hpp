@@ -154,7 +154,8 @@ struct SelectArgs {
   uint32_t* keys;            // [B * T][Hkv][pitch]
   int32_t* pages;            // [B * T][Hkv][count]
   int Hq, G;
-  int queries, sets;         // queries of a block of 16 columns, blocks of a sequence
+  int width, columns;        // log2 of the columns that a query's heads take in a block of 16, blocks of a workgroup
+  int queries, sets;         // queries of a workgroup, workgroups that a sequence's queries take
   int first, last, count;
   int pitch;
 };
@@ -174,25 +175,63 @@ __device__ inline uint32_t key_of(float score) {
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-// grid (B * sets * Hkv, chunks): 16 pages and 16 columns (heads of `queries` queries, or 16 of one query's heads at a time) a
-// wavefront, one matrix product over 2 D features.  Lane (row, k): row = lane & 15, 16 codes from 16 (lane >> 4) on in each of the 64.
+// Largest over the 2^width neighbouring lanes of a row of 16 that hold a query's heads.
+__device__ inline float head_max(float v, int width) {
+  if (width > 0) v = fmaxf(v, dpp_f32<0xB1>(v));
+  if (width > 1) v = fmaxf(v, dpp_f32<0x4E>(v));
+  if (width > 2) v = fmaxf(v, dpp_f32<0x141>(v));
+  if (width > 3) v = fmaxf(v, dpp_f32<0x140>(v));
+  return v;
+}
+template <int CTRL>
+__device__ inline int dpp_max(int v) { return max(v, __builtin_amdgcn_update_dpp(v, v, CTRL, 0xf, 0xf, false)); }
+__device__ inline int head_max(int v, int width) {
+  if (width > 0) v = dpp_max<0xB1>(v);
+  if (width > 1) v = dpp_max<0x4E>(v);
+  if (width > 2) v = dpp_max<0x141>(v);
+  if (width > 3) v = dpp_max<0x140>(v);
+  return v;
+}
+
+constexpr int kScoreColumns = 4;                       // blocks of 16 columns of a workgroup (as many as one query takes, where that is more)
+
+// grid (B * sets * Hkv, chunks): a product of pages by heads over 2 D features, 16 by 16 a matrix instruction.  A query's heads take the next
+// power of two of columns (repeating the last one), so their largest score is a fold in a row of lanes; more than 16 take several
+// blocks.  The queries' codes are worked out once a workgroup and shared through LDS; each wavefront runs through its pages, 16 at a time, with the next ones' bounds
+// on their way.  Lane (row, k): row = lane & 15, 16 codes from 16 (lane >> 4) on in each 64.
 template <int D>
 __global__ __launch_bounds__(256) void kv4_score_kernel(SelectArgs p) {
   constexpr int NI = D / 64;                           // matrix instructions of a half
-  __shared__ int dots[4][16][17];
-  __shared__ float tops[4][256];
+  extern __shared__ __align__(16) uint8_t score_lds[];       // [columns][2 NI][64] of 16 bytes
+  v4i* const codes = reinterpret_cast<v4i*>(score_lds);
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), col = lane & 15, kb = lane >> 4;
   const int head = blockIdx.x % p.kv.Hkv, set = blockIdx.x / p.kv.Hkv, b = set / p.sets, j0 = (set - b * p.sets) * p.queries;
   const int queries = min(p.queries, p.kv.T - j0);
   const int n = pages_in_sight(p.kv, b, j0 + queries - 1);
   if (n <= p.count) return;                            // all of them are taken
+  if ((int)blockIdx.y * 64 >= n) return;
+  const size_t row_bytes = bounds_page_bytes(p.kv.Hkv, D);
+  // ---- the bounds of 16 pages
+  v4i u[NI], l[NI];
+  float grid;                                          // of page i0 + col; below zero: there is none
+  const auto load_pages = [&](int i0) {
+    const int mine = i0 + col;
+    const int page = mine < n ? kv_page(p.kv, b, (long long)mine << p.kv.page_shift) : -1;
+    const uint8_t* const in = p.bounds + (size_t)max(page, 0) * row_bytes;
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      u[i] = *reinterpret_cast<const v4i*>(in + (size_t)head * (2 * D) + 64 * i + 16 * kb);
+      l[i] = *reinterpret_cast<const v4i*>(in + (size_t)head * (2 * D) + D + 64 * i + 16 * kb);
+    }
+    const float g = reinterpret_cast<const float*>(in + (size_t)p.kv.Hkv * 2 * D)[head];
+    grid = page >= 0 ? g : -1.0f;
+  };
   int i0 = (blockIdx.y * 4 + wave) * 16;
-  if (i0 >= n) return;                                 // (wavefronts are on their own from here on)
-  const int passes = (min(p.queries, 16) * p.G + 15) / 16;       // of the heads: one, or one query's in sets of 16
-  const int columns = queries * p.G;
-  typedef uint4 Rows[2 * NI];
-  const auto load = [&](int pass, Rows& x) {           // 16 features from 16 kb + 64 i on
-    const int c = min(pass * 16 + col, columns - 1), j = c / p.G, g = c - j * p.G;
+  load_pages(i0);                                      // (past the last page: there is none)
+  // ---- the codes of the queries: block c by wavefront c % 4
+  const int per = 16 >> p.width;                       // queries of a block, where they take one
+  const auto load_row = [&](int c, uint4 (&x)[2 * NI]) {       // 16 features from 16 kb + 64 i on
+    const int j = p.G > 16 ? 0 : min(c * per + (col >> p.width), queries - 1), g = p.G > 16 ? min(c * 16 + col, p.G - 1) : min(col & ((1 << p.width) - 1), p.G - 1);
     const uint16_t* const src = p.q + (((size_t)b * p.kv.T + j0 + j) * p.Hq + (size_t)head * p.G + g) * D + kb * 16;
 #pragma unroll
     for (int i = 0; i < NI; ++i) {
@@ -200,10 +239,7 @@ __global__ __launch_bounds__(256) void kv4_score_kernel(SelectArgs p) {
       x[2 * i + 1] = reinterpret_cast<const uint4*>(src + 64 * i)[1];
     }
   };
-  // ---- the grid of each query
-  Rows x;
-  for (int pass = 0; pass < passes; ++pass) {
-    load(pass, x);
+  const auto top_of = [&](const uint4 (&x)[2 * NI]) {          // of a block's queries; infinite where one feature is no finite number
     float top = 0.0f, odd = 0.0f;
 #pragma unroll
     for (int i = 0; i < 2 * NI; ++i) {
@@ -211,85 +247,77 @@ __global__ __launch_bounds__(256) void kv4_score_kernel(SelectArgs p) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) { top = fmaxf(top, fabsf((float)h[e])); odd += (float)h[e] * 0.0f; }
     }
-    top = odd == 0.0f ? top : __builtin_inff();
-    top = column_max(top);
-    if (kb == 0) tops[wave][pass * 16 + col] = top;
-  }
-  wave_lds_order();
-  const auto inverse_of = [&](int pass) {              // of a column's query: 1 / grid, or 0 for one that holds what is no number
-    const int c = min(pass * 16 + col, columns - 1), j = c / p.G;
-    float top = 0.0f;
-    for (int g = 0; g < p.G; ++g) top = fmaxf(top, tops[wave][j * p.G + g]);
-    return top < __builtin_inff() ? 1.0f / grid_of(top) : 0.0f;
+    return head_max(column_max(odd == 0.0f ? top : __builtin_inff()), p.width);
   };
-  const auto codes = [&](const Rows& x, float inverse, v4i (&plus)[NI], v4i (&minus)[NI]) {
+  const int blocks = p.G > 16 ? p.columns : (queries + per - 1) / per;
+  float all_heads = 0.0f;
+  for (int c = 0; c < (p.G > 16 ? blocks : 0); ++c) {
+    uint4 x[2 * NI];
+    load_row(c, x);
+    all_heads = fmaxf(all_heads, top_of(x));
+  }
+  for (int c = wave; c < blocks; c += 4) {
+    uint4 x[2 * NI];
+    load_row(c, x);
+    const float top = p.G > 16 ? all_heads : top_of(x), inverse = top < __builtin_inff() ? 1.0f / grid_of(top) : 0.0f;
 #pragma unroll
     for (int i = 0; i < NI; ++i) {
+      v4i plus, minus;
 #pragma unroll
       for (int w = 0; w < 4; ++w) {
         const v8h h = __builtin_bit_cast(v8h, x[2 * i + w / 2]);
         uint32_t a = 0, m = 0;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const float f = (float)h[4 * (w & 1) + e];
-          const int c = inverse > 0.0f ? (int)rintf(f * inverse) : 0;
-          a |= (uint32_t)max(c, 0) << (8 * e);
-          m |= ((uint32_t)min(c, 0) & 255u) << (8 * e);
+          const int k = inverse > 0.0f ? (int)rintf((float)h[4 * (w & 1) + e] * inverse) : 0;
+          a |= (uint32_t)max(k, 0) << (8 * e);
+          m |= ((uint32_t)min(k, 0) & 255u) << (8 * e);
         }
-        plus[i][w] = (int)a;
-        minus[i][w] = (int)m;
+        plus[w] = (int)a;
+        minus[w] = (int)m;
       }
+      codes[(c * 2 * NI + i) * 64 + lane] = plus;
+      codes[(c * 2 * NI + NI + i) * 64 + lane] = minus;
     }
-  };
-  v4i plus[NI], minus[NI];
-  if (passes == 1) codes(x, inverse_of(0), plus, minus);
-  const size_t row_bytes = bounds_page_bytes(p.kv.Hkv, D);
+  }
+  __syncthreads();
   for (; i0 < n; i0 += gridDim.y * 64) {
-    // ---- the bounds of 16 pages
-    const int mine = i0 + col;
-    const int page = mine < n ? kv_page(p.kv, b, (long long)mine << p.kv.page_shift) : -1;
-    const uint8_t* const in = p.bounds + (size_t)max(page, 0) * row_bytes;
-    v4i u[NI], l[NI];
+    v4i now_u[NI], now_l[NI];
+    float g4[4];
 #pragma unroll
-    for (int i = 0; i < NI; ++i) {
-      u[i] = *reinterpret_cast<const v4i*>(in + (size_t)head * (2 * D) + 64 * i + 16 * kb);
-      l[i] = *reinterpret_cast<const v4i*>(in + (size_t)head * (2 * D) + D + 64 * i + 16 * kb);
-    }
-    const float grid = page >= 0 ? reinterpret_cast<const float*>(in + (size_t)p.kv.Hkv * 2 * D)[head] : 0.0f;
-    int best = -0x7fffffff;                            // (several passes: of one query)
-    for (int pass = 0; pass < passes; ++pass) {
-      if (passes > 1) {
-        load(pass, x);
-        codes(x, inverse_of(pass), plus, minus);
-      }
+    for (int i = 0; i < NI; ++i) { now_u[i] = u[i]; now_l[i] = l[i]; }
+#pragma unroll
+    for (int r = 0; r < 4; ++r) g4[r] = __shfl(grid, 4 * kb + r);
+    const int here = i0;
+    if (i0 + (int)gridDim.y * 64 < n) load_pages(i0 + gridDim.y * 64);
+    v4i best = {};
+    for (int c = 0; c < blocks; ++c) {
       v4i dot = {0, 0, 0, 0};
 #pragma unroll
       for (int i = 0; i < NI; ++i) {
-        dot = __builtin_amdgcn_mfma_i32_16x16x64_i8(u[i], plus[i], dot, 0, 0, 0);
-        dot = __builtin_amdgcn_mfma_i32_16x16x64_i8(l[i], minus[i], dot, 0, 0, 0);
+        dot = __builtin_amdgcn_mfma_i32_16x16x64_i8(now_u[i], codes[(c * 2 * NI + i) * 64 + lane], dot, 0, 0, 0);
+        dot = __builtin_amdgcn_mfma_i32_16x16x64_i8(now_l[i], codes[(c * 2 * NI + NI + i) * 64 + lane], dot, 0, 0, 0);
       }
-      wave_lds_order();
+      if (p.G > 16) {
 #pragma unroll
-      for (int r = 0; r < 4; ++r) dots[wave][4 * kb + r][col] = dot[r];
-      wave_lds_order();
-      if (passes > 1) {
-        for (int c = 0; c < min(16, columns - pass * 16); ++c) best = max(best, dots[wave][col][c]);
+        for (int r = 0; r < 4; ++r) best[r] = c == 0 ? dot[r] : max(best[r], dot[r]);
+        if (c + 1 < blocks) continue;
+        dot = best;
       }
-    }
-    // ---- the best of a query's heads: lane (page, query)
-    for (int j = kb; j < queries; j += 4) {
-      if (passes == 1) {
-        best = dots[wave][col][j * p.G];
-        for (int g = 1; g < p.G; ++g) best = max(best, dots[wave][col][j * p.G + g]);
+      uint32_t key[4];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const float score = (float)head_max(dot[r], p.width) * g4[r];
+        key[r] = g4[r] < 0.0f ? kKeyNone : g4[r] == g4[r] ? key_of(score) : kKeyOdd;
       }
-      const uint32_t key = page < 0 ? kKeyNone : grid == grid ? key_of((float)best * grid) : kKeyOdd;
-      if (mine < n) p.keys[(((size_t)b * p.kv.T + j0 + j) * p.kv.Hkv + head) * p.pitch + mine] = key;
+      const int j = p.G > 16 ? 0 : c * per + (col >> p.width);
+      if ((col & ((1 << p.width) - 1)) == 0 && j < queries)      // (up to the end of 16 pages: rows have room for whole sets of 64)
+        *reinterpret_cast<uint4*>(p.keys + (((size_t)b * p.kv.T + j0 + j) * p.kv.Hkv + head) * p.pitch + here + 4 * kb) = uint4{key[0], key[1], key[2], key[3]};
     }
-    wave_lds_order();
   }
 }
 
-constexpr int kChooseThreads = 256, kChooseKeys = 8192, kChooseBins = 2048;
+constexpr int kChooseThreads = 256, kChooseBins = 2048;
 
 // Sum of v over the threads before this one, and over all.
 __device__ inline uint32_t scan_before(uint32_t v, uint32_t* waves, uint32_t& all) {
@@ -313,12 +341,176 @@ __device__ inline uint32_t scan_before(uint32_t v, uint32_t* waves, uint32_t& al
   return before + upto - v;
 }
 
-// grid (B * T * Hkv): one row's `count` best pages, in their order.  The key that the last of them has is found by histograms over the range
+// The need-th key from the top of low .. low + 2^width - 1 narrowed down by a histogram over 2048 parts of that range, in `bins`: the part it lies
+// in, which of its keys it is, and how many it has, in found.  The threads' own parts are 8 neighbouring ones, from the top.
+__device__ inline void find_part(const uint32_t* bins, uint32_t* waves, uint32_t* found, uint32_t need) {
+  const int tid = threadIdx.x;
+  uint32_t part[8], mine = 0, all;
+  const uint4 a = reinterpret_cast<const uint4*>(bins)[(kChooseBins - 8 - 8 * tid) / 4], b = reinterpret_cast<const uint4*>(bins)[(kChooseBins - 8 - 8 * tid) / 4 + 1];
+  part[0] = b.w; part[1] = b.z; part[2] = b.y; part[3] = b.x; part[4] = a.w; part[5] = a.z; part[6] = a.y; part[7] = a.x;
+#pragma unroll
+  for (int k = 0; k < 8; ++k) mine += part[k];
+  uint32_t before = scan_before(mine, waves, all);
+  if (before < need && before + mine >= need) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      if (before < need && before + part[k] >= need) {
+        found[0] = (uint32_t)(kChooseBins - 1 - (8 * tid + k));
+        found[1] = need - before;
+        found[2] = part[k];
+      }
+      before += part[k];
+    }
+  }
+  __syncthreads();
+}
+
+// grid (B * T * Hkv), up to 256 KEYS pages: one row's `count` best pages, in their order.  A thread's keys stay in its registers, key k that of
+// page 256 k + thread.  One histogram over their range leaves few keys beside the one looked for, as a rule; these are ranked by comparing each with all.
+// What is taken is written by its rank among the taken: their number in front of each set of 64 pages, and the lanes in front.
+template <int KEYS>
+__global__ __launch_bounds__(kChooseThreads) void kv4_choose_kernel(SelectArgs p) {
+  constexpr int kList = 64;                            // keys that are ranked by comparing
+  __shared__ __align__(16) uint32_t bins[kChooseBins];
+  __shared__ uint32_t waves[4], found[4], tops[12], list_key[kList], list_page[kList], sets[KEYS * 4];
+  const int row = blockIdx.x / p.kv.Hkv, b = row / p.kv.T, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int n = pages_in_sight(p.kv, b, row - b * p.kv.T);
+  int32_t* const out = p.pages + (size_t)blockIdx.x * p.count;
+  if (n <= p.count) {
+    for (int i = tid; i < p.count; i += kChooseThreads) out[i] = i < n ? i : -1;
+    return;
+  }
+  const uint32_t* const keys = p.keys + (size_t)blockIdx.x * p.pitch;
+  uint32_t key[KEYS];
+#pragma unroll
+  for (int k = 0; k < KEYS; ++k) key[k] = 256 * k + tid < n ? keys[256 * k + tid] : 0u;
+#pragma unroll
+  for (int i = 0; i < kChooseBins / kChooseThreads; ++i) bins[i * kChooseThreads + tid] = 0u;
+  uint32_t least = 0xFFFFFFFFu, most = 0u, odd = 0u, taken = 0u;      // taken: a bit a key
+#pragma unroll
+  for (int k = 0; k < KEYS; ++k) {
+    const int i = 256 * k + tid;
+    const bool forced = i < p.first || i >= n - p.last, there = i < n;
+    taken |= there && forced ? 1u << k : 0u;
+    const uint32_t own = there && !forced ? key[k] : 0u;
+    odd += own == kKeyOdd ? 1u : 0u;
+    least = min(least, there && !forced ? own : 0xFFFFFFFFu);
+    most = max(most, own < kKeyOdd ? own : 0u);
+  }
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    least = min(least, (uint32_t)__shfl_xor((int)least, d));
+    most = max(most, (uint32_t)__shfl_xor((int)most, d));
+    odd += (uint32_t)__shfl_xor((int)odd, d);
+  }
+  if (lane == 0) { tops[wave] = least; tops[4 + wave] = most; tops[8 + wave] = odd; }
+  if (tid == 0) found[3] = 0u;
+  __syncthreads();
+  least = min(min(tops[0], tops[1]), min(tops[2], tops[3]));
+  most = max(max(tops[4], tops[5]), max(tops[6], tops[7]));
+  odd = tops[8] + tops[9] + tops[10] + tops[11];
+  // The keys that may be taken: neither forced ones nor absent ones.  key >= low and < low + 2^width hold the need-th; larger ones are taken.
+  uint32_t low = kKeyOdd, need = (uint32_t)(p.count - p.first - p.last), inside = odd;
+  int width = 0;
+  const auto open = [&](int k) { return 256 * k + tid < n && !(taken >> k & 1u); };
+  if (odd < need) {
+    need -= odd;
+    low = least;
+    width = 32 - __builtin_clz(max(most - least, 1u));
+    inside = 0xFFFFFFFFu;
+    while (width > 0 && inside > (uint32_t)kList && inside != need) {
+      const int shift = max(width - 11, 0);
+      if (inside != 0xFFFFFFFFu) {                     // (the bins are clear the first time)
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < kChooseBins / kChooseThreads; ++i) bins[i * kChooseThreads + tid] = 0u;
+        __syncthreads();
+      }
+#pragma unroll
+      for (int k = 0; k < KEYS; ++k) {
+        if (!open(k) || key[k] < low || key[k] > most) continue;
+        const uint32_t part = (key[k] - low) >> shift;
+        if (part < 1u << (width - shift)) atomicAdd(&bins[part], 1u);
+      }
+      __syncthreads();
+      find_part(bins, waves, found, need);
+      low += found[0] << shift;
+      need = found[1];
+      inside = found[2];
+      width = shift;
+    }
+  }
+  // keys from low on that are inside: all of them taken (as many as are needed), equal to each other (width 0: the first of them), or few
+  const uint32_t high = width < 32 ? low + (1u << width) - 1u : 0xFFFFFFFFu;      // (no range reaches past the largest number)
+  const bool whole = inside == need, ranked = !whole && width > 0;
+  uint32_t ties = 0u;
+#pragma unroll
+  for (int k = 0; k < KEYS; ++k) {
+    if (!open(k) || need == 0) continue;
+    const bool in = key[k] >= low && key[k] <= high;
+    taken |= key[k] > high || (in && whole) ? 1u << k : 0u;
+    ties |= in && !whole ? 1u << k : 0u;
+  }
+  if (ranked) {
+#pragma unroll
+    for (int k = 0; k < KEYS; ++k) {
+      if (!(ties >> k & 1u)) continue;
+      const uint32_t at = atomicAdd(&found[3], 1u);
+      list_key[at] = key[k];
+      list_page[at] = (uint32_t)(256 * k + tid);
+    }
+    __syncthreads();
+    const uint32_t listed = found[3];
+#pragma unroll
+    for (int k = 0; k < KEYS; ++k) {
+      if (!(ties >> k & 1u)) continue;
+      uint32_t rank = 0;
+      for (uint32_t i = 0; i < listed; ++i)
+        rank += list_key[i] > key[k] || (list_key[i] == key[k] && list_page[i] < (uint32_t)(256 * k + tid)) ? 1u : 0u;
+      taken |= rank < need ? 1u << k : 0u;
+    }
+    ties = 0u;
+  }
+  // ---- by rank: taken ones in the lower half of a word, ties in the upper
+#pragma unroll
+  for (int k = 0; k < KEYS; ++k) {
+    const uint64_t a = __builtin_amdgcn_ballot_w64(taken >> k & 1u), t = __builtin_amdgcn_ballot_w64(ties >> k & 1u);
+    if (lane == 0) sets[4 * k + wave] = (uint32_t)__builtin_popcountll(a) | (uint32_t)__builtin_popcountll(t) << 16;
+  }
+  __syncthreads();
+  constexpr int EACH = (KEYS * 4 + 63) / 64;           // sets of 64 pages a lane
+  uint32_t mine[EACH], upto = 0;
+#pragma unroll
+  for (int i = 0; i < EACH; ++i) {
+    mine[i] = lane * EACH + i < KEYS * 4 ? sets[lane * EACH + i] : 0u;
+    upto += mine[i];
+  }
+  uint32_t before = upto;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const uint32_t other = __shfl_up(before, d);
+    before += lane >= d ? other : 0u;
+  }
+  before -= upto;
+#pragma unroll
+  for (int k = 0; k < KEYS; ++k) {
+    const int set = 4 * k + wave;
+    uint32_t in_front = (uint32_t)__shfl((int)before, set / EACH);
+#pragma unroll
+    for (int i = 0; i + 1 < EACH; ++i) in_front += i < set % EACH ? (uint32_t)__shfl((int)mine[i], set / EACH) : 0u;
+    const uint64_t a = __builtin_amdgcn_ballot_w64(taken >> k & 1u), t = __builtin_amdgcn_ballot_w64(ties >> k & 1u), lower = (1ull << lane) - 1;
+    const uint32_t taken_before = (in_front & 0xFFFFu) + (uint32_t)__builtin_popcountll(a & lower), ties_before = (in_front >> 16) + (uint32_t)__builtin_popcountll(t & lower);
+    const bool tie = (ties >> k & 1u) && ties_before < need;
+    if ((taken >> k & 1u) || tie) out[taken_before + min(ties_before, need)] = 256 * k + tid;
+  }
+}
+
+// grid (B * T * Hkv), any number of pages: one row's `count` best pages, in their order.  The key that the last of them has is found by histograms over the range
 // that is left, 2048 parts of it at a time; the pages with larger keys, and as many of those with that key as there is room for, are
 // written by their rank.
-__global__ __launch_bounds__(kChooseThreads) void kv4_choose_kernel(SelectArgs p) {
-  __shared__ __align__(16) uint32_t held[kChooseKeys];
-  __shared__ uint32_t bins[kChooseBins], waves[4], found[3];
+__global__ __launch_bounds__(kChooseThreads) void kv4_choose_many_kernel(SelectArgs p) {
+  __shared__ __align__(16) uint32_t bins[kChooseBins];
+  __shared__ uint32_t waves[4], found[3];
   const int row = blockIdx.x / p.kv.Hkv, b = row / p.kv.T, tid = threadIdx.x;
   const int n = pages_in_sight(p.kv, b, row - b * p.kv.T);
   int32_t* const out = p.pages + (size_t)blockIdx.x * p.count;
@@ -328,11 +520,9 @@ __global__ __launch_bounds__(kChooseThreads) void kv4_choose_kernel(SelectArgs p
   }
   const uint32_t* const keys = p.keys + (size_t)blockIdx.x * p.pitch;
   const auto fetch = [&](int i) { return i < p.first || i >= n - p.last ? kKeyForced : keys[i]; };
-  const bool fits = n <= kChooseKeys;
   uint32_t least = 0xFFFFFFFFu, most = 0u, odd = 0u;
   for (int i = tid; i < n; i += kChooseThreads) {
     const uint32_t key = fetch(i);
-    if (fits) held[i] = key;
     least = min(least, key);
     most = max(most, key < kKeyOdd ? key : 0u);
     odd += key == kKeyOdd ? 1u : 0u;
@@ -348,7 +538,6 @@ __global__ __launch_bounds__(kChooseThreads) void kv4_choose_kernel(SelectArgs p
   least = min(min(waves[0], waves[1]), min(waves[2], waves[3]));
   most = max(max(bins[0], bins[1]), max(bins[2], bins[3]));
   odd = bins[4] + bins[5] + bins[6] + bins[7];
-  const auto key_at = [&](int i) { return fits ? held[i] : fetch(i); };
   // The key looked for is the need-th from the top of low .. low + 2^width - 1; larger ones are taken.  whole: all from low on are.
   const uint32_t forced = (uint32_t)(p.first + p.last), count = (uint32_t)p.count;       // (fewer than n)
   uint32_t low = kKeyOdd, need = count - forced;
@@ -366,28 +555,13 @@ __global__ __launch_bounds__(kChooseThreads) void kv4_choose_kernel(SelectArgs p
       for (int i = tid; i < kChooseBins; i += kChooseThreads) bins[i] = 0u;
       __syncthreads();
       for (int i = tid; i < n; i += kChooseThreads) {
-        const uint32_t key = key_at(i);
+        const uint32_t key = fetch(i);
         if (key < low || key > most) continue;
         const uint32_t part = (key - low) >> shift;
         if (part < 1u << (width - shift)) atomicAdd(&bins[part], 1u);
       }
       __syncthreads();
-      uint32_t mine = 0, all;                          // a thread's 8 parts, from the top
-#pragma unroll
-      for (int k = 0; k < 8; ++k) mine += bins[kChooseBins - 1 - (8 * tid + k)];
-      uint32_t before = scan_before(mine, waves, all);
-      if (before < need && before + mine >= need) {
-        for (int k = 0; k < 8; ++k) {
-          const uint32_t part = (uint32_t)(kChooseBins - 1 - (8 * tid + k)), c = bins[part];
-          if (before < need && before + c >= need) {
-            found[0] = part;
-            found[1] = need - before;
-            found[2] = c;
-          }
-          before += c;
-        }
-      }
-      __syncthreads();
+      find_part(bins, waves, found, need);
       low += found[0] << shift;
       need = found[1];
       whole = found[2] == need;
@@ -398,14 +572,14 @@ __global__ __launch_bounds__(kChooseThreads) void kv4_choose_kernel(SelectArgs p
   const int per = ((n + kChooseThreads - 1) / kChooseThreads) | 1, begin = min(tid * per, n), end = min(begin + per, n);
   uint32_t larger = 0, equal = 0, all;
   for (int i = begin; i < end; ++i) {
-    const uint32_t key = key_at(i);
+    const uint32_t key = fetch(i);
     larger += key > low || (whole && key == low) ? 1u : 0u;
     equal += !whole && key == low ? 1u : 0u;
   }
   const uint32_t equal_before = scan_before(equal, waves, all);
   uint32_t at = scan_before(larger, waves, all) + min(equal_before, need), room = need - min(equal_before, need);
   for (int i = begin; i < end; ++i) {
-    const uint32_t key = key_at(i);
+    const uint32_t key = fetch(i);
     const bool tie = !whole && key == low && room > 0;
     if (tie) --room;
     if (tie || key > low || (whole && key == low)) out[at++] = i;

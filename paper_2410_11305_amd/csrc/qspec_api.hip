@@ -1500,18 +1500,27 @@ int qspec_kv4_select(const void* q_f16, const void* bounds, const int32_t* pos, 
   if ((long long)B * T * Hkv * count * 4 >= 0x7fffffffLL) return QSPEC_ERR_SHAPE;
   if (misaligned(q_f16) || misaligned(bounds) || misaligned(workspace) || misaligned4(pos) || misaligned4(page_table) || misaligned4(pages)) return QSPEC_ERR_ALIGN;
   if (workspace_bytes < qspec_kv4_select_workspace_bytes(B, T, Hq, Hkv, max_pages)) return QSPEC_ERR_WORKSPACE;
-  const int G = Hq / Hkv, queries = G > 16 ? 1 : 16 / G;        // of a block of columns
-  const long long sets = (long long)B * ((T + queries - 1) / queries);
-  if (sets * Hkv > 0x7fffffffLL) return QSPEC_ERR_SHAPE;
+  // a query's heads take 2^width columns of a block, or several blocks
+  const int G = Hq / Hkv, width = G > 8 ? 4 : G > 4 ? 3 : G > 2 ? 2 : G > 1 ? 1 : 0, per = 16 >> width;
+  const int columns = G > 16 ? (G + 15) / 16 : (T + per - 1) / per < kScoreColumns ? (T + per - 1) / per : kScoreColumns;
+  const int queries = G > 16 ? 1 : per * columns;
+  const long long sets = (T + queries - 1) / queries, rows = (long long)B * sets * Hkv;
   if (int st = check_device()) return st;
   SelectArgs a{kv_shape(pos, page_table, T, Hkv, page_size, max_pages, n_pages), static_cast<const uint16_t*>(q_f16), static_cast<const uint8_t*>(bounds),
-               static_cast<uint32_t*>(workspace), pages, Hq, G, queries, (T + queries - 1) / queries, first, last, count, select_row_keys(max_pages)};
+               static_cast<uint32_t*>(workspace), pages, Hq, G, width, columns, queries, (int)sets, first, last, count, select_row_keys(max_pages)};
   const hipStream_t s = static_cast<hipStream_t>(stream);
-  const unsigned chunks = blocks_for((size_t)max_pages, 64);
-  const dim3 grid((unsigned)(sets * Hkv), chunks < 65535u ? chunks : 65535u);
-  if (D == 128) launch_kernel(kv4_score_kernel<128>, grid, dim3(256), 0, s, a);
-  else launch_kernel(kv4_score_kernel<64>, grid, dim3(256), 0, s, a);
-  launch_kernel(kv4_choose_kernel, dim3((unsigned)(B * T * Hkv)), dim3(kChooseThreads), 0, s, a);
+  // 64 pages a workgroup, more where there would be thousands of workgroups
+  unsigned chunks = blocks_for((size_t)max_pages, 64);
+  const unsigned room = (unsigned)(rows < 2048 ? 2048 / rows : 1);
+  if (chunks > room) chunks = room;
+  const size_t lds = (size_t)columns * (D / 32) * 1024;
+  const dim3 grid((unsigned)rows, chunks);
+  if (D == 128) launch_kernel(kv4_score_kernel<128>, grid, dim3(256), lds, s, a);
+  else launch_kernel(kv4_score_kernel<64>, grid, dim3(256), lds, s, a);
+  const dim3 each((unsigned)(B * T * Hkv)), threads(kChooseThreads);
+  if (max_pages <= 8 * kChooseThreads) launch_kernel(kv4_choose_kernel<8>, each, threads, 0, s, a);
+  else if (max_pages <= 32 * kChooseThreads) launch_kernel(kv4_choose_kernel<32>, each, threads, 0, s, a);
+  else launch_kernel(kv4_choose_many_kernel, each, threads, 0, s, a);
   return launch_status();
 }
 
