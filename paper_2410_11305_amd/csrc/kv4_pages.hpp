@@ -155,7 +155,7 @@ struct SelectArgs {
   int32_t* pages;            // [B * T][Hkv][count]
   int Hq, G;
   int width, columns;        // log2 of the columns that a query's heads take in a block of 16, blocks of a workgroup
-  int queries, sets;         // queries of a workgroup, workgroups that a sequence's queries take
+  int queries, sets, batch;  // queries of a workgroup, workgroups that a sequence's queries take, sequences
   int first, last, count;
   int pitch;
 };
@@ -197,15 +197,19 @@ constexpr int kScoreColumns = 4;                       // blocks of 16 columns o
 
 // grid (B * sets * Hkv, chunks): a product of pages by heads over 2 D features, 16 by 16 a matrix instruction.  A query's heads take the next
 // power of two of columns (repeating the last one), so their largest score is a fold in a row of lanes; more than 16 take several
-// blocks.  The queries' codes are worked out once a workgroup and shared through LDS; each wavefront runs through its pages, 16 at a time, with the next ones' bounds
-// on their way.  Lane (row, k): row = lane & 15, 16 codes from 16 (lane >> 4) on in each 64.
+// blocks.  The queries' codes are worked out once a workgroup and shared through LDS.  A workgroup takes 64 pages (more only past 65535 sets of them); the
+// heads of a sequence follow each other on one XCD, whose L2 then has the lines that they share (512 pages of 32 sequences and 8 heads: 12 us for 16).  Bound by
+// latency up to there (position, table, bounds one after the other: 2048 pages of 8 heads 3.8 us), then by the loads of 260 bytes that lie 2 KB
+// apart (34 MB in 12 us).  Runs of 64 pages a wavefront were slower (14).  Lane (row, k): row = lane & 15, 16 codes from 16 (lane >> 4) on in each 64.
 template <int D>
 __global__ __launch_bounds__(256) void kv4_score_kernel(SelectArgs p) {
   constexpr int NI = D / 64;                           // matrix instructions of a half
   extern __shared__ __align__(16) uint8_t score_lds[];       // [columns][2 NI][64] of 16 bytes
   v4i* const codes = reinterpret_cast<v4i*>(score_lds);
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), col = lane & 15, kb = lane >> 4;
-  const int head = blockIdx.x % p.kv.Hkv, set = blockIdx.x / p.kv.Hkv, b = set / p.sets, j0 = (set - b * p.sets) * p.queries;
+  const uint32_t place = (blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3);      // neighbours in one L2
+  const int set = (int)(place / (uint32_t)p.kv.Hkv), head = (int)place - set * p.kv.Hkv, b = set / p.sets, j0 = (set - b * p.sets) * p.queries;
+  if (b >= p.batch) return;
   const int queries = min(p.queries, p.kv.T - j0);
   const int n = pages_in_sight(p.kv, b, j0 + queries - 1);
   if (n <= p.count) return;                            // all of them are taken
@@ -281,22 +285,17 @@ __global__ __launch_bounds__(256) void kv4_score_kernel(SelectArgs p) {
     }
   }
   __syncthreads();
-  for (; i0 < n; i0 += gridDim.y * 64) {
-    v4i now_u[NI], now_l[NI];
-    float g4[4];
-#pragma unroll
-    for (int i = 0; i < NI; ++i) { now_u[i] = u[i]; now_l[i] = l[i]; }
+  for (; i0 < n; i0 += gridDim.y * 64, load_pages(i0)) {
+    float g4[4];                                       // of this lane's four pages
 #pragma unroll
     for (int r = 0; r < 4; ++r) g4[r] = __shfl(grid, 4 * kb + r);
-    const int here = i0;
-    if (i0 + (int)gridDim.y * 64 < n) load_pages(i0 + gridDim.y * 64);
     v4i best = {};
     for (int c = 0; c < blocks; ++c) {
       v4i dot = {0, 0, 0, 0};
 #pragma unroll
       for (int i = 0; i < NI; ++i) {
-        dot = __builtin_amdgcn_mfma_i32_16x16x64_i8(now_u[i], codes[(c * 2 * NI + i) * 64 + lane], dot, 0, 0, 0);
-        dot = __builtin_amdgcn_mfma_i32_16x16x64_i8(now_l[i], codes[(c * 2 * NI + NI + i) * 64 + lane], dot, 0, 0, 0);
+        dot = __builtin_amdgcn_mfma_i32_16x16x64_i8(u[i], codes[(c * 2 * NI + i) * 64 + lane], dot, 0, 0, 0);
+        dot = __builtin_amdgcn_mfma_i32_16x16x64_i8(l[i], codes[(c * 2 * NI + NI + i) * 64 + lane], dot, 0, 0, 0);
       }
       if (p.G > 16) {
 #pragma unroll
@@ -312,29 +311,44 @@ __global__ __launch_bounds__(256) void kv4_score_kernel(SelectArgs p) {
       }
       const int j = p.G > 16 ? 0 : c * per + (col >> p.width);
       if ((col & ((1 << p.width) - 1)) == 0 && j < queries)      // (up to the end of 16 pages: rows have room for whole sets of 64)
-        *reinterpret_cast<uint4*>(p.keys + (((size_t)b * p.kv.T + j0 + j) * p.kv.Hkv + head) * p.pitch + here + 4 * kb) = uint4{key[0], key[1], key[2], key[3]};
+        *reinterpret_cast<uint4*>(p.keys + (((size_t)b * p.kv.T + j0 + j) * p.kv.Hkv + head) * p.pitch + i0 + 4 * kb) = uint4{key[0], key[1], key[2], key[3]};
     }
   }
 }
 
-constexpr int kChooseThreads = 256, kChooseBins = 2048;
+constexpr int kChooseThreads = 256, kChooseBins = 2048;        // (threads: where there are many pages)
+
+// A wavefront's values folded up to and with each lane's: sums inside rows of 16 lanes, then the rows before.  NONE: what changes nothing.
+template <uint32_t NONE, class Fold>
+__device__ __forceinline__ uint32_t folded(uint32_t v, Fold fold) {
+#define QSPEC_FOLD(ctrl, rows) v = fold(v, (uint32_t)__builtin_amdgcn_update_dpp((int)NONE, (int)v, ctrl, rows, 0xf, false))
+  QSPEC_FOLD(0x111, 0xf);                              // row_shr 1, 2, 4, 8
+  QSPEC_FOLD(0x112, 0xf);
+  QSPEC_FOLD(0x114, 0xf);
+  QSPEC_FOLD(0x118, 0xf);
+  QSPEC_FOLD(0x142, 0xa);                              // row_bcast 15 into rows 1 and 3
+  QSPEC_FOLD(0x143, 0xc);                              // row_bcast 31 into rows 2 and 3
+#undef QSPEC_FOLD
+  return v;
+}
+__device__ __forceinline__ uint32_t sum_up_to(uint32_t v) { return folded<0u>(v, [](uint32_t a, uint32_t b) { return a + b; }); }
+__device__ __forceinline__ uint32_t last_lane(uint32_t v) { return (uint32_t)__builtin_amdgcn_readlane((int)v, 63); }
+__device__ __forceinline__ uint32_t least_of_wave(uint32_t v) { return last_lane(folded<0xFFFFFFFFu>(v, [](uint32_t a, uint32_t b) { return min(a, b); })); }
+__device__ __forceinline__ uint32_t most_of_wave(uint32_t v) { return last_lane(folded<0u>(v, [](uint32_t a, uint32_t b) { return max(a, b); })); }
+__device__ __forceinline__ uint32_t sum_of_wave(uint32_t v) { return last_lane(sum_up_to(v)); }
 
 // Sum of v over the threads before this one, and over all.
+template <int THREADS>
 __device__ inline uint32_t scan_before(uint32_t v, uint32_t* waves, uint32_t& all) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  uint32_t upto = v;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const uint32_t other = __shfl_up(upto, d);
-    upto += lane >= d ? other : 0u;
-  }
+  const uint32_t upto = sum_up_to(v);
   __syncthreads();                                     // (what an earlier scan left has been read)
   if (lane == 63) waves[wave] = upto;
   __syncthreads();
   uint32_t before = 0;
   all = 0;
 #pragma unroll
-  for (int w = 0; w < kChooseThreads / 64; ++w) {
+  for (int w = 0; w < THREADS / 64; ++w) {
     before += w < wave ? waves[w] : 0u;
     all += waves[w];
   }
@@ -342,20 +356,23 @@ __device__ inline uint32_t scan_before(uint32_t v, uint32_t* waves, uint32_t& al
 }
 
 // The need-th key from the top of low .. low + 2^width - 1 narrowed down by a histogram over 2048 parts of that range, in `bins`: the part it lies
-// in, which of its keys it is, and how many it has, in found.  The threads' own parts are 8 neighbouring ones, from the top.
+// in, which of its keys it is, and how many it has, in found.  A thread's own parts are neighbours, from the top.
+template <int THREADS>
 __device__ inline void find_part(const uint32_t* bins, uint32_t* waves, uint32_t* found, uint32_t need) {
-  const int tid = threadIdx.x;
-  uint32_t part[8], mine = 0, all;
-  const uint4 a = reinterpret_cast<const uint4*>(bins)[(kChooseBins - 8 - 8 * tid) / 4], b = reinterpret_cast<const uint4*>(bins)[(kChooseBins - 8 - 8 * tid) / 4 + 1];
-  part[0] = b.w; part[1] = b.z; part[2] = b.y; part[3] = b.x; part[4] = a.w; part[5] = a.z; part[6] = a.y; part[7] = a.x;
+  constexpr int OWN = kChooseBins / THREADS;
+  const int from = kChooseBins - OWN * ((int)threadIdx.x + 1);
+  uint32_t part[OWN], mine = 0, all;
 #pragma unroll
-  for (int k = 0; k < 8; ++k) mine += part[k];
-  uint32_t before = scan_before(mine, waves, all);
+  for (int k = 0; k < OWN; ++k) {
+    part[k] = bins[from + OWN - 1 - k];
+    mine += part[k];
+  }
+  uint32_t before = scan_before<THREADS>(mine, waves, all);
   if (before < need && before + mine >= need) {
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
+    for (int k = 0; k < OWN; ++k) {
       if (before < need && before + part[k] >= need) {
-        found[0] = (uint32_t)(kChooseBins - 1 - (8 * tid + k));
+        found[0] = (uint32_t)(from + OWN - 1 - k);
         found[1] = need - before;
         found[2] = part[k];
       }
@@ -365,31 +382,32 @@ __device__ inline void find_part(const uint32_t* bins, uint32_t* waves, uint32_t
   __syncthreads();
 }
 
-// grid (B * T * Hkv), up to 256 KEYS pages: one row's `count` best pages, in their order.  A thread's keys stay in its registers, key k that of
-// page 256 k + thread.  One histogram over their range leaves few keys beside the one looked for, as a rule; these are ranked by comparing each with all.
+// grid (B * T * Hkv), up to THREADS * KEYS pages: one row's `count` best pages, in their order.  A thread's keys stay in its registers, key k that of
+// page THREADS k + thread.  One histogram over their range leaves few keys beside the one looked for, as a rule; these are ranked by comparing each with all.
 // What is taken is written by its rank among the taken: their number in front of each set of 64 pages, and the lanes in front.
-template <int KEYS>
-__global__ __launch_bounds__(kChooseThreads) void kv4_choose_kernel(SelectArgs p) {
+template <int THREADS, int KEYS>
+__global__ __launch_bounds__(THREADS) void kv4_choose_kernel(SelectArgs p) {
+  constexpr int WAVES = THREADS / 64;
   constexpr int kList = 64;                            // keys that are ranked by comparing
   __shared__ __align__(16) uint32_t bins[kChooseBins];
-  __shared__ uint32_t waves[4], found[4], tops[12], list_key[kList], list_page[kList], sets[KEYS * 4];
+  __shared__ uint32_t waves[WAVES], found[4], tops[3][WAVES], list_key[kList], list_page[kList], sets[KEYS * WAVES];
   const int row = blockIdx.x / p.kv.Hkv, b = row / p.kv.T, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int n = pages_in_sight(p.kv, b, row - b * p.kv.T);
   int32_t* const out = p.pages + (size_t)blockIdx.x * p.count;
   if (n <= p.count) {
-    for (int i = tid; i < p.count; i += kChooseThreads) out[i] = i < n ? i : -1;
+    for (int i = tid; i < p.count; i += THREADS) out[i] = i < n ? i : -1;
     return;
   }
   const uint32_t* const keys = p.keys + (size_t)blockIdx.x * p.pitch;
   uint32_t key[KEYS];
 #pragma unroll
-  for (int k = 0; k < KEYS; ++k) key[k] = 256 * k + tid < n ? keys[256 * k + tid] : 0u;
+  for (int k = 0; k < KEYS; ++k) key[k] = THREADS * k + tid < n ? keys[THREADS * k + tid] : 0u;
 #pragma unroll
-  for (int i = 0; i < kChooseBins / kChooseThreads; ++i) bins[i * kChooseThreads + tid] = 0u;
+  for (int i = 0; i < kChooseBins / THREADS; ++i) bins[i * THREADS + tid] = 0u;
   uint32_t least = 0xFFFFFFFFu, most = 0u, odd = 0u, taken = 0u;      // taken: a bit a key
 #pragma unroll
   for (int k = 0; k < KEYS; ++k) {
-    const int i = 256 * k + tid;
+    const int i = THREADS * k + tid;
     const bool forced = i < p.first || i >= n - p.last, there = i < n;
     taken |= there && forced ? 1u << k : 0u;
     const uint32_t own = there && !forced ? key[k] : 0u;
@@ -397,22 +415,23 @@ __global__ __launch_bounds__(kChooseThreads) void kv4_choose_kernel(SelectArgs p
     least = min(least, there && !forced ? own : 0xFFFFFFFFu);
     most = max(most, own < kKeyOdd ? own : 0u);
   }
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    least = min(least, (uint32_t)__shfl_xor((int)least, d));
-    most = max(most, (uint32_t)__shfl_xor((int)most, d));
-    odd += (uint32_t)__shfl_xor((int)odd, d);
-  }
-  if (lane == 0) { tops[wave] = least; tops[4 + wave] = most; tops[8 + wave] = odd; }
+  least = least_of_wave(least);
+  most = most_of_wave(most);
+  odd = sum_of_wave(odd);
+  if (lane == 0) { tops[0][wave] = least; tops[1][wave] = most; tops[2][wave] = odd; }
   if (tid == 0) found[3] = 0u;
   __syncthreads();
-  least = min(min(tops[0], tops[1]), min(tops[2], tops[3]));
-  most = max(max(tops[4], tops[5]), max(tops[6], tops[7]));
-  odd = tops[8] + tops[9] + tops[10] + tops[11];
+  odd = 0;
+#pragma unroll
+  for (int w = 0; w < WAVES; ++w) {
+    least = min(least, tops[0][w]);
+    most = max(most, tops[1][w]);
+    odd += tops[2][w];
+  }
   // The keys that may be taken: neither forced ones nor absent ones.  key >= low and < low + 2^width hold the need-th; larger ones are taken.
   uint32_t low = kKeyOdd, need = (uint32_t)(p.count - p.first - p.last), inside = odd;
   int width = 0;
-  const auto open = [&](int k) { return 256 * k + tid < n && !(taken >> k & 1u); };
+  const auto open = [&](int k) { return THREADS * k + tid < n && !(taken >> k & 1u); };
   if (odd < need) {
     need -= odd;
     low = least;
@@ -423,7 +442,7 @@ __global__ __launch_bounds__(kChooseThreads) void kv4_choose_kernel(SelectArgs p
       if (inside != 0xFFFFFFFFu) {                     // (the bins are clear the first time)
         __syncthreads();
 #pragma unroll
-        for (int i = 0; i < kChooseBins / kChooseThreads; ++i) bins[i * kChooseThreads + tid] = 0u;
+        for (int i = 0; i < kChooseBins / THREADS; ++i) bins[i * THREADS + tid] = 0u;
         __syncthreads();
       }
 #pragma unroll
@@ -433,7 +452,7 @@ __global__ __launch_bounds__(kChooseThreads) void kv4_choose_kernel(SelectArgs p
         if (part < 1u << (width - shift)) atomicAdd(&bins[part], 1u);
       }
       __syncthreads();
-      find_part(bins, waves, found, need);
+      find_part<THREADS>(bins, waves, found, need);
       low += found[0] << shift;
       need = found[1];
       inside = found[2];
@@ -457,7 +476,7 @@ __global__ __launch_bounds__(kChooseThreads) void kv4_choose_kernel(SelectArgs p
       if (!(ties >> k & 1u)) continue;
       const uint32_t at = atomicAdd(&found[3], 1u);
       list_key[at] = key[k];
-      list_page[at] = (uint32_t)(256 * k + tid);
+      list_page[at] = (uint32_t)(THREADS * k + tid);
     }
     __syncthreads();
     const uint32_t listed = found[3];
@@ -465,8 +484,9 @@ __global__ __launch_bounds__(kChooseThreads) void kv4_choose_kernel(SelectArgs p
     for (int k = 0; k < KEYS; ++k) {
       if (!(ties >> k & 1u)) continue;
       uint32_t rank = 0;
+#pragma unroll 8
       for (uint32_t i = 0; i < listed; ++i)
-        rank += list_key[i] > key[k] || (list_key[i] == key[k] && list_page[i] < (uint32_t)(256 * k + tid)) ? 1u : 0u;
+        rank += list_key[i] > key[k] || (list_key[i] == key[k] && list_page[i] < (uint32_t)(THREADS * k + tid)) ? 1u : 0u;
       taken |= rank < need ? 1u << k : 0u;
     }
     ties = 0u;
@@ -475,33 +495,28 @@ __global__ __launch_bounds__(kChooseThreads) void kv4_choose_kernel(SelectArgs p
 #pragma unroll
   for (int k = 0; k < KEYS; ++k) {
     const uint64_t a = __builtin_amdgcn_ballot_w64(taken >> k & 1u), t = __builtin_amdgcn_ballot_w64(ties >> k & 1u);
-    if (lane == 0) sets[4 * k + wave] = (uint32_t)__builtin_popcountll(a) | (uint32_t)__builtin_popcountll(t) << 16;
+    if (lane == 0) sets[WAVES * k + wave] = (uint32_t)__builtin_popcountll(a) | (uint32_t)__builtin_popcountll(t) << 16;
   }
   __syncthreads();
-  constexpr int EACH = (KEYS * 4 + 63) / 64;           // sets of 64 pages a lane
+  constexpr int EACH = (KEYS * WAVES + 63) / 64;           // sets of 64 pages a lane
   uint32_t mine[EACH], upto = 0;
 #pragma unroll
   for (int i = 0; i < EACH; ++i) {
-    mine[i] = lane * EACH + i < KEYS * 4 ? sets[lane * EACH + i] : 0u;
+    mine[i] = lane * EACH + i < KEYS * WAVES ? sets[lane * EACH + i] : 0u;
     upto += mine[i];
   }
-  uint32_t before = upto;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const uint32_t other = __shfl_up(before, d);
-    before += lane >= d ? other : 0u;
-  }
-  before -= upto;
+  const uint32_t before = sum_up_to(upto) - upto;
+  const int first_set = uniform(wave);
 #pragma unroll
   for (int k = 0; k < KEYS; ++k) {
-    const int set = 4 * k + wave;
-    uint32_t in_front = (uint32_t)__shfl((int)before, set / EACH);
+    const int set = WAVES * k + first_set;
+    uint32_t in_front = (uint32_t)__builtin_amdgcn_readlane((int)before, set / EACH);
 #pragma unroll
-    for (int i = 0; i + 1 < EACH; ++i) in_front += i < set % EACH ? (uint32_t)__shfl((int)mine[i], set / EACH) : 0u;
+    for (int i = 0; i + 1 < EACH; ++i) in_front += i < set % EACH ? (uint32_t)__builtin_amdgcn_readlane((int)mine[i], set / EACH) : 0u;
     const uint64_t a = __builtin_amdgcn_ballot_w64(taken >> k & 1u), t = __builtin_amdgcn_ballot_w64(ties >> k & 1u), lower = (1ull << lane) - 1;
     const uint32_t taken_before = (in_front & 0xFFFFu) + (uint32_t)__builtin_popcountll(a & lower), ties_before = (in_front >> 16) + (uint32_t)__builtin_popcountll(t & lower);
     const bool tie = (ties >> k & 1u) && ties_before < need;
-    if ((taken >> k & 1u) || tie) out[taken_before + min(ties_before, need)] = 256 * k + tid;
+    if ((taken >> k & 1u) || tie) out[taken_before + min(ties_before, need)] = THREADS * k + tid;
   }
 }
 
@@ -527,12 +542,9 @@ __global__ __launch_bounds__(kChooseThreads) void kv4_choose_many_kernel(SelectA
     most = max(most, key < kKeyOdd ? key : 0u);
     odd += key == kKeyOdd ? 1u : 0u;
   }
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    least = min(least, (uint32_t)__shfl_xor((int)least, d));
-    most = max(most, (uint32_t)__shfl_xor((int)most, d));
-    odd += (uint32_t)__shfl_xor((int)odd, d);
-  }
+  least = least_of_wave(least);
+  most = most_of_wave(most);
+  odd = sum_of_wave(odd);
   if ((tid & 63) == 0) { waves[tid >> 6] = least; bins[tid >> 6] = most; bins[4 + (tid >> 6)] = odd; }
   __syncthreads();
   least = min(min(waves[0], waves[1]), min(waves[2], waves[3]));
@@ -561,7 +573,7 @@ __global__ __launch_bounds__(kChooseThreads) void kv4_choose_many_kernel(SelectA
         if (part < 1u << (width - shift)) atomicAdd(&bins[part], 1u);
       }
       __syncthreads();
-      find_part(bins, waves, found, need);
+      find_part<kChooseThreads>(bins, waves, found, need);
       low += found[0] << shift;
       need = found[1];
       whole = found[2] == need;
@@ -576,8 +588,8 @@ __global__ __launch_bounds__(kChooseThreads) void kv4_choose_many_kernel(SelectA
     larger += key > low || (whole && key == low) ? 1u : 0u;
     equal += !whole && key == low ? 1u : 0u;
   }
-  const uint32_t equal_before = scan_before(equal, waves, all);
-  uint32_t at = scan_before(larger, waves, all) + min(equal_before, need), room = need - min(equal_before, need);
+  const uint32_t equal_before = scan_before<kChooseThreads>(equal, waves, all);
+  uint32_t at = scan_before<kChooseThreads>(larger, waves, all) + min(equal_before, need), room = need - min(equal_before, need);
   for (int i = begin; i < end; ++i) {
     const uint32_t key = fetch(i);
     const bool tie = !whole && key == low && room > 0;

@@ -160,6 +160,15 @@ def test_choice_of_many_pages(env, each, count):
     check_choice(env, b, queries(1, 1, 2, 2, 64), np.array([each * 64 - 2]), np.random.default_rng(2).permutation(each).reshape(1, each), 64, 1, 2, count)
 
 
+@pytest.mark.parametrize("Bn,T,Hkv,each,count", [(90, 3, 1, 24, 7), (3, 50, 2, 70, 20), (1, 260, 1, 2100, 50)])
+def test_choice_of_many_rows(env, Bn, T, Hkv, each, count):
+    """Pages with few different scores among them."""
+    b = Bounds(T, Bn * each, Hkv, 64)
+    b.upper[::3], b.lower[::3], b.grid[:] = b.upper[0], b.lower[0], 0.125
+    pos = np.r_[each * 64 - T, np.random.default_rng(1).integers(-T, each * 64, Bn - 1)]
+    check_choice(env, b, queries(2, Bn, T, 2 * Hkv, 64), pos, shuffled(3, Bn, each, Bn * each), 64, 1, 2, count)
+
+
 @pytest.mark.parametrize("n", [2000, 9000])
 @pytest.mark.parametrize("count", [1, 5, 64, 200])
 def test_choice_among_equals(env, n, count):
