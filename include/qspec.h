@@ -413,8 +413,9 @@ int qspec_attn_kv4(const void* q_f16, const void* cache, const int32_t* pos, con
  * may have them.  Rows at positions before shared[g] see the shared tokens up to their own.
  *   shared  int32 [groups], device memory; 0 or less: none.  Held to max_pages * page_size.
  *   (B / groups) * T <= 2^20, and the count of work at qspec_attn_kv4 holds for the groups as sequences of (B / groups) * T rows too.
- *   A row in front of its sequence gets zeros.  Everything else, NaN and limits of scale and scores included, as in qspec_attn_kv4;
- *   two launches, partial sums of the shared tokens in binary32.
+ *   A row in front of its sequence gets zeros.  Everything else, NaN and limits of scale and scores included, as in qspec_attn_kv4.
+ *   Where the table's rows are short (max_pages * page_size tokens) and what one reading for all saves is little, each sequence reads the shared tokens
+ *   for itself in one launch; otherwise there are two, with partial sums of the shared tokens in binary32 between them.
  *   workspace  qspec_attn_kv4_shared_workspace_bytes(...) bytes; the workspace rule at qspec_workspace_bytes holds.
  */
 size_t qspec_attn_kv4_shared_workspace_bytes(int B, int T, int Hq, int Hkv, int D, int groups);

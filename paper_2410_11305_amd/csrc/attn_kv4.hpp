@@ -76,8 +76,8 @@ struct AttnArgs {
 
 // What a launch reads and what becomes of its sums.  kAttnWhole: every token in sight, results.  kAttnPrefix: the tokens that the sequences of a
 // group share, as partial sums of every row; kAttnRest: those behind them, joined with these sums, results.  kAttnPages: the pages
-// that a list names for each row, results.
-enum { kAttnWhole, kAttnPrefix, kAttnRest, kAttnPages };
+// that a list names for each row, results.  kAttnBoth: shared tokens and those behind them of one sequence after the other, results.
+enum { kAttnWhole, kAttnPrefix, kAttnRest, kAttnPages, kAttnBoth };
 
 struct AttnPartArgs : AttnArgs {
   // kAttnPrefix: kv.T and B are the rows of a group and the groups;  kAttnPages: one row each and all rows
@@ -111,7 +111,8 @@ __device__ __forceinline__ int row_group(const AttnPartArgs& p) { return p.group
 __device__ __forceinline__ int row_count(const AttnArgs&) { return 1; }
 __device__ __forceinline__ int row_count(const AttnPartArgs& p) { return p.rows; }
 
-// Where a sequence stands.  at: position of its first row (kAttnPrefix: how many tokens the group shares);  from: its first token (kAttnRest).
+// Where a sequence stands.  at: position of its first row (kAttnPrefix: how many tokens the group shares);  from: the first token of its own
+// (kAttnRest, kAttnBoth).
 struct AttnWhere {
   int at, from;
 };
@@ -143,8 +144,9 @@ __device__ __forceinline__ AttnSpan attn_span(const Args& p, AttnWhere w, int bl
     s.steps = max(min(p.count, pages) * ((1 << p.kv.page_shift) / STEP), 1);
     return s;
   }
-  if constexpr (MODE == kAttnRest) {
+  if constexpr (MODE == kAttnRest || MODE == kAttnBoth) {
     s.first = w.from / STEP;
+    if constexpr (MODE == kAttnBoth) s.sink_steps = max((min(w.from, end) + STEP - 1) / STEP, 0);      // the shared ones in front
   } else {
     s.first = p.window > 0 ? max(behind_window(p, s.lo) + 1, 0) / STEP : 0;
     s.sink_steps = p.window > 0 ? max(min((min(p.sinks, end) + STEP - 1) / STEP, s.first), 0) : 0;
@@ -239,7 +241,7 @@ __device__ __forceinline__ void attn_kv4_work(const Args& p) {
   const auto where_is = [&](int seq, auto load) {        // load(array, index)
     if constexpr (MODE == kAttnPrefix) {
       return AttnWhere{max(load(p.shared, seq), 0), 0};
-    } else if constexpr (MODE == kAttnRest) {
+    } else if constexpr (MODE == kAttnRest || MODE == kAttnBoth) {
       return AttnWhere{load(p.kv.pos, seq), min(max(load(p.shared, seq / p.group), 0), p.kv.max_pages << p.kv.page_shift)};
     } else if constexpr (MODE == kAttnPages) {
       const int b = p.rows == 1 ? seq : seq / p.rows;
@@ -418,9 +420,10 @@ __device__ __forceinline__ void attn_kv4_work(const Args& p) {
         const size_t at_page = (size_t)table_row(b) * p.kv.max_pages + entry;
         return Tile{p.kv.table != nullptr ? p.kv.table[at_page] : (int)at_page, (entry << p.kv.page_shift) + (step - (at << shift)) * STEP};
       }
-      const int i = (first_token(min(s + lane / TILES * WAVES, span.steps - 1)) + lane % TILES * 16) >> p.kv.page_shift;
+      const int step = min(s + lane / TILES * WAVES, span.steps - 1), i = (first_token(step) + lane % TILES * 16) >> p.kv.page_shift;
       if (i >= p.kv.max_pages) return Tile{-1, 0};
-      const size_t at_page = (size_t)table_row(b) * p.kv.max_pages + i;
+      const int row = MODE == kAttnBoth && step < span.sink_steps ? b - b % row_group(p) : table_row(b);
+      const size_t at_page = (size_t)row * p.kv.max_pages + i;
       return Tile{p.kv.table != nullptr ? p.kv.table[at_page] : (int)at_page, 0};
     };
     Tile known = look_up(begin + wave), ahead = Tile{-1, 0};
@@ -578,8 +581,9 @@ __device__ __forceinline__ void attn_kv4_work(const Args& p) {
       const int t_next = token_of(s + WAVES, k);       // (the last one's loads repeat a step)
       const Pages next = pages_of(k);
       // every token of the step in sight of every row
-      const bool whole = pages.there == (1u << TILES) - 1 && t + STEP - 1 <= span.lo &&
-                         (MODE == kAttnRest ? t >= here.from : MODE != kAttnWhole || p.window == 0 || t > behind_window(p, span.hi) || t + STEP <= p.sinks);
+      const bool front = MODE == kAttnBoth && s < span.sink_steps;        // of the shared tokens
+      const bool whole = pages.there == (1u << TILES) - 1 && t + STEP - 1 <= (front ? min(span.lo, here.from - 1) : span.lo) &&
+                         (MODE == kAttnRest || MODE == kAttnBoth ? front || t >= here.from : MODE != kAttnWhole || p.window == 0 || t > behind_window(p, span.hi) || t + STEP <= p.sinks);
       v4f sc[NB][TILES];
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb)
@@ -628,7 +632,8 @@ __device__ __forceinline__ void attn_kv4_work(const Args& p) {
         uint32_t any = 0;                     // bit x: a row of this lane sees its token x
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
-          const int at_row = position(nb), behind = MODE == kAttnRest ? here.from - 1 : MODE == kAttnWhole && p.window > 0 ? behind_window(p, at_row) : -1;
+          const int at_row = front ? min(position(nb), here.from - 1) : position(nb);
+          const int behind = MODE == kAttnRest || (MODE == kAttnBoth && !front) ? here.from - 1 : MODE == kAttnWhole && p.window > 0 ? behind_window(p, at_row) : -1;
 #pragma unroll
           for (int x = 0; x < NX; ++x) {
             const int tok = t + ((x >> 2) * F + mine_tile) * 16 + 4 * kb + (x & 3);

@@ -925,6 +925,21 @@ SharedWorkspace attn_shared_workspace(int B, int T, int Hq, int Hkv, int D, int 
   w.bytes = w.joint + (size_t)B * T * Hq * attn_part_floats(D) * sizeof(float);
   return w;
 }
+// What a token costs an item of an instance where the whole card is busy, in ps (measured, 128 sequences of 4096 and 12288 tokens).
+double attn_token_ps(AttnPlan plan, int D) {
+  static constexpr double ps[2][5] = {{9, 11, 13, 18, 32}, {11.5, 13.7, 18, 23, 39}};
+  return ps[D == 128][plan.f == 4 ? 0 : plan.f == 2 ? 1 : plan.nb == 1 ? 2 : plan.nb == 2 ? 3 : 4];
+}
+// Whether every sequence reads the shared tokens for itself, in one launch, instead of one for all and a second launch: what the first of the two
+// saves at most, with the longest contexts that the tables hold, is less than the second one and its joins cost (8 us and 20 ns an item).  Measured, one launch
+// and two (us): 4 samples of 500 tokens, 32 heads 10.3 and 16.9; 8 users of 2000, 4 rows, 32 heads 24 and 29; 16 prompts of 1500 to 6000 by 8 samples, 4 rows, 64 over 8
+// heads of 64 104 and 121; 128 users, one row of 64 over 8 heads: of 2048 tokens 50 and 54, of 4096 78 and 64, of 8197 147 and 100.
+bool shared_in_one(const AttnPartArgs& first, AttnPlan first_plan, const AttnPartArgs& own, AttnPlan own_plan, int D, long long tokens) {
+  const double alone = (double)own.B * own.blocks * attn_token_ps(own_plan, D), together = (double)first.B * first.blocks * attn_token_ps(first_plan, D);
+  const double items = (double)own.B * own.blocks * own.kv.Hkv;
+  return (alone - together) * own.kv.Hkv * (double)tokens <= 8e6 + 2e4 * items;
+}
+
 int check_attn_shared(int B, int T, int Hq, int Hkv, int D, int groups) {
   if (int st = check_attn(B, T, Hq, Hkv, D)) return st;
   if (groups < 1 || B % groups != 0 || (long long)(B / groups) * T > (1 << 20)) return QSPEC_ERR_SHAPE;
@@ -1404,6 +1419,11 @@ int qspec_attn_kv4_shared(const void* q_f16, const void* cache, const int32_t* p
   if (!attn_counts(first, tokens) || !attn_counts(rest, tokens)) return QSPEC_ERR_SHAPE;
   if (int st = check_device()) return st;
   const hipStream_t s = static_cast<hipStream_t>(stream);
+  if (shared_in_one(first, plan, rest, rest_plan, D, tokens)) {
+    if (D == 128) launch_attn_part<128, kAttnBoth>(rest, rest_plan, s);
+    else launch_attn_part<64, kAttnBoth>(rest, rest_plan, s);
+    return launch_status();
+  }
   if (D == 128) {
     launch_attn_part<128, kAttnPrefix>(first, plan, s);
     launch_attn_part<128, kAttnRest>(rest, rest_plan, s);

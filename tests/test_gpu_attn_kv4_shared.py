@@ -67,6 +67,19 @@ def compare(got, cache, q, pos, table, shared, scale=None, rows=None):
 
 
 def check(env, cache, q, pos, table, shared, scale=None, no_table=False, workspace=None, rows=None, raw=None):
+    """In one launch or two as the library chooses by the length of the table's rows; rows that are long, of which the far pages are not there, take two."""
+    torch, B = env
+    if not no_table and workspace is None and table.shape[1] * cache.P <= 4096:
+        check_one(env, cache, q, pos, far(table, cache.P), shared, scale, False, None, rows, raw, len_=table.shape[1])
+    return check_one(env, cache, q, pos, table, shared, scale, no_table, workspace, rows, raw)
+
+
+def far(table, P):
+    """The table's rows with room for 2^19 tokens, behind their own pages none."""
+    return np.concatenate((table, np.full((len(table), (1 << 19) // P - table.shape[1]), -1)), 1)
+
+
+def check_one(env, cache, q, pos, table, shared, scale=None, no_table=False, workspace=None, rows=None, raw=None, len_=None):
     torch, B = env
     Bn, T, Hq, D = q.shape
     guard = torch.full((q.size + 64,), 123.0, dtype=torch.float16, device="cuda")
@@ -76,7 +89,7 @@ def check(env, cache, q, pos, table, shared, scale=None, no_table=False, workspa
                       cache.Hkv, cache.P, None if no_table else dev(torch, table.astype(np.int32)), scale, out=out, workspace=workspace)
     torch.cuda.synchronize()
     assert (guard[:32] == 123.0).all() and (guard[-32:] == 123.0).all()
-    compare(out.cpu().numpy().astype(np.float64), cache, q, pos, table, shared, scale, rows)
+    compare(out.cpu().numpy().astype(np.float64), cache, q, pos, table[:, :len_], shared, scale, rows)
     return out
 
 
@@ -145,6 +158,11 @@ def test_long_sequences_are_shared_out_and_joined(env, groups, per, T, Hq, Hkv, 
     assert int(ws[:16384].count_nonzero()) == 0
     again = check(*args, workspace=ws, rows=[0])
     assert torch.equal(first, again)
+    args = args[:4] + (far(table, P), shared)                 # in two launches
+    first = check_one(*args, workspace=ws, rows=range(0, Bn, 7), len_=each)
+    assert int(ws[:16384].count_nonzero()) == 0
+    again = check_one(*args, workspace=ws, rows=[0], len_=each)
+    assert torch.equal(first, again)
 
 
 def test_agrees_with_the_attention_of_each_alone(env):
@@ -187,6 +205,8 @@ def test_rows_nobody_sees_may_hold_anything(env, T):
     got = check(env, c, queries(T, 2, T, 3, D), pos, table, shared, raw=bad.bytes())
     torch, _ = env
     assert torch.equal(want, got)
+    args = (env, c, queries(T, 2, T, 3, D), pos, far(table, P), shared)
+    assert torch.equal(check_one(*args, len_=each), check_one(*args, len_=each, raw=bad.bytes()))
 
 
 def test_what_is_no_number_shows_where_it_is_seen(env):
@@ -196,8 +216,13 @@ def test_what_is_no_number_shows_where_it_is_seen(env):
     table = tables(4, 1, 4, each, P, shared, 4 * each)
     c = Cache(11, 4 * each, Hkv, D, P)
     q = queries(3, 4, 1, Hq, D)
-    run = lambda q, c: B.attn_kv4_shared(dev(torch, q), dev(torch, c.bytes()), dev(torch, pos.astype(np.int32)), dev(torch, np.array(shared, np.int32)), Hkv, P,
-                                         dev(torch, table.astype(np.int32))).isnan().cpu().numpy()
+
+    def run(q, c):
+        one, two = (B.attn_kv4_shared(dev(torch, q), dev(torch, c.bytes()), dev(torch, pos.astype(np.int32)), dev(torch, np.array(shared, np.int32)), Hkv, P,
+                                      dev(torch, t.astype(np.int32))).isnan().cpu().numpy() for t in (table, far(table, P)))
+        assert (one == two).all()
+        return one
+
     odd = q.copy()
     odd[1, 0, 2, 5], odd[2, 0, 0, 0] = np.nan, np.inf
     got = run(odd, c)
@@ -219,13 +244,14 @@ def test_what_is_no_number_shows_where_it_is_seen(env):
     assert (got == want).all()
 
 
-def test_two_streams_with_a_workspace_each_and_a_graph(env):
+@pytest.mark.parametrize("long_rows", [False, True])
+def test_two_streams_with_a_workspace_each_and_a_graph(env, long_rows):
     torch, B = env
     groups, per, T, Hq, Hkv, D, P, n = 2, 3, 4, 8, 2, 128, 64, 2500
     Bn, each = groups * per, -(-n // P)
     c = Cache(20, Bn * each, Hkv, D, P)
     table = np.random.default_rng(1).permutation(Bn * each).reshape(Bn, each)
-    cache, tab = dev(torch, c.bytes()), dev(torch, table.astype(np.int32))
+    cache, tab = dev(torch, c.bytes()), dev(torch, (far(table, P) if long_rows else table).astype(np.int32))
     pos = torch.tensor([2400, 2000, 2100, 1000, 1500, 2496], dtype=torch.int32, device="cuda")
     shared = torch.tensor([1999, 1000], dtype=torch.int32, device="cuda")
     size = B.attn_kv4_shared_workspace_bytes(Bn, T, Hq, Hkv, D, groups)
