@@ -92,7 +92,8 @@ struct AttnPartArgs : AttnArgs {
   int first_shift, first_blocks;      // rows of a block of an item (a power of two), blocks of a group
   const int32_t* list;       // [B * rows][Hkv][count]
   int count;
-  int split;                 // log2 of the parts of an item
+  int split;                 // log2 of the parts of an item at most
+  int whole_rounds;          // an item of up to so many rounds of its wavefronts stays whole
 };
 
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
@@ -213,6 +214,8 @@ __device__ __forceinline__ void attn_kv4_work(const Args& p) {
   constexpr int WAVES = W, THREADS = 64 * WAVES, TILES = Form::tiles, STEP = Form::step, RB = Form::rows, OVER = Form::over;
   // (sums that are not joined in this launch cost less: 2048 shared tokens of 1024 rows over 8 heads 39 us for 55)
   constexpr int LEAST = MODE == kAttnWhole || F > 1 ? Form::least : (NB == 4 ? 512 : 256) / STEP;
+  // A workgroup for each part of each item, without a division of the steps: where the host knows how long items are at most.
+  constexpr bool FIXED = MODE == kAttnPages || MODE == kAttnBoth || MODE == kAttnRest;
   constexpr int NK = D / 32;                  // matrix instructions of a tile of q k^T; words of a lane of a key
   constexpr int NV = D / 16;                  // matrix instructions of two tiles of p v
   constexpr int COLS = 16 / F;                // rows of a block of columns
@@ -263,7 +266,7 @@ __device__ __forceinline__ void attn_kv4_work(const Args& p) {
     return (uint32_t)(OVER + attn_span<STEP, MODE>(p, at, e - sequence_of(e) * p.blocks, RB).steps) * (uint32_t)Hkv;
   };
   uint32_t mine = 0;
-  for (int e = lane * per; MODE != kAttnPages && e < min(entries, (lane + 1) * per); ++e) mine += size_of(e, where(sequence_of(e)));
+  for (int e = lane * per; !FIXED && e < min(entries, (lane + 1) * per); ++e) mine += size_of(e, where(sequence_of(e)));
   uint32_t upto = mine;                       // of the entries up to this lane's
 #define QSPEC_DPP_ADD(ctrl, rows) upto += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)upto, ctrl, rows, 0xf, false)
   QSPEC_DPP_ADD(0x111, 0xf);                  // row_shr 1, 2, 4, 8: sums inside a row of 16
@@ -276,7 +279,7 @@ __device__ __forceinline__ void attn_kv4_work(const Args& p) {
   const uint32_t total = (uint32_t)__builtin_amdgcn_readlane((int)upto, 63);
   const uint32_t groups = uniform(min((uint32_t)gridDim.x, max((uint32_t)(entries * Hkv), (total - (uint32_t)(entries * Hkv) * OVER) / LEAST)));
   const uint32_t me = blockIdx.x;
-  if (MODE != kAttnPages && me >= groups) return;
+  if (!FIXED && me >= groups) return;
   // workgroup w begins at w * share, and the first `more` of them take one more each; inside an item it begins a whole
   // number of rounds of its wavefronts in, or with the item in one that is not shared out
   const uint32_t share = uniform(total / groups), more = total - share * groups;
@@ -308,7 +311,7 @@ __device__ __forceinline__ void attn_kv4_work(const Args& p) {
   const uint32_t items = (uint32_t)(entries * Hkv);
   const auto dealt = [&](uint32_t round, uint32_t w) { return round * gridDim.x + (round & 1 ? gridDim.x - 1 - w : w); };
   bool whole_items = false;
-  if (MODE != kAttnPages && items > gridDim.x && items <= kAttnRounds * gridDim.x && (NB == 4 || entries <= THREADS)) {
+  if (!FIXED && items > gridDim.x && items <= kAttnRounds * gridDim.x && (NB == 4 || entries <= THREADS)) {
     // Prompts of one length and history are in order by their blocks; the fullest workgroup is one of the ends, or at the
     // end of the last round.  Few rows: one block, or a few, a sequence, and the lengths are sorted, in the LDS of the sums to come.
     uint32_t* const lengths = reinterpret_cast<uint32_t*>(&o_lds[0][0][0]);
@@ -372,7 +375,7 @@ __device__ __forceinline__ void attn_kv4_work(const Args& p) {
     entry = (int)uniform(i / (uint32_t)Hkv);
     head = (int)(i - (uint32_t)entry * (uint32_t)Hkv);
   };
-  if constexpr (MODE == kAttnPages) {         // lists have a length that the host knows: a workgroup for each part of each item
+  if constexpr (FIXED) {
     item = me >> p.split;
     entry = (int)uniform(item / (uint32_t)Hkv);
     head = (int)(item - (uint32_t)entry * (uint32_t)Hkv);
@@ -393,13 +396,13 @@ __device__ __forceinline__ void attn_kv4_work(const Args& p) {
     span.steps = uniform(span.steps); span.sink_steps = uniform(span.sink_steps); span.first = uniform(span.first);
     span.lo = uniform(span.lo); span.hi = uniform(span.hi);
     int stop = entry == last_entry && head == last_head ? last_step : span.steps;
-    int page_parts = 1;
-    if constexpr (MODE == kAttnPages) {
-      const int rounds = (span.steps + WAVES - 1) / WAVES, each = (rounds + (1 << p.split) - 1) >> p.split;
+    int item_parts = 1;
+    if constexpr (FIXED) {
+      const int rounds = (span.steps + WAVES - 1) / WAVES, each = rounds <= p.whole_rounds ? rounds : (rounds + (1 << p.split) - 1) >> p.split;
       begin = (int)(me - (item << p.split)) * each * WAVES;
       if (begin >= span.steps) return;
       stop = min(span.steps, begin + each * WAVES);
-      page_parts = (span.steps + each * WAVES - 1) / (each * WAVES);
+      item_parts = (span.steps + each * WAVES - 1) / (each * WAVES);
     }
     const int rows = min(RB, R - block * RB);
 
@@ -763,9 +766,9 @@ __device__ __forceinline__ void attn_kv4_work(const Args& p) {
     // ---- the wavefronts' sums, a block of columns at a time
     const bool shared = begin > 0 || stop < span.steps;
     uint32_t w0 = me, w1 = me;                // the workgroups that hold a part of it
-    if constexpr (MODE == kAttnPages) {
+    if constexpr (FIXED) {
       w0 = item << p.split;
-      w1 = w0 + (uint32_t)page_parts - 1;
+      w1 = w0 + (uint32_t)item_parts - 1;
     } else if (shared) {
       w0 = group_of(item + OVER + WAVES - 1);
       w1 = group_of(item + OVER + span.steps - 1);
@@ -887,7 +890,7 @@ __device__ __forceinline__ void attn_kv4_work(const Args& p) {
         if (!shared) {
           write_row(block * RB + r, v, total_l, ref);
         } else {
-          write_part(MODE == kAttnPages ? me : 2 * me + (first_run ? 0 : 1), r, ref, total_l, v);
+          write_part(FIXED ? me : 2 * me + (first_run ? 0 : 1), r, ref, total_l, v);
         }
       }
       __syncthreads();
@@ -896,7 +899,7 @@ __device__ __forceinline__ void attn_kv4_work(const Args& p) {
     // ---- the last of the item's workgroups joins their parts; of many parts, the last of each eight theirs first (a
     // workgroup reads parts past the caches at tens of GB/s: 64 parts of 8 rows in one go take 14 us)
     const uint32_t parts = w1 - w0 + 1;
-    const auto slot_of = [&](uint32_t w) { return MODE == kAttnPages ? w : w == w0 ? 2 * w0 + (start_of(w0) < item ? 1 : 0) : 2 * w; };
+    const auto slot_of = [&](uint32_t w) { return FIXED ? w : w == w0 ? 2 * w0 + (start_of(w0) < item ? 1 : 0) : 2 * w; };
 #pragma unroll 1
     for (int stage = parts > 16 ? 0 : 1; shared && stage < 2; ++stage) {
       if constexpr (MODE == kAttnPrefix) break;
@@ -964,7 +967,7 @@ __device__ __forceinline__ void attn_kv4_work(const Args& p) {
         __syncthreads();
       }
     }
-    if constexpr (MODE == kAttnPages) return;
+    if constexpr (FIXED) return;
     if (last_head < 0) {
       ++item;
       take();

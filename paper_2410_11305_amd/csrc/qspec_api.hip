@@ -875,6 +875,9 @@ void launch_attn(const AttnArgs& a, AttnPlan plan, hipStream_t s) {
   else launch_attn_inst<D, 4, 1>(a, s);
 }
 
+// Rounds of its four wavefronts up to which an item is not shared out: joins cost more (us, 4 sequences of 32 heads: 573 tokens 9.2 for 11.5, 1085 tokens 13.8 for 12.7).
+constexpr int kAttnWholeRounds = 3;
+
 template <int D, int MODE>
 void launch_attn_part(const AttnPartArgs& a, AttnPlan plan, hipStream_t s, unsigned workgroups = AttnForm<1, 1>::workgroups) {
   const dim3 grid(workgroups), threads(64 * AttnForm<1, 1>::waves);
@@ -919,7 +922,7 @@ SharedWorkspace attn_shared_workspace(int B, int T, int Hq, int Hkv, int D, int 
   const size_t items = (size_t)groups * (((size_t)rows * G + block - 1) / block) * Hkv;
   const auto up = [](size_t n) { return (n + 255) & ~(size_t)255; };
   SharedWorkspace w;
-  w.parts = up(attn_workspace_bytes(T, G, D));
+  w.parts = up(attn_workspace_bytes(T, G, D) * 2);        // (places for up to 2048 parts)
   w.items = w.parts + up(attn_workspace_bytes(rows, G, D) - kAttnTicketBytes);
   w.joint = w.items + up(items * sizeof(int2));
   w.bytes = w.joint + (size_t)B * T * Hq * attn_part_floats(D) * sizeof(float);
@@ -932,8 +935,8 @@ double attn_token_ps(AttnPlan plan, int D) {
 }
 // Whether every sequence reads the shared tokens for itself, in one launch, instead of one for all and a second launch: what the first of the two
 // saves at most, with the longest contexts that the tables hold, is less than the second one and its joins cost (8 us and 20 ns an item).  Measured, one launch
-// and two (us): 4 samples of 500 tokens, 32 heads 10.3 and 16.9; 8 users of 2000, 4 rows, 32 heads 24 and 29; 16 prompts of 1500 to 6000 by 8 samples, 4 rows, 64 over 8
-// heads of 64 104 and 121; 128 users, one row of 64 over 8 heads: of 2048 tokens 50 and 54, of 4096 78 and 64, of 8197 147 and 100.
+// and two (us): 4 samples of 500 tokens, 32 heads 9.3 and 15.7; 8 users of 2000, 4 rows, 32 heads 18.6 and 23.3; 16 prompts of 1500 to 6000 by 8 samples, 4 rows, 64 over 8
+// heads of 64 108 and 112; 128 users, one row of 64 over 8 heads: of 2048 tokens 40 and 47, of 4000 66 and 60, of 8197 133 and 93.
 bool shared_in_one(const AttnPartArgs& first, AttnPlan first_plan, const AttnPartArgs& own, AttnPlan own_plan, int D, long long tokens) {
   const double alone = (double)own.B * own.blocks * attn_token_ps(own_plan, D), together = (double)first.B * first.blocks * attn_token_ps(first_plan, D);
   const double items = (double)own.B * own.blocks * own.kv.Hkv;
@@ -1409,7 +1412,7 @@ int qspec_attn_kv4_shared(const void* q_f16, const void* cache, const int32_t* p
   KvShape kv = kv_shape(pos, page_table, T * group, Hkv, page_size, max_pages, n_pages);
   AttnPartArgs first{attn_args(kv, q_f16, cache, out_f16, workspace, groups, Hq, plan, scale, 0, 0), T, group, shared,
                      reinterpret_cast<float*>(base + w.joint), reinterpret_cast<float*>(base + w.parts), reinterpret_cast<int2*>(base + w.items),
-                     log2_exact(16 * plan.nb / plan.f), 0, nullptr, 0, 0};
+                     log2_exact(16 * plan.nb / plan.f), 0, nullptr, 0, 0, kAttnWholeRounds};
   first.first_blocks = first.blocks;
   first.parts = first.first_parts;
   kv.T = T;
@@ -1419,17 +1422,22 @@ int qspec_attn_kv4_shared(const void* q_f16, const void* cache, const int32_t* p
   if (!attn_counts(first, tokens) || !attn_counts(rest, tokens)) return QSPEC_ERR_SHAPE;
   if (int st = check_device()) return st;
   const hipStream_t s = static_cast<hipStream_t>(stream);
+  const long long items = (long long)B * rest.blocks * Hkv;
+  // A part of an item to every compute unit.  Long rows may leave one sequence with most of the work: its items are divided further, from 16 rounds on.
+  while (rest.split < 4 && items << (rest.split + 1) <= 256) ++rest.split;
+  while (rest.split < 4 && items << (rest.split + 1) <= 2048 && tokens >> rest.split > 16384) { ++rest.split; rest.whole_rounds = 16; }
+  const unsigned workgroups = (unsigned)(items << rest.split);
   if (shared_in_one(first, plan, rest, rest_plan, D, tokens)) {
-    if (D == 128) launch_attn_part<128, kAttnBoth>(rest, rest_plan, s);
-    else launch_attn_part<64, kAttnBoth>(rest, rest_plan, s);
+    if (D == 128) launch_attn_part<128, kAttnBoth>(rest, rest_plan, s, workgroups);
+    else launch_attn_part<64, kAttnBoth>(rest, rest_plan, s, workgroups);
     return launch_status();
   }
   if (D == 128) {
     launch_attn_part<128, kAttnPrefix>(first, plan, s);
-    launch_attn_part<128, kAttnRest>(rest, rest_plan, s);
+    launch_attn_part<128, kAttnRest>(rest, rest_plan, s, workgroups);
   } else {
     launch_attn_part<64, kAttnPrefix>(first, plan, s);
-    launch_attn_part<64, kAttnRest>(rest, rest_plan, s);
+    launch_attn_part<64, kAttnRest>(rest, rest_plan, s, workgroups);
   }
   return launch_status();
 }
@@ -1460,7 +1468,7 @@ int qspec_attn_kv4_blocks(const void* q_f16, const void* cache, const int32_t* p
   const bool single = plan.nb < 4 && (items >= 2048 || (items >= 1024 && steps <= 8));
   int split = 0;
   while (!single && split < 4 && items << (split + 1) <= 256 && steps >> (split + 1) >= 4) ++split;
-  const AttnPartArgs a{common, T, 1, nullptr, nullptr, nullptr, nullptr, 0, 0, pages, count, split};
+  const AttnPartArgs a{common, T, 1, nullptr, nullptr, nullptr, nullptr, 0, 0, pages, count, split, kAttnWholeRounds};
   if (int st = check_device()) return st;
   const hipStream_t s = static_cast<hipStream_t>(stream);
   const unsigned workgroups = (unsigned)(items << split);
