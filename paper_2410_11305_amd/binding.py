@@ -634,14 +634,24 @@ def kv4_bounds(cache: torch.Tensor, pos: torch.Tensor, T: int, bounds: torch.Ten
     kv4_bounds_bytes], updated in place.  To be called behind each rope_kv4_append."""
     device, c, at, table, B, max_pages, n_pages = _kv4(cache, pos, page_table, Hkv, D, page_size, "qspec_kv4_bounds")
     _check(lib().qspec_kv4_bounds(c, at, table, B, T, Hkv, D, page_size, max_pages, n_pages,
-                                  _shaped(bounds, torch.uint8, (n_pages, kv4_bounds_bytes(Hkv, D)), device, "bounds"), _stream()), "qspec_kv4_bounds")
+                                  _shaped(bounds, torch.uint8, (n_pages, _kv4_bounds_bytes(Hkv, D)), device, "bounds"), _stream()), "qspec_kv4_bounds")
     return bounds
+
+
+_bounds_bytes = {}
+
+
+def _kv4_bounds_bytes(Hkv, D):
+    nbytes = _bounds_bytes.get((Hkv, D))
+    if nbytes is None:
+        nbytes = _bounds_bytes[Hkv, D] = kv4_bounds_bytes(Hkv, D)
+    return nbytes
 
 
 def _kv4_bounds(bounds, pos, page_table, Hkv, D, where):
     """(device number, bounds, pos, table pointers, B, max_pages, n_pages) of a call that reads bounds."""
     n_pages, B = bounds.shape[0], pos.shape[0]
-    nbytes = kv4_bounds_bytes(Hkv, D)
+    nbytes = _kv4_bounds_bytes(Hkv, D)
     if B == 0 or n_pages == 0 or nbytes == 0:
         raise QSpecError(ERR_SHAPE, where)
     device = _here(bounds, "bounds")

@@ -197,10 +197,11 @@ constexpr int kScoreColumns = 4;                       // blocks of 16 columns o
 
 // grid (B * sets * Hkv, chunks): a product of pages by heads over 2 D features, 16 by 16 a matrix instruction.  A query's heads take the next
 // power of two of columns (repeating the last one), so their largest score is a fold in a row of lanes; more than 16 take several
-// blocks.  The queries' codes are worked out once a workgroup and shared through LDS.  A workgroup takes 64 pages (more only past 65535 sets of them); the
-// heads of a sequence follow each other on one XCD, whose L2 then has the lines that they share (512 pages of 32 sequences and 8 heads: 12 us for 16).  Bound by
-// latency up to there (position, table, bounds one after the other: 2048 pages of 8 heads 3.8 us), then by the loads of 260 bytes that lie 2 KB
-// apart (34 MB in 12 us).  Runs of 64 pages a wavefront were slower (14).  Lane (row, k): row = lane & 15, 16 codes from 16 (lane >> 4) on in each 64.
+// blocks.  The queries' codes are worked out once a workgroup and shared through LDS.  A wavefront runs through its pages 16 at a time, the next ones'
+// bounds on their way; the heads of a sequence follow each other on one XCD, whose L2 then has the lines that they share (512 pages of 32 sequences and 8 heads: 12
+// us for 16).  Bound by latency (position, table, bounds one after the other: 2048 pages of 8 heads 3.8 us), then by the loads of 260 bytes that lie 2 KB
+// apart (34 MB in 12 us).  Runs of 64 pages with all their loads at once were slower (14): fewer wavefronts fit.
+// Lane (row, k): row = lane & 15, 16 codes from 16 (lane >> 4) on in each 64.
 template <int D>
 __global__ __launch_bounds__(256) void kv4_score_kernel(SelectArgs p) {
   constexpr int NI = D / 64;                           // matrix instructions of a half
@@ -285,17 +286,21 @@ __global__ __launch_bounds__(256) void kv4_score_kernel(SelectArgs p) {
     }
   }
   __syncthreads();
-  for (; i0 < n; i0 += gridDim.y * 64, load_pages(i0)) {
+  for (; i0 < n; i0 += gridDim.y * 64) {
+    v4i now_u[NI], now_l[NI];
     float g4[4];                                       // of this lane's four pages
 #pragma unroll
+    for (int i = 0; i < NI; ++i) { now_u[i] = u[i]; now_l[i] = l[i]; }
+#pragma unroll
     for (int r = 0; r < 4; ++r) g4[r] = __shfl(grid, 4 * kb + r);
+    if (i0 + (int)gridDim.y * 64 < n) load_pages(i0 + gridDim.y * 64);
     v4i best = {};
     for (int c = 0; c < blocks; ++c) {
       v4i dot = {0, 0, 0, 0};
 #pragma unroll
       for (int i = 0; i < NI; ++i) {
-        dot = __builtin_amdgcn_mfma_i32_16x16x64_i8(u[i], codes[(c * 2 * NI + i) * 64 + lane], dot, 0, 0, 0);
-        dot = __builtin_amdgcn_mfma_i32_16x16x64_i8(l[i], codes[(c * 2 * NI + NI + i) * 64 + lane], dot, 0, 0, 0);
+        dot = __builtin_amdgcn_mfma_i32_16x16x64_i8(now_u[i], codes[(c * 2 * NI + i) * 64 + lane], dot, 0, 0, 0);
+        dot = __builtin_amdgcn_mfma_i32_16x16x64_i8(now_l[i], codes[(c * 2 * NI + NI + i) * 64 + lane], dot, 0, 0, 0);
       }
       if (p.G > 16) {
 #pragma unroll

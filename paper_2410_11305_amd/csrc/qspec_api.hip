@@ -1537,16 +1537,19 @@ int qspec_kv4_select(const void* q_f16, const void* bounds, const int32_t* pos, 
   SelectArgs a{kv_shape(pos, page_table, T, Hkv, page_size, max_pages, n_pages), static_cast<const uint16_t*>(q_f16), static_cast<const uint8_t*>(bounds),
                static_cast<uint32_t*>(workspace), pages, Hq, G, width, columns, queries, (int)sets, B, first, last, count, select_row_keys(max_pages)};
   const hipStream_t s = static_cast<hipStream_t>(stream);
-  const unsigned chunks = blocks_for((size_t)max_pages, 64);
+  // 64 pages a workgroup, runs of them where there would be more than a thousand workgroups (128 queries of up to 512 pages: 16.6 us for 17.4; 512: 19.3)
+  unsigned chunks = blocks_for((size_t)max_pages, 64);
+  while (chunks > 1 && rows * chunks > 1024) chunks = (chunks + 1) / 2;
   const size_t lds = (size_t)columns * (D / 32) * 1024;
   const dim3 grid((unsigned)((rows + 7) / 8 * 8), chunks < 65535u ? chunks : 65535u);
   if (D == 128) launch_kernel(kv4_score_kernel<128>, grid, dim3(256), lds, s, a);
   else launch_kernel(kv4_score_kernel<64>, grid, dim3(256), lds, s, a);
-  // Sixteen wavefronts to a row where every row has a compute unit (us of the whole call, 8 rows 10.0 for 11.6), four where they share them (1024
-  // rows of 512 pages: 22 for 25).
+  // Sixteen wavefronts to a row where every row has a compute unit (us of the whole call, 8 rows of 2048 pages 10.0 for 11.6), four where they share them
+  // (1024 rows of 512 pages: 22 for 25), and no more keys to a thread than there can be (the same: 17.5 for 19.7).
   const int lists = B * T * Hkv;
   const dim3 each((unsigned)lists);
-  if (max_pages > 8192) launch_kernel(kv4_choose_many_kernel, each, dim3(kChooseThreads), 0, s, a);
+  if (max_pages <= 512) launch_kernel((kv4_choose_kernel<256, 2>), each, dim3(256), 0, s, a);
+  else if (max_pages > 8192) launch_kernel(kv4_choose_many_kernel, each, dim3(kChooseThreads), 0, s, a);
   else if (lists <= 256 && max_pages <= 2048) launch_kernel((kv4_choose_kernel<1024, 2>), each, dim3(1024), 0, s, a);
   else if (lists <= 256) launch_kernel((kv4_choose_kernel<1024, 8>), each, dim3(1024), 0, s, a);
   else if (max_pages <= 2048) launch_kernel((kv4_choose_kernel<256, 8>), each, dim3(256), 0, s, a);

@@ -1,12 +1,15 @@
 """Host-side checks of attention behind shared beginnings, the bounds of pages, the choice of pages and attention over them that need no
 GPU: sizes, refusals before anything is launched, and pins of the oracle."""
 import math
+import os
+import re
 
 import numpy as np
 import pytest
 
 from oracle import kv4_pages_oracle as pg
 from paper_2410_11305_amd import binding as B
+from paper_2410_11305_amd import build
 
 A = 4096          # any 16-byte aligned non-null address: rejected before use
 
@@ -122,6 +125,35 @@ def test_binding_refuses_tensors_that_do_not_fit():
         B.kv4_select(q, bounds, torch.zeros(0, dtype=torch.int32), 2, 64, 2)
     with pytest.raises(B.QSpecError):
         B.kv4_bounds_read(bounds, pos, 1, 2, 80, 64)
+
+
+# ------------------------------------------------------------------ parts of an item
+def test_parts_of_an_item_take_every_step_once():
+    """A workgroup's share of an item as the kernel has it, with the formulas read from the source: parts follow each other, cover all steps, and are as many as are
+    waited for."""
+    source = re.sub(r"//.*", "", open(os.path.join(build.HERE, "csrc", "attn_kv4.hpp")).read())
+    block = source[source.index("if constexpr (FIXED) {\n      const int rounds"):]
+    expression = lambda text: eval_of(re.search(text, block).group(1))
+    eval_of = lambda e: re.sub(r"(.*) \? (.*) : (.*)", r"((\2) if \1 else (\3))", e.replace("/", "//").replace("span.steps", "steps").replace("p.split", "split").replace("p.whole_rounds", "whole"))
+    rounds_of, each_of, parts_of = (expression(r"const int rounds = ([^,;]*),"), expression(r"each = ([^;]*);"), expression(r"item_parts = ([^;]*);"))
+    begin_of = expression(r"begin = \(int\)\(me - \(item << p.split\)\) \* ([^;]*);")
+    assert "if (begin >= span.steps) return;" in block and "stop = min(span.steps, begin + each * WAVES);" in block
+    for WAVES in (1, 4):
+        for whole in (3, 16):
+            for split in range(5):
+                for steps in list(range(1, 300)) + [1000, 1023, 1024, 1025, 65536]:
+                    names = dict(WAVES=WAVES, whole=whole, split=split, steps=steps)
+                    names["rounds"] = eval(rounds_of, {}, names)
+                    names["each"] = eval(each_of, {}, names)
+                    parts, at = eval(parts_of, {}, names), 0
+                    for part in range(1 << split):
+                        begin = part * eval(begin_of, {}, names)
+                        if begin >= steps:
+                            assert part >= parts
+                            continue
+                        assert begin == at and part < parts
+                        at = min(steps, begin + names["each"] * WAVES)
+                    assert at == steps and 1 <= parts <= 1 << split
 
 
 # ------------------------------------------------------------------ pins of the oracle
