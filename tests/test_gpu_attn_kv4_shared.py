@@ -108,6 +108,20 @@ def test_groups_rows_and_lengths(env, groups, per, T, Hq, Hkv, D, P, shared):
     check(env, c, queries(D, Bn, T, Hq, D), pos, tables(1, groups, per, each, P, shared, Bn * each), shared, rows=range(Bn) if Bn <= 20 else range(0, Bn, 7))
 
 
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("groups,per,T,Hq,Hkv,n", [(1, 18, 1, 16, 8, 700), (3, 6, 4, 16, 8, 90), (2, 9, 2, 64, 8, 1400), (1, 17, 4, 64, 8, 300), (1, 150, 8, 8, 1, 40)])
+def test_an_item_to_a_compute_unit(env, groups, per, T, Hq, Hkv, D, n):
+    """129 to 256 items, of every size up to 32 rows and more."""
+    P, shared, rng = 64, [n - 20 * g for g in range(groups)], np.random.default_rng(n)
+    Bn = groups * per
+    pos = np.repeat(shared, per) + rng.integers(-3, 900, Bn)
+    each = -(-(int(pos.max()) + T) // P)
+    table = tables(1, groups, per, each, P, shared, Bn * each)
+    used, inverse = np.unique(table, return_inverse=True)
+    c = Cache(T + D, len(used), Hkv, D, P)
+    check(env, c, queries(D, Bn, T, Hq, D), pos, inverse.reshape(table.shape), shared, rows=range(0, Bn, 5))
+
+
 @pytest.mark.parametrize("T", [1, 6])
 def test_rows_in_front_of_the_end_of_what_is_shared(env, T):
     """Rows that see part of the shared tokens, all of them but one, none; idle sequences, the first of its group among them; positions and
