@@ -301,3 +301,116 @@ def test_two_streams_with_a_workspace_each_and_a_graph(env, long_rows):
         assert torch.equal(outs[0], outs[2])
         compare(outs[0].cpu().numpy().astype(np.float64), c, q_new, at, table, sh)
         assert int(works[0][:16384].count_nonzero()) == 0
+
+
+@pytest.mark.parametrize("what", ["zero", "constant", "subnormal", "huge", "mixed", "shared large", "own large"])
+def test_value_steps_of_every_size(env, what):
+    """Constant rows, fp16's smallest and largest, and the two parts' sums on references that lie far apart."""
+    P, each, per, shared, D, Hkv = 64, 16, 3, [500], 128, 2
+    pos = np.array([900, 520, 1000])
+    table = tables(1, 1, per, each, P, shared, per * each)
+    c = Cache(10, per * each, Hkv, D, P)
+    if what == "zero":
+        c.vs[:], c.vl[:], c.ks[:], c.kl[:] = 0, 0, 0, 0
+    elif what == "constant":
+        c.vs[:] = 0
+    elif what == "subnormal":
+        c.vs[:], c.vl[:] = 2.0 ** -24, -7 * 2.0 ** -24
+    elif what == "huge":
+        c.vs[:], c.vl[:] = 8000.0, -60000.0
+    elif what == "mixed":
+        c.vs[:] = (2.0 ** np.random.default_rng(1).integers(-20, 12, c.vs.shape)).astype(np.float16)
+        c.vl[:] = -8 * c.vs.astype(np.float32)
+    else:
+        first = np.zeros(per * each, bool)
+        first[table[0, :8]] = True
+        large = first if what == "shared large" else ~first
+        c.vs[large], c.vs[~large] = 1000.0, 2.0 ** -20
+        c.vl[large], c.vl[~large] = -8000.0, 0.0
+    check(env, c, queries(11, per, 2, 4, D), pos, table, shared)
+
+
+@pytest.mark.parametrize("size,scale", [(0.0, None), (60.0, None), (1e-3, 100.0), (2.0 ** -24, 1e6), (1.0, 1e-6)])
+def test_queries_of_every_size(env, size, scale):
+    P, each, per, shared, D = 32, 20, 3, [300], 128
+    c = Cache(12, per * each, 2, D, P)
+    check(env, c, queries(13, per, 3, 4, D, size), np.array([600, 310, 200]), tables(2, 1, per, each, P, shared, per * each), shared, scale=scale)
+
+
+def test_caches_of_more_than_four_gib(env):
+    """The pages at both ends and past the 32-bit offsets: shared attention, bounds, attention over chosen pages."""
+    torch, B = env
+    from oracle import kv4_pages_oracle as pg
+    from tests.test_gpu_kv4_pages import Bounds, compare_blocks, empty_bounds, oracle_bounds, oracle_choice
+    P, Hkv, D, each, T, Hq = 256, 8, 128, 2, 2, 16
+    page = B.kv4_page_bytes(Hkv, D, P)
+    n_pages = (5 << 30) // page
+    small = Cache(17, 4, Hkv, D, P)
+    cache, bounds = torch.zeros((n_pages, page), dtype=torch.uint8, device="cuda"), B.alloc_kv4_bounds(n_pages, Hkv, D)
+    where = np.array([n_pages - 1, 3, n_pages // 2 + 1, n_pages - 7])
+    cache[torch.from_numpy(where).cuda()] = dev(torch, small.bytes())
+    table, small_table = where[[[0, 1], [0, 2]]], np.array([[0, 1], [0, 2]])
+    q, pos = queries(18, 2, T, Hq, D), np.array([500, 400])
+    at, tab = dev(torch, pos.astype(np.int32)), dev(torch, table.astype(np.int32))
+    shared = [300]
+    small.k[2, :, :44], small.v[2, :, :44] = 0, 0             # (not read: shared)
+    for t in (tab, dev(torch, far(table, P).astype(np.int32))):
+        got = B.attn_kv4_shared(dev(torch, q), cache, at, dev(torch, np.array(shared, np.int32)), Hkv, P, t)
+        compare(got.cpu().numpy().astype(np.float64), small, q, pos, small_table, shared)
+    small = Cache(17, 4, Hkv, D, P)
+    one = dev(torch, np.array([[where[3], where[0]], [where[2], where[1]]], dtype=np.int32))
+    own = np.array([[3, 0], [2, 1]])
+    B.kv4_bounds(cache, dev(torch, np.zeros(2, np.int32)), 500, bounds, Hkv, D, P, one)
+    state = empty_bounds(small)
+    oracle_bounds(small, own, np.zeros(2, np.int64), 500, *state)
+    assert (bounds[torch.from_numpy(where).cuda()].cpu().numpy() == pg.bounds_bytes(*state)).all()
+    picked = B.kv4_select(dev(torch, q), bounds, at, Hkv, P, 1, one, first=0, last=0)
+    reference = Bounds(0, 4, Hkv, D)
+    reference.upper, reference.lower, reference.grid = state
+    want = oracle_choice(reference, q, pos, own, P, 0, 0, 1)
+    assert (picked.cpu().numpy() == want).all()
+    got = B.attn_kv4_blocks(dev(torch, q), cache, at, picked, Hkv, P, one)
+    compare_blocks(got.cpu().numpy().astype(np.float64), small, q, pos, own, want)
+
+
+def test_one_workspace_serves_all_in_turn(env):
+    torch, B = env
+    from paper_2410_11305_amd import synth
+    M, N, K = 200, 1024, 4096
+    codes, scales, x = synth.generic_case(23, M, N, K)
+    blob, xd = B.pack_weights(dev(torch, codes), dev(torch, scales)), dev(torch, x)
+    c = Cache(24, 40, 2, 128, 64)
+    cache, pos, q = dev(torch, c.bytes()), torch.tensor([2500, 2000], dtype=torch.int32, device="cuda"), dev(torch, queries(25, 2, 1, 8, 128))
+    table = torch.arange(40, dtype=torch.int32, device="cuda").repeat(2, 1)
+    long_table = torch.full((2, 1 << 13), -1, dtype=torch.int32, device="cuda")
+    long_table[:, :40] = table
+    shared = torch.tensor([1900], dtype=torch.int32, device="cuda")
+    blocks = torch.arange(0, 40, 2, dtype=torch.int32, device="cuda").repeat(2, 1, 2, 1)
+    ws = B.alloc_workspace(max(B.workspace_bytes(M, N, K), B.attn_kv4_workspace_bytes(2, 1, 8, 2, 128), B.attn_kv4_shared_workspace_bytes(2, 1, 8, 2, 128, 1),
+                               B.attn_kv4_blocks_workspace_bytes(2, 1, 8, 2, 128)))
+    calls = [lambda w: B.gemm_w4a16(blob, xd, N, workspace=w), lambda w: B.attn_kv4(q, cache, pos, 2, 64, table, workspace=w),
+             lambda w: B.attn_kv4_shared(q, cache, pos, shared, 2, 64, table, workspace=w), lambda w: B.attn_kv4_shared(q, cache, pos, shared, 2, 64, long_table, workspace=w),
+             lambda w: B.attn_kv4_blocks(q, cache, pos, blocks, 2, 64, table, workspace=w)]
+    alone = [call(None) for call in calls]
+    for _ in range(3):
+        for call, want in zip(calls, alone):
+            assert torch.equal(call(ws), want)
+            assert int(ws[:16384].count_nonzero()) == 0
+
+
+def test_tensors_that_do_not_fit_are_refused(env):
+    torch, B = env
+    cache, pos, q = B.alloc_kv4_cache(8, 2, 64, 64), torch.zeros(2, dtype=torch.int32, device="cuda"), torch.zeros((2, 1, 4, 64), dtype=torch.float16, device="cuda")
+    bounds, shared, blocks = B.alloc_kv4_bounds(8, 2, 64), torch.zeros(1, dtype=torch.int32, device="cuda"), torch.zeros((2, 1, 2, 3), dtype=torch.int32, device="cuda")
+    bad = [lambda: B.attn_kv4_shared(q, cache, pos, shared.long(), 2, 64), lambda: B.attn_kv4_shared(q, cache, pos, shared.cpu(), 2, 64), lambda: B.attn_kv4_shared(q.float(), cache, pos, shared, 2, 64),
+           lambda: B.attn_kv4_shared(q, cache, pos, shared, 2, 64, out=q[:1]), lambda: B.attn_kv4_blocks(q, cache, pos, blocks[:, :, :1], 2, 64), lambda: B.attn_kv4_blocks(q, cache, pos, blocks.long(), 2, 64),
+           lambda: B.attn_kv4_blocks(q, cache, pos, blocks.transpose(1, 2), 2, 64), lambda: B.kv4_bounds(cache, pos, 1, bounds[:4], 2, 64, 64), lambda: B.kv4_bounds(cache, pos, 1, bounds[:, 16:], 2, 64, 64),
+           lambda: B.kv4_bounds_read(bounds, pos, 1, 2, 64, 64, upper=torch.zeros((2, 1, 2, 64), device="cuda")), lambda: B.kv4_select(q, bounds, pos, 2, 64, 3, blocks=blocks[..., :2]),
+           lambda: B.kv4_select(q, bounds, pos, 2, 64, 3, page_table=torch.zeros((3, 4), dtype=torch.int32, device="cuda")), lambda: B.kv4_select(q, bounds.float(), pos, 2, 64, 3)]
+    for call in bad:
+        with pytest.raises(ValueError):
+            call()
+    for call in (lambda: B.attn_kv4_shared(q, cache, pos, torch.zeros(3, dtype=torch.int32, device="cuda"), 2, 64), lambda: B.kv4_select(q, bounds, pos, 2, 64, 3, first=2, last=2),
+                 lambda: B.kv4_select(q, bounds, pos, 2, 64, 0), lambda: B.attn_kv4_blocks(q, B.alloc_kv4_cache(8, 2, 64, 32), pos, blocks, 2, 32)):
+        with pytest.raises(B.QSpecError):
+            call()
