@@ -31,6 +31,12 @@
 // as they issue, the vector unit works in 27 to 34 % of its cycles.  From 17 rows on it works in 55 % (32 rows), 37 % (64: two wavefronts a SIMD,
 // in which the products and the exponentials of a step wait for one another), the matrix unit in 12 %: it takes 5 to 7 vector
 // instructions a word to widen and a dozen a score.
+//
+// The same loop serves calls that read other tokens than a sequence's own from its start (attn_kv4_part_kernel, MODE below): those that a group
+// of sequences shares, once for all of its rows or by each sequence, those behind them, and the pages of a list.  Measured (device time): 4 samples of 500 shared
+// tokens, 32 heads 9.3 us; 8 users of 2000, 4 rows, 32 heads 16.5; 128 users of 8197 shared tokens and 100 to 1500 of their own, one row of 64 over 8 heads 94, of which
+// the shared ones 66 (530 TF/s) and the others 29 (3.5 TB/s); 16 pages of 6000 tokens, 32 heads 8.7; 64 of 2048 pages, 64 over 8 heads 10.5; 64 rows of 16 pages of 256,
+// 64 over 8 heads 48 (5.9 TB/s); 128 rows of 32 pages, 64 over 8 heads of 64 27 (5.8 TB/s).
 #pragma once
 #include "common.hpp"
 #include "exchange.hpp"
@@ -214,8 +220,11 @@ __device__ __forceinline__ void attn_kv4_work(const Args& p) {
   constexpr int WAVES = W, THREADS = 64 * WAVES, TILES = Form::tiles, STEP = Form::step, RB = Form::rows, OVER = Form::over;
   // (sums that are not joined in this launch cost less: 2048 shared tokens of 1024 rows over 8 heads 39 us for 55)
   constexpr int LEAST = MODE == kAttnWhole || F > 1 ? Form::least : (NB == 4 ? 512 : 256) / STEP;
-  // A workgroup for each part of each item, without a division of the steps: where the host knows how long items are at most.
+  // A workgroup for each part of each item, without a division of the steps: fewer registers (up to three workgroups to a unit), 2 us less before
+  // the first scores, few joins (us: 8 users of 2000 shared tokens 24 -> 18.7, 128 rows of 32 pages 38 -> 27).  A long item among short ones holds the launch up
+  // where the division would spread it.
   constexpr bool FIXED = MODE == kAttnPages || MODE == kAttnBoth || MODE == kAttnRest;
+  static_assert(FIXED || LEAST >= 2 * WAVES, "no workgroup's share rounds down to nothing");
   constexpr int NK = D / 32;                  // matrix instructions of a tile of q k^T; words of a lane of a key
   constexpr int NV = D / 16;                  // matrix instructions of two tiles of p v
   constexpr int COLS = 16 / F;                // rows of a block of columns
@@ -514,9 +523,8 @@ __device__ __forceinline__ void attn_kv4_work(const Args& p) {
     const auto position_of = [&](int nb) {
       const int j = over_group(p, row_of_column(nb));
       if constexpr (MODE == kAttnPrefix) {
-        // (what a row in front of its sequence collects here is not used)
-        const int seq = p.rows == 1 ? j : j / p.rows, at = held_position(p.kv.pos[b * p.group + seq], p.rows) + (j - seq * p.rows);
-        return at < 0 ? span.hi : min(at, span.hi);
+        const int seq = p.rows == 1 ? j : j / p.rows;
+        return min(held_position(p.kv.pos[b * p.group + seq], p.rows) + (j - seq * p.rows), span.hi);
       }
       return span.lo + j - over_group(p, block * RB);
     };
@@ -564,10 +572,12 @@ __device__ __forceinline__ void attn_kv4_work(const Args& p) {
     const auto factor = [&](int nb) { return Q_LDS ? f_lds[nb * 16 + col].x : f_own[Q_LDS ? 0 : nb]; };
     const auto shift = [&](int nb) { return Q_LDS ? f_lds[nb * 16 + col].y : shift_own[Q_LDS ? 0 : nb]; };
     const auto position = [&](int nb) { return Q_LDS ? __builtin_bit_cast(int, f_lds[nb * 16 + col].z) : pos_own[Q_LDS ? 0 : nb]; };
-    if constexpr (MODE == kAttnPrefix) {      // the first of the rows' last tokens
-      int least = Q_LDS ? __builtin_bit_cast(int, f_lds[Q_LDS ? lane & (RB - 1) : 0].z) : pos_own[0];
+    if constexpr (MODE == kAttnPrefix) {
+      // The first of the rows' last tokens.  (Rows in front of their sequences have none, and what they collect where all others see everything is not used.)
+      const auto last_of = [&](int at) { return at < 0 ? span.hi : at; };
+      int least = last_of(Q_LDS ? __builtin_bit_cast(int, f_lds[Q_LDS ? lane & (RB - 1) : 0].z) : pos_own[0]);
 #pragma unroll
-      for (int nb = 1; nb < (Q_LDS ? 1 : NB); ++nb) least = min(least, pos_own[nb]);
+      for (int nb = 1; nb < (Q_LDS ? 1 : NB); ++nb) least = min(least, last_of(pos_own[nb]));
 #pragma unroll
       for (int d = 1; d < 64; d <<= 1) least = min(least, __shfl_xor(least, d));
       span.lo = uniform(least);

@@ -223,6 +223,20 @@ def test_rows_nobody_sees_may_hold_anything(env, T):
     assert torch.equal(check_one(*args, len_=each), check_one(*args, len_=each, raw=bad.bytes()))
 
 
+@pytest.mark.parametrize("bad", [60000.0, np.inf, np.nan])
+@pytest.mark.parametrize("T,G", [(1, 3), (5, 4), (20, 2)])
+def test_idle_sequences_do_not_bring_tokens_in(env, T, G, bad):
+    """Shared tokens behind every row, of steps of fp16's largest size or that are no numbers, beside sequences that are not running."""
+    P, each, shared, D = 16, 12, [150], 64
+    pos = np.array([-T, 40, -T - 5, 60 - T, -T])
+    table = tables(5, 1, 5, each, P, shared, 5 * each)
+    c = Cache(21, 5 * each, 1, D, P)
+    for token in range(max(int(pos.max()) + T, 41 + T), 150):
+        c.vs[table[0, token // P], 0, token % P], c.vl[table[0, token // P], 0, token % P] = bad, -bad
+        c.ks[table[0, token // P], 0, token % P] = bad
+    check(env, c, queries(T, 5, T, G, D), pos, table, shared)
+
+
 def test_what_is_no_number_shows_where_it_is_seen(env):
     torch, B = env
     P, each, shared, D, Hq, Hkv = 16, 8, [50], 64, 4, 2
