@@ -414,8 +414,9 @@ int qspec_attn_kv4(const void* q_f16, const void* cache, const int32_t* pos, con
  *   shared  int32 [groups], device memory; 0 or less: none.  Held to max_pages * page_size.
  *   (B / groups) * T <= 2^20, and the count of work at qspec_attn_kv4 holds for the groups as sequences of (B / groups) * T rows too.
  *   A row in front of its sequence gets zeros.  Everything else, NaN and limits of scale and scores included, as in qspec_attn_kv4.
- *   Where the table's rows are short (max_pages * page_size tokens) and what one reading for all saves is little, each sequence reads the shared tokens
- *   for itself in one launch; otherwise there are two, with partial sums of the shared tokens in binary32 between them.
+ *   Where a group shares so little that one reading for all would save less than it costs, its sequences read the shared tokens for themselves; where the
+ *   table's rows (max_pages * page_size tokens) are too short for anything else, that is one launch.  Otherwise there are two, with partial sums of the shared
+ *   tokens in binary32 between them.
  *   workspace  qspec_attn_kv4_shared_workspace_bytes(...) bytes; the workspace rule at qspec_workspace_bytes holds.
  */
 size_t qspec_attn_kv4_shared_workspace_bytes(int B, int T, int Hq, int Hkv, int D, int groups);
@@ -512,6 +513,8 @@ int qspec_sample(const void* logits_f16, const float* u, const float* temperatur
  *   "QSPEC_STREAM_MAX_W4A4"   32..128: the draft-mode streaming kernel takes every M up to
  *                             this one and none above
  *   "QSPEC_TILE_W4A4",    "QSPEC_TILE_W4A16"     value "shape,S": workgroup shape, K-slices
+ *   "QSPEC_ATTN_SHARED"       shared tokens from which on qspec_attn_kv4_shared reads them once for all sequences of a group
+ *                             (0: always; past the table's rows: never)
  *   "QSPEC_MLP_SPIN"          polls before a workgroup of qspec_mlp_draft gives up waiting
  * `value` NULL (or unparsable) clears that override; both are host strings.  The same
  * names are read from the environment once, at the library's first use; no entry point

@@ -81,15 +81,16 @@ struct AttnArgs {
 };
 
 // What a launch reads and what becomes of its sums.  kAttnWhole: every token in sight, results.  kAttnPrefix: the tokens that the sequences of a
-// group share, as partial sums of every row; kAttnRest: those behind them, joined with these sums, results.  kAttnPages: the pages
-// that a list names for each row, results.  kAttnBoth: shared tokens and those behind them of one sequence after the other, results.
-enum { kAttnWhole, kAttnPrefix, kAttnRest, kAttnPages, kAttnBoth };
+// group share, as partial sums of every row; kAttnOwn: those behind them, joined with these sums, or, where a group shares too few for that, the shared ones and
+// those behind them, results.  kAttnPages: the pages that a list names for each row, results.
+enum { kAttnWhole, kAttnPrefix, kAttnOwn, kAttnPages };
 
 struct AttnPartArgs : AttnArgs {
   // kAttnPrefix: kv.T and B are the rows of a group and the groups;  kAttnPages: one row each and all rows
   int rows;                  // rows of a sequence (T of the call)
   int group;                 // sequences of a group
   const int32_t* shared;     // [groups]: tokens that they share
+  int least_shared;          // of so many on they are read once for all
   // Partial sums of the shared tokens, attn_part_floats a row: in `joint` [B * rows * Hq], or in several parts, for an item that several
   // workgroups hold.  (They stay as they are: the launch that reads them has the rows of an item in many workgroups.)
   float* joint;
@@ -98,8 +99,7 @@ struct AttnPartArgs : AttnArgs {
   int first_shift, first_blocks;      // rows of a block of an item (a power of two), blocks of a group
   const int32_t* list;       // [B * rows][Hkv][count]
   int count;
-  int split;                 // log2 of the parts of an item at most
-  int whole_rounds;          // an item of up to so many rounds of its wavefronts stays whole
+  int fill, split;           // log2 of the parts of an item: ordinarily, and at most
 };
 
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
@@ -119,9 +119,10 @@ __device__ __forceinline__ int row_count(const AttnArgs&) { return 1; }
 __device__ __forceinline__ int row_count(const AttnPartArgs& p) { return p.rows; }
 
 // Where a sequence stands.  at: position of its first row (kAttnPrefix: how many tokens the group shares);  from: the first token of its own
-// (kAttnRest, kAttnBoth).
+// (kAttnOwn), and whether those in front of it are read for all.
 struct AttnWhere {
   int at, from;
+  bool joined;
 };
 
 // The position that a row of a block's window begins behind.  (A row in front of the sequence sees nothing, whatever its window.)
@@ -138,7 +139,7 @@ __device__ __forceinline__ AttnSpan attn_span(const Args& p, AttnWhere w, int bl
   AttnSpan s;
   s.first = s.sink_steps = 0;
   if constexpr (MODE == kAttnPrefix) {
-    s.lo = s.hi = min(w.at, last) - 1;        // (of the rows that see them all)
+    s.lo = s.hi = w.at - 1;                   // (of the rows that see them all)
     s.steps = max((s.hi + STEP) / STEP, 1);
     return s;
   }
@@ -151,9 +152,9 @@ __device__ __forceinline__ AttnSpan attn_span(const Args& p, AttnWhere w, int bl
     s.steps = max(min(p.count, pages) * ((1 << p.kv.page_shift) / STEP), 1);
     return s;
   }
-  if constexpr (MODE == kAttnRest || MODE == kAttnBoth) {
+  if constexpr (MODE == kAttnOwn) {
     s.first = w.from / STEP;
-    if constexpr (MODE == kAttnBoth) s.sink_steps = max((min(w.from, end) + STEP - 1) / STEP, 0);      // the shared ones in front
+    if (!w.joined) s.sink_steps = max((min(w.from, end) + STEP - 1) / STEP, 0);      // the shared ones in front
   } else {
     s.first = p.window > 0 ? max(behind_window(p, s.lo) + 1, 0) / STEP : 0;
     s.sink_steps = p.window > 0 ? max(min((min(p.sinks, end) + STEP - 1) / STEP, s.first), 0) : 0;
@@ -221,9 +222,11 @@ __device__ __forceinline__ void attn_kv4_work(const Args& p) {
   // (sums that are not joined in this launch cost less: 2048 shared tokens of 1024 rows over 8 heads 39 us for 55)
   constexpr int LEAST = MODE == kAttnWhole || F > 1 ? Form::least : (NB == 4 ? 512 : 256) / STEP;
   // A workgroup for each part of each item, without a division of the steps: fewer registers (up to three workgroups to a unit), 2 us less before
-  // the first scores, few joins (us: 8 users of 2000 shared tokens 24 -> 18.7, 128 rows of 32 pages 38 -> 27).  A long item among short ones holds the launch up
-  // where the division would spread it.
-  constexpr bool FIXED = MODE == kAttnPages || MODE == kAttnBoth || MODE == kAttnRest;
+  // the first scores, few joins (us: 8 users of 2000 shared tokens 24 -> 18.7, 128 rows of 32 pages 38 -> 27).  An item stays whole up to WHOLE rounds of its wavefronts
+  // (joins cost more: 4 sequences of 32 heads, 573 tokens 9.2 us for 11.5, 1085 tokens 13.8 for 12.7), has 2^fill parts from there on, and more where these would be longer than LONG: a
+  // long one among short ones holds the launch up.
+  constexpr bool FIXED = MODE == kAttnPages || MODE == kAttnOwn;
+  constexpr int WHOLE = 3, LONG = 8;
   static_assert(FIXED || LEAST >= 2 * WAVES, "no workgroup's share rounds down to nothing");
   constexpr int NK = D / 32;                  // matrix instructions of a tile of q k^T; words of a lane of a key
   constexpr int NV = D / 16;                  // matrix instructions of two tiles of p v
@@ -250,16 +253,19 @@ __device__ __forceinline__ void attn_kv4_work(const Args& p) {
   const uint32_t region_bytes = (uint32_t)P * (D + 8);
   const int row_of = tid / LANES, own = (tid & (LANES - 1)) * 4;       // join: row, first feature
   const auto sequence_of = [&](int e) { return p.blocks == 1 ? e : e / p.blocks; };
+  const auto held = [&](int shared) { return min(max(shared, 0), p.kv.max_pages << p.kv.page_shift); };
   const auto where_is = [&](int seq, auto load) {        // load(array, index)
     if constexpr (MODE == kAttnPrefix) {
-      return AttnWhere{max(load(p.shared, seq), 0), 0};
-    } else if constexpr (MODE == kAttnRest || MODE == kAttnBoth) {
-      return AttnWhere{load(p.kv.pos, seq), min(max(load(p.shared, seq / p.group), 0), p.kv.max_pages << p.kv.page_shift)};
+      const int n = held(load(p.shared, seq));
+      return AttnWhere{n < p.least_shared ? 0 : n, 0, false};
+    } else if constexpr (MODE == kAttnOwn) {
+      const int n = held(load(p.shared, seq / p.group));
+      return AttnWhere{load(p.kv.pos, seq), n, n >= p.least_shared};
     } else if constexpr (MODE == kAttnPages) {
       const int b = p.rows == 1 ? seq : seq / p.rows;
-      return AttnWhere{held_position(load(p.kv.pos, b), p.rows) + (seq - b * p.rows), 0};
+      return AttnWhere{held_position(load(p.kv.pos, b), p.rows) + (seq - b * p.rows), 0, false};
     } else {
-      return AttnWhere{load(p.kv.pos, seq), 0};
+      return AttnWhere{load(p.kv.pos, seq), 0, false};
     }
   };
   const auto where = [&](int seq) { return where_is(seq, [](const int32_t* a, int i) { return a[i]; }); };
@@ -274,6 +280,11 @@ __device__ __forceinline__ void attn_kv4_work(const Args& p) {
   const auto size_of = [&](int e, AttnWhere at) {
     return (uint32_t)(OVER + attn_span<STEP, MODE>(p, at, e - sequence_of(e) * p.blocks, RB).steps) * (uint32_t)Hkv;
   };
+  if constexpr (MODE == kAttnPrefix) {        // nothing that is read for all
+    bool any = false;
+    for (int e = lane; e < p.B; e += 64) any |= held(p.shared[e]) >= p.least_shared;
+    if (__builtin_amdgcn_ballot_w64(any) == 0) return;
+  }
   uint32_t mine = 0;
   for (int e = lane * per; !FIXED && e < min(entries, (lane + 1) * per); ++e) mine += size_of(e, where(sequence_of(e)));
   uint32_t upto = mine;                       // of the entries up to this lane's
@@ -339,7 +350,7 @@ __device__ __forceinline__ void attn_kv4_work(const Args& p) {
       const AttnWhere at = where_scalar(0);
       for (int e = lane; e < p.B; e += 64) {
         const AttnWhere other = where(e);
-        even &= other.at == at.at && other.from == at.from;
+        even &= other.at == at.at;
       }
       const uint32_t rest = max(items % gridDim.x, 1u);
       const uint32_t load = load_of(lane == 0 ? 0 : lane == 1 ? gridDim.x - 1 : lane == 2 ? rest - 1 : gridDim.x - rest, [&](uint32_t place) {
@@ -384,8 +395,8 @@ __device__ __forceinline__ void attn_kv4_work(const Args& p) {
     entry = (int)uniform(i / (uint32_t)Hkv);
     head = (int)(i - (uint32_t)entry * (uint32_t)Hkv);
   };
-  if constexpr (FIXED) {
-    item = me >> p.split;
+  if constexpr (FIXED) {                      // (first parts first: of the others few are needed)
+    item = me % items;
     entry = (int)uniform(item / (uint32_t)Hkv);
     head = (int)(item - (uint32_t)entry * (uint32_t)Hkv);
   } else if (whole_items) {
@@ -400,15 +411,16 @@ __device__ __forceinline__ void attn_kv4_work(const Args& p) {
   while (entry < last_entry || (entry == last_entry && (head < last_head || (head == last_head && begin < last_step)))) {
     const int b = uniform(sequence_of(entry)), block = entry - b * p.blocks;
     AttnWhere here = where_scalar(b);
-    here.at = uniform(here.at); here.from = uniform(here.from);
+    here.at = uniform(here.at); here.from = uniform(here.from); here.joined = uniform((int)here.joined) != 0;
     AttnSpan span = attn_span<STEP, MODE>(p, here, block, RB);
     span.steps = uniform(span.steps); span.sink_steps = uniform(span.sink_steps); span.first = uniform(span.first);
     span.lo = uniform(span.lo); span.hi = uniform(span.hi);
     int stop = entry == last_entry && head == last_head ? last_step : span.steps;
     int item_parts = 1;
     if constexpr (FIXED) {
-      const int rounds = (span.steps + WAVES - 1) / WAVES, each = rounds <= p.whole_rounds ? rounds : (rounds + (1 << p.split) - 1) >> p.split;
-      begin = (int)(me - (item << p.split)) * each * WAVES;
+      const int rounds = (span.steps + WAVES - 1) / WAVES, even = (rounds + (1 << p.fill) - 1) >> p.fill, least = (rounds + (1 << p.split) - 1) >> p.split;
+      const int each = rounds <= WHOLE ? rounds : even <= LONG ? even : max(least, LONG);
+      begin = (int)(me / items) * each * WAVES;
       if (begin >= span.steps) return;
       stop = min(span.steps, begin + each * WAVES);
       item_parts = (span.steps + each * WAVES - 1) / (each * WAVES);
@@ -434,7 +446,7 @@ __device__ __forceinline__ void attn_kv4_work(const Args& p) {
       }
       const int step = min(s + lane / TILES * WAVES, span.steps - 1), i = (first_token(step) + lane % TILES * 16) >> p.kv.page_shift;
       if (i >= p.kv.max_pages) return Tile{-1, 0};
-      const int row = MODE == kAttnBoth && step < span.sink_steps ? b - b % row_group(p) : table_row(b);
+      const int row = MODE == kAttnOwn && step < span.sink_steps ? b - b % row_group(p) : table_row(b);
       const size_t at_page = (size_t)row * p.kv.max_pages + i;
       return Tile{p.kv.table != nullptr ? p.kv.table[at_page] : (int)at_page, 0};
     };
@@ -594,9 +606,9 @@ __device__ __forceinline__ void attn_kv4_work(const Args& p) {
       const int t_next = token_of(s + WAVES, k);       // (the last one's loads repeat a step)
       const Pages next = pages_of(k);
       // every token of the step in sight of every row
-      const bool front = MODE == kAttnBoth && s < span.sink_steps;        // of the shared tokens
+      const bool front = MODE == kAttnOwn && s < span.sink_steps;        // of the shared tokens
       const bool whole = pages.there == (1u << TILES) - 1 && t + STEP - 1 <= (front ? min(span.lo, here.from - 1) : span.lo) &&
-                         (MODE == kAttnRest || MODE == kAttnBoth ? front || t >= here.from : MODE != kAttnWhole || p.window == 0 || t > behind_window(p, span.hi) || t + STEP <= p.sinks);
+                         (MODE == kAttnOwn ? front || t >= here.from : MODE != kAttnWhole || p.window == 0 || t > behind_window(p, span.hi) || t + STEP <= p.sinks);
       v4f sc[NB][TILES];
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb)
@@ -646,7 +658,7 @@ __device__ __forceinline__ void attn_kv4_work(const Args& p) {
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
           const int at_row = front ? min(position(nb), here.from - 1) : position(nb);
-          const int behind = MODE == kAttnRest || (MODE == kAttnBoth && !front) ? here.from - 1 : MODE == kAttnWhole && p.window > 0 ? behind_window(p, at_row) : -1;
+          const int behind = MODE == kAttnOwn && !front ? here.from - 1 : MODE == kAttnWhole && p.window > 0 ? behind_window(p, at_row) : -1;
 #pragma unroll
           for (int x = 0; x < NX; ++x) {
             const int tok = t + ((x >> 2) * F + mine_tile) * 16 + 4 * kb + (x & 3);
@@ -777,8 +789,8 @@ __device__ __forceinline__ void attn_kv4_work(const Args& p) {
     const bool shared = begin > 0 || stop < span.steps;
     uint32_t w0 = me, w1 = me;                // the workgroups that hold a part of it
     if constexpr (FIXED) {
-      w0 = item << p.split;
-      w1 = w0 + (uint32_t)item_parts - 1;
+      w0 = 0;                                 // (by their numbers)
+      w1 = (uint32_t)item_parts - 1;
     } else if (shared) {
       w0 = group_of(item + OVER + WAVES - 1);
       w1 = group_of(item + OVER + span.steps - 1);
@@ -792,9 +804,9 @@ __device__ __forceinline__ void attn_kv4_work(const Args& p) {
         *reinterpret_cast<float4*>(part + 4 + own) = float4{v[0], v[1], v[2], v[3]};
         return;
       }
-      if constexpr (MODE == kAttnRest) {
+      if constexpr (MODE == kAttnOwn) {
         const int set = b / p.group, in_set = ((b - set * p.group) * p.rows + j) * p.G + g;
-        const int2 item_of = p.first_items[(size_t)(set * p.first_blocks + (in_set >> p.first_shift)) * Hkv + head];
+        const int2 item_of = here.joined ? p.first_items[(size_t)(set * p.first_blocks + (in_set >> p.first_shift)) * Hkv + head] : int2{0, 0};
         const int n = span.lo + j - over_group(p, block * RB) < 0 ? 0 : item_of.y;      // (a row in front of its sequence has seen nothing)
         constexpr int FLY = 4;
         for (int i0 = 0; i0 < n; i0 += FLY) {
@@ -909,12 +921,13 @@ __device__ __forceinline__ void attn_kv4_work(const Args& p) {
     // ---- the last of the item's workgroups joins their parts; of many parts, the last of each eight theirs first (a
     // workgroup reads parts past the caches at tens of GB/s: 64 parts of 8 rows in one go take 14 us)
     const uint32_t parts = w1 - w0 + 1;
-    const auto slot_of = [&](uint32_t w) { return FIXED ? w : w == w0 ? 2 * w0 + (start_of(w0) < item ? 1 : 0) : 2 * w; };
+    const auto slot_of = [&](uint32_t w) { return FIXED ? w * items + item : w == w0 ? 2 * w0 + (start_of(w0) < item ? 1 : 0) : 2 * w; };
 #pragma unroll 1
     for (int stage = parts > 16 ? 0 : 1; shared && stage < 2; ++stage) {
       if constexpr (MODE == kAttnPrefix) break;
       uint32_t first = w0, stride = 1, n = parts, counter = w0;
-      if (stage == 0) {
+      if constexpr (FIXED) counter = item;
+      if (!FIXED && stage == 0) {
         first = w0 + ((me - w0) & ~7u);
         n = min(8u, w1 + 1 - first);
         // One on its own has its part in place already.  It must not count: the next item's first eight may begin with this

@@ -113,6 +113,7 @@ constexpr int kNumCU = 256;
 //                                   wavefronts of a workgroup (8, or 4 where that instance exists)
 //   QSPEC_STREAM_MAX_W4A4 / _W4A16  the streaming kernels take every M up to this one and none above
 //   QSPEC_TILE_W4A4 / _W4A16        "shape,S": workgroup shape index, K-slices
+//   QSPEC_ATTN_SHARED               shared tokens from which on qspec_attn_kv4_shared reads them once for all of a group
 struct PlanOverrides {
   bool generic = false;
   int stream_fields[2] = {0, 0};      // [w4a4]: how many of nt, S, ms, waves were given (0: no override)
@@ -120,6 +121,7 @@ struct PlanOverrides {
   int stream_max[2] = {0, 0};         // 0: the default bound
   bool tile_set[2] = {false, false};
   int tile[2][2] = {{0, 0}, {0, 0}};
+  int attn_shared = -1;               // below 0: by cost
   unsigned mlp_spin = 0;              // 0: the default number of polls of the persistent MLP kernel's wait
 };
 
@@ -127,6 +129,7 @@ struct PlanOverrides {
 bool apply_override(PlanOverrides& o, const char* name, const char* value) {
   if (strcmp(name, "QSPEC_KERNEL") == 0) { o.generic = value && strcmp(value, "generic") == 0; return true; }
   if (strcmp(name, "QSPEC_MLP_SPIN") == 0) { o.mlp_spin = value ? (unsigned)strtoul(value, nullptr, 10) : 0u; return true; }
+  if (strcmp(name, "QSPEC_ATTN_SHARED") == 0) { o.attn_shared = value ? atoi(value) : -1; return true; }
   for (int w4a4 = 0; w4a4 < 2; ++w4a4) {
     if (strcmp(name, w4a4 ? "QSPEC_STREAM_W4A4" : "QSPEC_STREAM_W4A16") == 0) {
       int* f = o.stream[w4a4];
@@ -153,7 +156,7 @@ bool apply_override(PlanOverrides& o, const char* name, const char* value) {
 
 constexpr const char* kOverrideNames[] = {"QSPEC_KERNEL", "QSPEC_STREAM_W4A4", "QSPEC_STREAM_W4A16",
                                           "QSPEC_STREAM_MAX_W4A4", "QSPEC_STREAM_MAX_W4A16",
-                                          "QSPEC_TILE_W4A4", "QSPEC_TILE_W4A16", "QSPEC_MLP_SPIN"};
+                                          "QSPEC_TILE_W4A4", "QSPEC_TILE_W4A16", "QSPEC_MLP_SPIN", "QSPEC_ATTN_SHARED"};
 
 PlanOverrides& overrides() {
   static PlanOverrides o = [] {
@@ -875,9 +878,6 @@ void launch_attn(const AttnArgs& a, AttnPlan plan, hipStream_t s) {
   else launch_attn_inst<D, 4, 1>(a, s);
 }
 
-// Rounds of its four wavefronts up to which an item is not shared out: joins cost more (us, 4 sequences of 32 heads: 573 tokens 9.2 for 11.5, 1085 tokens 13.8 for 12.7).
-constexpr int kAttnWholeRounds = 3;
-
 template <int D, int MODE>
 void launch_attn_part(const AttnPartArgs& a, AttnPlan plan, hipStream_t s, unsigned workgroups = AttnForm<1, 1>::workgroups) {
   const dim3 grid(workgroups), threads(64 * AttnForm<1, 1>::waves);
@@ -913,6 +913,8 @@ bool attn_counts(const AttnArgs& a, long long tokens) { return (long long)a.B * 
 // (the bounds of the scale keep every score inside binary32, and off the reference of a row that has seen nothing)
 inline bool scale_fits(float scale) { return scale >= 1e-10f && scale <= 1e10f; }
 
+// Parts of items that a call has places and counters for.
+inline long long attn_most_parts(AttnPlan plan) { return plan.nb == 4 ? 2048 : 4096; }
 // A call's workspace: what the second launch has for itself, then the first one's partial sums, their directory, and those that are whole.
 struct SharedWorkspace { size_t parts, items, joint, bytes; };
 SharedWorkspace attn_shared_workspace(int B, int T, int Hq, int Hkv, int D, int groups) {
@@ -922,7 +924,7 @@ SharedWorkspace attn_shared_workspace(int B, int T, int Hq, int Hkv, int D, int 
   const size_t items = (size_t)groups * (((size_t)rows * G + block - 1) / block) * Hkv;
   const auto up = [](size_t n) { return (n + 255) & ~(size_t)255; };
   SharedWorkspace w;
-  w.parts = up(attn_workspace_bytes(T, G, D) * 2);        // (places for up to 2048 parts)
+  w.parts = up(attn_workspace_bytes(T, G, D) * (attn_plan(T, G).nb == 4 ? 2 : 4));        // (places for attn_most_parts)
   w.items = w.parts + up(attn_workspace_bytes(rows, G, D) - kAttnTicketBytes);
   w.joint = w.items + up(items * sizeof(int2));
   w.bytes = w.joint + (size_t)B * T * Hq * attn_part_floats(D) * sizeof(float);
@@ -933,14 +935,14 @@ double attn_token_ps(AttnPlan plan, int D) {
   static constexpr double ps[2][5] = {{9, 11, 13, 18, 32}, {11.5, 13.7, 18, 23, 39}};
   return ps[D == 128][plan.f == 4 ? 0 : plan.f == 2 ? 1 : plan.nb == 1 ? 2 : plan.nb == 2 ? 3 : 4];
 }
-// Whether every sequence reads the shared tokens for itself, in one launch, instead of one for all and a second launch: what the first of the two
-// saves at most, with the longest contexts that the tables hold, is less than the second one and its joins cost (8 us and 20 ns an item).  Measured, one launch
-// and two (us): 4 samples of 500 tokens, 32 heads 9.3 and 15.7; 8 users of 2000, 4 rows, 32 heads 18.6 and 23.3; 16 prompts of 1500 to 6000 by 8 samples, 4 rows, 64 over 8
-// heads of 64 108 and 112; 128 users, one row of 64 over 8 heads: of 2048 tokens 40 and 47, of 4000 66 and 60, of 8197 133 and 93.
-bool shared_in_one(const AttnPartArgs& first, AttnPlan first_plan, const AttnPartArgs& own, AttnPlan own_plan, int D, long long tokens) {
+// From how many shared tokens on they are read once for all of a group, in a launch of its own: what that saves passes what the second launch and its joins
+// cost (8 us and 20 ns an item).  Measured, each sequence reading them for itself and one reading for all (us): 4 samples of 500 tokens, 32 heads 9.3 and 15.7; 8 users of 2000, 4 rows, 32 heads
+// 18.6 and 23.3; 16 prompts of 1500 to 6000 by 8 samples, 4 rows, 64 over 8 heads of 64 108 and 112; 128 users, one row of 64 over 8 heads: of 2048 tokens 40 and 47,
+// of 4000 66 and 60, of 8197 133 and 93.
+int least_shared(const AttnArgs& first, AttnPlan first_plan, const AttnArgs& own, AttnPlan own_plan, int D) {
   const double alone = (double)own.B * own.blocks * attn_token_ps(own_plan, D), together = (double)first.B * first.blocks * attn_token_ps(first_plan, D);
-  const double items = (double)own.B * own.blocks * own.kv.Hkv;
-  return (alone - together) * own.kv.Hkv * (double)tokens <= 8e6 + 2e4 * items;
+  const double items = (double)own.B * own.blocks * own.kv.Hkv, saved = (alone - together) * own.kv.Hkv, tokens = saved > 0 ? (8e6 + 2e4 * items) / saved : 1e9;
+  return tokens < 1e9 ? (int)tokens + 1 : 1000000000;
 }
 
 int check_attn_shared(int B, int T, int Hq, int Hkv, int D, int groups) {
@@ -1410,9 +1412,9 @@ int qspec_attn_kv4_shared(const void* q_f16, const void* cache, const int32_t* p
   uint8_t* const base = static_cast<uint8_t*>(workspace);
   const AttnPlan plan = attn_plan(T * group, G), rest_plan = attn_plan(T, G);
   KvShape kv = kv_shape(pos, page_table, T * group, Hkv, page_size, max_pages, n_pages);
-  AttnPartArgs first{attn_args(kv, q_f16, cache, out_f16, workspace, groups, Hq, plan, scale, 0, 0), T, group, shared,
+  AttnPartArgs first{attn_args(kv, q_f16, cache, out_f16, workspace, groups, Hq, plan, scale, 0, 0), T, group, shared, 0,
                      reinterpret_cast<float*>(base + w.joint), reinterpret_cast<float*>(base + w.parts), reinterpret_cast<int2*>(base + w.items),
-                     log2_exact(16 * plan.nb / plan.f), 0, nullptr, 0, 0, kAttnWholeRounds};
+                     log2_exact(16 * plan.nb / plan.f), 0, nullptr, 0, 0, 0};
   first.first_blocks = first.blocks;
   first.parts = first.first_parts;
   kv.T = T;
@@ -1422,27 +1424,24 @@ int qspec_attn_kv4_shared(const void* q_f16, const void* cache, const int32_t* p
   if (!attn_counts(first, tokens) || !attn_counts(rest, tokens)) return QSPEC_ERR_SHAPE;
   if (int st = check_device()) return st;
   const hipStream_t s = static_cast<hipStream_t>(stream);
+  first.least_shared = overrides().attn_shared >= 0 ? overrides().attn_shared : least_shared(first, plan, rest, rest_plan, D);
+  const bool once = first.least_shared < tokens;         // (where no group can share so many, there is nothing to launch)
+  rest.least_shared = once ? first.least_shared : 0x7fffffff;
+  // A part of an item to every compute unit.  Long rows may leave one sequence with most of the work: its items are divided further (us, 30000 tokens beside 15
+  // sequences of 1300, one row of 64 over 8 heads: 34, 100 without, 21 as the device divides the work of qspec_attn_kv4; beside 127 of them 82, 102 and 54).
   const long long items = (long long)B * rest.blocks * Hkv;
-  // A part of an item to every compute unit.  Long rows may leave one sequence with most of the work: its items are divided further, from 16 rounds on.
-  while (rest.split < 4 && items << (rest.split + 1) <= 256) ++rest.split;
-  while (rest.split < 4 && items << (rest.split + 1) <= 2048 && tokens >> rest.split > 16384) { ++rest.split; rest.whole_rounds = 16; }
+  while (rest.fill < 4 && items << (rest.fill + 1) <= 256) ++rest.fill;
+  rest.split = rest.fill;
+  while (rest.split < 4 && items << (rest.split + 1) <= attn_most_parts(rest_plan) && tokens >> rest.split > 2048) ++rest.split;
   const unsigned workgroups = (unsigned)(items << rest.split);
-  if (shared_in_one(first, plan, rest, rest_plan, D, tokens)) {
-    // a whole item to a compute unit: eight wavefronts (us, 256 items of 2300 tokens 16.4 for 18.8, of 4000 tokens 21.3 for 25.4)
-    if (rest.split == 0 && items <= 256 && rest_plan.nb < 4) {
-      if (D == 128) launch_attn_waves<128, kAttnBoth, 8>(rest, rest_plan, s, workgroups);
-      else launch_attn_waves<64, kAttnBoth, 8>(rest, rest_plan, s, workgroups);
-    } else if (D == 128) launch_attn_part<128, kAttnBoth>(rest, rest_plan, s, workgroups);
-    else launch_attn_part<64, kAttnBoth>(rest, rest_plan, s, workgroups);
-    return launch_status();
-  }
-  if (D == 128) {
-    launch_attn_part<128, kAttnPrefix>(first, plan, s);
-    launch_attn_part<128, kAttnRest>(rest, rest_plan, s, workgroups);
-  } else {
-    launch_attn_part<64, kAttnPrefix>(first, plan, s);
-    launch_attn_part<64, kAttnRest>(rest, rest_plan, s, workgroups);
-  }
+  if (once && D == 128) launch_attn_part<128, kAttnPrefix>(first, plan, s);
+  else if (once) launch_attn_part<64, kAttnPrefix>(first, plan, s);
+  // a whole item to a compute unit: eight wavefronts (us, 256 items of 2300 tokens 16.4 for 18.8, of 4000 tokens 21.3 for 25.4)
+  if (rest.fill == 0 && items <= 256 && rest_plan.nb < 4) {
+    if (D == 128) launch_attn_waves<128, kAttnOwn, 8>(rest, rest_plan, s, workgroups);
+    else launch_attn_waves<64, kAttnOwn, 8>(rest, rest_plan, s, workgroups);
+  } else if (D == 128) launch_attn_part<128, kAttnOwn>(rest, rest_plan, s, workgroups);
+  else launch_attn_part<64, kAttnOwn>(rest, rest_plan, s, workgroups);
   return launch_status();
 }
 
@@ -1472,7 +1471,7 @@ int qspec_attn_kv4_blocks(const void* q_f16, const void* cache, const int32_t* p
   const bool single = plan.nb < 4 && (items >= 2048 || (items >= 1024 && steps <= 8));
   int split = 0;
   while (!single && split < 4 && items << (split + 1) <= 256 && steps >> (split + 1) >= 4) ++split;
-  const AttnPartArgs a{common, T, 1, nullptr, nullptr, nullptr, nullptr, 0, 0, pages, count, split, kAttnWholeRounds};
+  const AttnPartArgs a{common, T, 1, nullptr, 0, nullptr, nullptr, nullptr, 0, 0, pages, count, split, split};
   if (int st = check_device()) return st;
   const hipStream_t s = static_cast<hipStream_t>(stream);
   const unsigned workgroups = (unsigned)(items << split);

@@ -2,6 +2,8 @@
 
 How far an output may be off: as in the attention of one sequence (tests/test_gpu_attn_kv4.py), and for the join of the two parts' sums, in
 binary32, a dozen roundings of numbers no larger than the values: 16 * 2^-24 of the largest."""
+import contextlib
+
 import numpy as np
 import pytest
 
@@ -67,19 +69,23 @@ def compare(got, cache, q, pos, table, shared, scale=None, rows=None):
 
 
 def check(env, cache, q, pos, table, shared, scale=None, no_table=False, workspace=None, rows=None, raw=None):
-    """In one launch or two as the library chooses by the length of the table's rows; rows that are long, of which the far pages are not there, take two."""
+    """Each sequence with its own reading of the shared tokens, and one reading for all of a group."""
     torch, B = env
-    if not no_table and workspace is None and table.shape[1] * cache.P <= 4096:
-        check_one(env, cache, q, pos, far(table, cache.P), shared, scale, False, None, rows, raw, len_=table.shape[1])
+    with once_for_all(B):
+        check_one(env, cache, q, pos, table, shared, scale, no_table, workspace, rows, raw)
     return check_one(env, cache, q, pos, table, shared, scale, no_table, workspace, rows, raw)
 
 
-def far(table, P):
-    """The table's rows with room for 2^19 tokens, behind their own pages none."""
-    return np.concatenate((table, np.full((len(table), (1 << 19) // P - table.shape[1]), -1)), 1)
+@contextlib.contextmanager
+def once_for_all(B, tokens=0):
+    B.debug_set_plan("QSPEC_ATTN_SHARED", str(tokens))
+    try:
+        yield
+    finally:
+        B.debug_set_plan("QSPEC_ATTN_SHARED", None)
 
 
-def check_one(env, cache, q, pos, table, shared, scale=None, no_table=False, workspace=None, rows=None, raw=None, len_=None):
+def check_one(env, cache, q, pos, table, shared, scale=None, no_table=False, workspace=None, rows=None, raw=None):
     torch, B = env
     Bn, T, Hq, D = q.shape
     guard = torch.full((q.size + 64,), 123.0, dtype=torch.float16, device="cuda")
@@ -89,7 +95,7 @@ def check_one(env, cache, q, pos, table, shared, scale=None, no_table=False, wor
                       cache.Hkv, cache.P, None if no_table else dev(torch, table.astype(np.int32)), scale, out=out, workspace=workspace)
     torch.cuda.synchronize()
     assert (guard[:32] == 123.0).all() and (guard[-32:] == 123.0).all()
-    compare(out.cpu().numpy().astype(np.float64), cache, q, pos, table[:, :len_], shared, scale, rows)
+    compare(out.cpu().numpy().astype(np.float64), cache, q, pos, table, shared, scale, rows)
     return out
 
 
@@ -120,6 +126,32 @@ def test_an_item_to_a_compute_unit(env, groups, per, T, Hq, Hkv, D, n):
     used, inverse = np.unique(table, return_inverse=True)
     c = Cache(T + D, len(used), Hkv, D, P)
     check(env, c, queries(D, Bn, T, Hq, D), pos, inverse.reshape(table.shape), shared, rows=range(0, Bn, 5))
+
+
+@pytest.mark.parametrize("T", [1, 3])
+def test_groups_that_share_little_beside_groups_that_share_much(env, T):
+    torch, B = env
+    P, per, shared, Hkv, D = 64, 3, [700, 40, 0, 399, 400, -3], 2, 64
+    rng = np.random.default_rng(T)
+    pos = np.repeat(np.maximum(shared, 0), per) + rng.integers(-2, 300, len(shared) * per)
+    each = -(-(int(pos.max()) + T) // P)
+    table = tables(1, len(shared), per, each, P, shared, len(pos) * each)
+    c = Cache(T, len(pos) * each, Hkv, D, P)
+    for tokens in (400, 701, 1 << 20):
+        with once_for_all(B, tokens):
+            check_one(env, c, queries(D, len(pos), T, 4, D), pos, table, shared)
+
+
+def test_one_long_sequence_among_short_ones(env):
+    """Its items have more parts than theirs."""
+    P, per, shared, D = 256, 9, [300], 64
+    pos = np.array([20011, 300, 310, 400, 299, 5000, 1000, 350, 12345])
+    each = -(-(int(pos.max()) + 2) // P)
+    table = np.full((per, each), -1)
+    for i in range(per):
+        table[i, :-(-(int(pos[i]) + 2) // P)] = np.arange(-(-(int(pos[i]) + 2) // P)) + table.max() + 1
+    c = Cache(3, int(table.max()) + 1, 16, D, P)
+    check(env, c, queries(4, per, 2, 16, D), pos, table, shared)
 
 
 @pytest.mark.parametrize("T", [1, 6])
@@ -172,11 +204,10 @@ def test_long_sequences_are_shared_out_and_joined(env, groups, per, T, Hq, Hkv, 
     assert int(ws[:16384].count_nonzero()) == 0
     again = check(*args, workspace=ws, rows=[0])
     assert torch.equal(first, again)
-    args = args[:4] + (far(table, P), shared)                 # in two launches
-    first = check_one(*args, workspace=ws, rows=range(0, Bn, 7), len_=each)
-    assert int(ws[:16384].count_nonzero()) == 0
-    again = check_one(*args, workspace=ws, rows=[0], len_=each)
-    assert torch.equal(first, again)
+    with once_for_all(B):
+        first = check_one(*args, workspace=ws, rows=range(0, Bn, 7))
+        assert int(ws[:16384].count_nonzero()) == 0
+        assert torch.equal(first, check_one(*args, workspace=ws, rows=[0]))
 
 
 def test_agrees_with_the_attention_of_each_alone(env):
@@ -219,8 +250,9 @@ def test_rows_nobody_sees_may_hold_anything(env, T):
     got = check(env, c, queries(T, 2, T, 3, D), pos, table, shared, raw=bad.bytes())
     torch, _ = env
     assert torch.equal(want, got)
-    args = (env, c, queries(T, 2, T, 3, D), pos, far(table, P), shared)
-    assert torch.equal(check_one(*args, len_=each), check_one(*args, len_=each, raw=bad.bytes()))
+    with once_for_all(env[1]):
+        args = (env, c, queries(T, 2, T, 3, D), pos, table, shared)
+        assert torch.equal(check_one(*args), check_one(*args, raw=bad.bytes()))
 
 
 @pytest.mark.parametrize("bad", [60000.0, np.inf, np.nan])
@@ -246,8 +278,11 @@ def test_what_is_no_number_shows_where_it_is_seen(env):
     q = queries(3, 4, 1, Hq, D)
 
     def run(q, c):
-        one, two = (B.attn_kv4_shared(dev(torch, q), dev(torch, c.bytes()), dev(torch, pos.astype(np.int32)), dev(torch, np.array(shared, np.int32)), Hkv, P,
-                                      dev(torch, t.astype(np.int32))).isnan().cpu().numpy() for t in (table, far(table, P)))
+        call = lambda: B.attn_kv4_shared(dev(torch, q), dev(torch, c.bytes()), dev(torch, pos.astype(np.int32)), dev(torch, np.array(shared, np.int32)), Hkv, P,
+                                         dev(torch, table.astype(np.int32))).isnan().cpu().numpy()
+        one = call()
+        with once_for_all(B):
+            two = call()
         assert (one == two).all()
         return one
 
@@ -272,14 +307,20 @@ def test_what_is_no_number_shows_where_it_is_seen(env):
     assert (got == want).all()
 
 
-@pytest.mark.parametrize("long_rows", [False, True])
-def test_two_streams_with_a_workspace_each_and_a_graph(env, long_rows):
+@pytest.mark.parametrize("tokens", [0, 900, 1 << 30])
+def test_two_streams_with_a_workspace_each_and_a_graph(env, tokens):
+    """One reading of the shared tokens for all of a group, of the groups that share 900 and more, of none."""
+    with once_for_all(env[1], tokens):
+        two_streams_and_a_graph(env)
+
+
+def two_streams_and_a_graph(env):
     torch, B = env
     groups, per, T, Hq, Hkv, D, P, n = 2, 3, 4, 8, 2, 128, 64, 2500
     Bn, each = groups * per, -(-n // P)
     c = Cache(20, Bn * each, Hkv, D, P)
     table = np.random.default_rng(1).permutation(Bn * each).reshape(Bn, each)
-    cache, tab = dev(torch, c.bytes()), dev(torch, (far(table, P) if long_rows else table).astype(np.int32))
+    cache, tab = dev(torch, c.bytes()), dev(torch, table.astype(np.int32))
     pos = torch.tensor([2400, 2000, 2100, 1000, 1500, 2496], dtype=torch.int32, device="cuda")
     shared = torch.tensor([1999, 1000], dtype=torch.int32, device="cuda")
     size = B.attn_kv4_shared_workspace_bytes(Bn, T, Hq, Hkv, D, groups)
@@ -368,8 +409,9 @@ def test_caches_of_more_than_four_gib(env):
     at, tab = dev(torch, pos.astype(np.int32)), dev(torch, table.astype(np.int32))
     shared = [300]
     small.k[2, :, :44], small.v[2, :, :44] = 0, 0             # (not read: shared)
-    for t in (tab, dev(torch, far(table, P).astype(np.int32))):
-        got = B.attn_kv4_shared(dev(torch, q), cache, at, dev(torch, np.array(shared, np.int32)), Hkv, P, t)
+    for tokens in (0, 1 << 30):
+        with once_for_all(B, tokens):
+            got = B.attn_kv4_shared(dev(torch, q), cache, at, dev(torch, np.array(shared, np.int32)), Hkv, P, tab)
         compare(got.cpu().numpy().astype(np.float64), small, q, pos, small_table, shared)
     small = Cache(17, 4, Hkv, D, P)
     one = dev(torch, np.array([[where[3], where[0]], [where[2], where[1]]], dtype=np.int32))
@@ -396,14 +438,17 @@ def test_one_workspace_serves_all_in_turn(env):
     c = Cache(24, 40, 2, 128, 64)
     cache, pos, q = dev(torch, c.bytes()), torch.tensor([2500, 2000], dtype=torch.int32, device="cuda"), dev(torch, queries(25, 2, 1, 8, 128))
     table = torch.arange(40, dtype=torch.int32, device="cuda").repeat(2, 1)
-    long_table = torch.full((2, 1 << 13), -1, dtype=torch.int32, device="cuda")
-    long_table[:, :40] = table
+
+    def shared_once(w):
+        with once_for_all(B):
+            return B.attn_kv4_shared(q, cache, pos, shared, 2, 64, table, workspace=w)
+
     shared = torch.tensor([1900], dtype=torch.int32, device="cuda")
     blocks = torch.arange(0, 40, 2, dtype=torch.int32, device="cuda").repeat(2, 1, 2, 1)
     ws = B.alloc_workspace(max(B.workspace_bytes(M, N, K), B.attn_kv4_workspace_bytes(2, 1, 8, 2, 128), B.attn_kv4_shared_workspace_bytes(2, 1, 8, 2, 128, 1),
                                B.attn_kv4_blocks_workspace_bytes(2, 1, 8, 2, 128)))
     calls = [lambda w: B.gemm_w4a16(blob, xd, N, workspace=w), lambda w: B.attn_kv4(q, cache, pos, 2, 64, table, workspace=w),
-             lambda w: B.attn_kv4_shared(q, cache, pos, shared, 2, 64, table, workspace=w), lambda w: B.attn_kv4_shared(q, cache, pos, shared, 2, 64, long_table, workspace=w),
+             lambda w: B.attn_kv4_shared(q, cache, pos, shared, 2, 64, table, workspace=w), shared_once,
              lambda w: B.attn_kv4_blocks(q, cache, pos, blocks, 2, 64, table, workspace=w)]
     alone = [call(None) for call in calls]
     for _ in range(3):

@@ -133,21 +133,25 @@ def test_parts_of_an_item_take_every_step_once():
     waited for."""
     source = re.sub(r"//.*", "", open(os.path.join(build.HERE, "csrc", "attn_kv4.hpp")).read())
     block = source[source.index("if constexpr (FIXED) {\n      const int rounds"):]
-    expression = lambda text: eval_of(re.search(text, block).group(1))
-    eval_of = lambda e: re.sub(r"(.*) \? (.*) : (.*)", r"((\2) if \1 else (\3))", e.replace("/", "//").replace("span.steps", "steps").replace("p.split", "split").replace("p.whole_rounds", "whole"))
-    rounds_of, each_of, parts_of = (expression(r"const int rounds = ([^,;]*),"), expression(r"each = ([^;]*);"), expression(r"item_parts = ([^;]*);"))
-    begin_of = expression(r"begin = \(int\)\(me - \(item << p.split\)\) \* ([^;]*);")
-    assert "if (begin >= span.steps) return;" in block and "stop = min(span.steps, begin + each * WAVES);" in block
-    for WAVES in (1, 4):
-        for whole in (3, 16):
-            for split in range(5):
+    whole, long_ = map(int, re.search(r"constexpr int WHOLE = (\d+), LONG = (\d+);", source).groups())
+
+    def formula(text):
+        e = re.search(text, block).group(1).replace("/", "//").replace("span.steps", "steps").replace("p.split", "split").replace("p.fill", "fill")
+        e = re.sub(r"(.*?) \? (.*?) : (.*?) \? (.*?) : (.*)", r"((\2) if \1 else (\4) if \3 else (\5))", e)
+        return compile(e, "formula", "eval")
+
+    rounds_of, even_of, least_of, each_of, parts_of = (formula(t) for t in (r"const int rounds = ([^,;]*),", r"even = ([^,;]*),", r"least = ([^,;]*);", r"const int each = ([^;]*);", r"item_parts = ([^;]*);"))
+    assert "begin = (int)(me / items) * each * WAVES;" in block and "if (begin >= span.steps) return;" in block and "stop = min(span.steps, begin + each * WAVES);" in block
+    for WAVES in (1, 4, 8):
+        for fill in range(5):
+            for split in range(fill, 5):
                 for steps in list(range(1, 300)) + [1000, 1023, 1024, 1025, 65536]:
-                    names = dict(WAVES=WAVES, whole=whole, split=split, steps=steps)
-                    names["rounds"] = eval(rounds_of, {}, names)
-                    names["each"] = eval(each_of, {}, names)
+                    names = dict(WAVES=WAVES, WHOLE=whole, LONG=long_, fill=fill, split=split, steps=steps, max=max)
+                    for name, code in (("rounds", rounds_of), ("even", even_of), ("least", least_of), ("each", each_of)):
+                        names[name] = eval(code, {}, names)
                     parts, at = eval(parts_of, {}, names), 0
                     for part in range(1 << split):
-                        begin = part * eval(begin_of, {}, names)
+                        begin = part * names["each"] * WAVES
                         if begin >= steps:
                             assert part >= parts
                             continue
