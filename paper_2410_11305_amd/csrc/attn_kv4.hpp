@@ -226,7 +226,7 @@ __device__ __forceinline__ void attn_kv4_work(const Args& p) {
   // (joins cost more: 4 sequences of 32 heads, 573 tokens 9.2 us for 11.5, 1085 tokens 13.8 for 12.7), has 2^fill parts from there on, and more where these would be longer than LONG: a
   // long one among short ones holds the launch up.
   constexpr bool FIXED = MODE == kAttnPages || MODE == kAttnOwn;
-  constexpr int WHOLE = 3, LONG = 8;
+  constexpr int WHOLE = 3, LONG = F > 1 ? 8 : 64;      // (more rows: joins of more than a few thousand tokens' parts save nothing either)
   static_assert(FIXED || LEAST >= 2 * WAVES, "no workgroup's share rounds down to nothing");
   constexpr int NK = D / 32;                  // matrix instructions of a tile of q k^T; words of a lane of a key
   constexpr int NV = D / 16;                  // matrix instructions of two tiles of p v
@@ -395,8 +395,15 @@ __device__ __forceinline__ void attn_kv4_work(const Args& p) {
     entry = (int)uniform(i / (uint32_t)Hkv);
     head = (int)(i - (uint32_t)entry * (uint32_t)Hkv);
   };
-  if constexpr (FIXED) {                      // (first parts first: of the others few are needed)
-    item = me % items;
+  uint32_t part_of_item = 0;
+  if constexpr (FIXED) {
+    if constexpr (MODE == kAttnOwn) {         // first parts first: of the others few are needed
+      part_of_item = uniform(me / items);
+      item = me - part_of_item * items;
+    } else {
+      item = me >> p.split;
+      part_of_item = me - (item << p.split);
+    }
     entry = (int)uniform(item / (uint32_t)Hkv);
     head = (int)(item - (uint32_t)entry * (uint32_t)Hkv);
   } else if (whole_items) {
@@ -420,7 +427,7 @@ __device__ __forceinline__ void attn_kv4_work(const Args& p) {
     if constexpr (FIXED) {
       const int rounds = (span.steps + WAVES - 1) / WAVES, even = (rounds + (1 << p.fill) - 1) >> p.fill, least = (rounds + (1 << p.split) - 1) >> p.split;
       const int each = rounds <= WHOLE ? rounds : even <= LONG ? even : max(least, LONG);
-      begin = (int)(me / items) * each * WAVES;
+      begin = (int)part_of_item * each * WAVES;
       if (begin >= span.steps) return;
       stop = min(span.steps, begin + each * WAVES);
       item_parts = (span.steps + each * WAVES - 1) / (each * WAVES);
@@ -921,12 +928,12 @@ __device__ __forceinline__ void attn_kv4_work(const Args& p) {
     // ---- the last of the item's workgroups joins their parts; of many parts, the last of each eight theirs first (a
     // workgroup reads parts past the caches at tens of GB/s: 64 parts of 8 rows in one go take 14 us)
     const uint32_t parts = w1 - w0 + 1;
-    const auto slot_of = [&](uint32_t w) { return FIXED ? w * items + item : w == w0 ? 2 * w0 + (start_of(w0) < item ? 1 : 0) : 2 * w; };
+    const auto slot_of = [&](uint32_t w) { return MODE == kAttnPages ? me - part_of_item + w : FIXED ? w * items + item : w == w0 ? 2 * w0 + (start_of(w0) < item ? 1 : 0) : 2 * w; };
 #pragma unroll 1
     for (int stage = parts > 16 ? 0 : 1; shared && stage < 2; ++stage) {
       if constexpr (MODE == kAttnPrefix) break;
       uint32_t first = w0, stride = 1, n = parts, counter = w0;
-      if constexpr (FIXED) counter = item;
+      if constexpr (FIXED) counter = item << p.split;        // (apart: neighbouring counters share a line, 64 of 2048 pages 11.4 us for 10.5)
       if (!FIXED && stage == 0) {
         first = w0 + ((me - w0) & ~7u);
         n = min(8u, w1 + 1 - first);

@@ -1432,7 +1432,7 @@ int qspec_attn_kv4_shared(const void* q_f16, const void* cache, const int32_t* p
   const long long items = (long long)B * rest.blocks * Hkv;
   while (rest.fill < 4 && items << (rest.fill + 1) <= 256) ++rest.fill;
   rest.split = rest.fill;
-  while (rest.split < 4 && items << (rest.split + 1) <= attn_most_parts(rest_plan) && tokens >> rest.split > 2048) ++rest.split;
+  while (rest.split < 4 && items << (rest.split + 1) <= attn_most_parts(rest_plan) && tokens >> rest.split > (rest.split == rest.fill ? 4096 : 2048)) ++rest.split;
   const unsigned workgroups = (unsigned)(items << rest.split);
   if (once && D == 128) launch_attn_part<128, kAttnPrefix>(first, plan, s);
   else if (once) launch_attn_part<64, kAttnPrefix>(first, plan, s);

@@ -133,7 +133,7 @@ def test_parts_of_an_item_take_every_step_once():
     waited for."""
     source = re.sub(r"//.*", "", open(os.path.join(build.HERE, "csrc", "attn_kv4.hpp")).read())
     block = source[source.index("if constexpr (FIXED) {\n      const int rounds"):]
-    whole, long_ = map(int, re.search(r"constexpr int WHOLE = (\d+), LONG = (\d+);", source).groups())
+    whole, *longs = map(int, re.search(r"constexpr int WHOLE = (\d+), LONG = F > 1 \? (\d+) : (\d+);", source).groups())
 
     def formula(text):
         e = re.search(text, block).group(1).replace("/", "//").replace("span.steps", "steps").replace("p.split", "split").replace("p.fill", "fill")
@@ -141,8 +141,8 @@ def test_parts_of_an_item_take_every_step_once():
         return compile(e, "formula", "eval")
 
     rounds_of, even_of, least_of, each_of, parts_of = (formula(t) for t in (r"const int rounds = ([^,;]*),", r"even = ([^,;]*),", r"least = ([^,;]*);", r"const int each = ([^;]*);", r"item_parts = ([^;]*);"))
-    assert "begin = (int)(me / items) * each * WAVES;" in block and "if (begin >= span.steps) return;" in block and "stop = min(span.steps, begin + each * WAVES);" in block
-    for WAVES in (1, 4, 8):
+    assert "begin = (int)part_of_item * each * WAVES;" in block and "if (begin >= span.steps) return;" in block and "stop = min(span.steps, begin + each * WAVES);" in block
+    for WAVES, long_ in [(w, n) for w in (1, 4, 8) for n in longs]:
         for fill in range(5):
             for split in range(fill, 5):
                 for steps in list(range(1, 300)) + [1000, 1023, 1024, 1025, 65536]:
