@@ -34,9 +34,9 @@
 //
 // The same loop serves calls that read other tokens than a sequence's own from its start (attn_kv4_part_kernel, MODE below): those that a group
 // of sequences shares, once for all of its rows or by each sequence, those behind them, and the pages of a list.  Measured (device time): 4 samples of 500 shared
-// tokens, 32 heads 9.3 us; 8 users of 2000, 4 rows, 32 heads 16.5; 128 users of 8197 shared tokens and 100 to 1500 of their own, one row of 64 over 8 heads 94, of which
-// the shared ones 66 (530 TF/s) and the others 29 (3.5 TB/s); 16 pages of 6000 tokens, 32 heads 8.7; 64 of 2048 pages, 64 over 8 heads 10.5; 64 rows of 16 pages of 256,
-// 64 over 8 heads 48 (5.9 TB/s); 128 rows of 32 pages, 64 over 8 heads of 64 27 (5.8 TB/s).
+// tokens, 32 heads 9.5 us; 8 users of 2000, 4 rows, 32 heads 17; 128 users of 8197 shared tokens and 100 to 1500 of their own, one row of 64 over 8 heads 94, of which
+// the shared ones 67 (530 TF/s) and the others 29 (3.5 TB/s); 16 pages of 6000 tokens, 32 heads 8.7; 64 of 2048 pages, 64 over 8 heads 10.5; 64 rows of 16 pages of 256,
+// 64 over 8 heads 49 (5.7 TB/s); 128 rows of 32 pages, 64 over 8 heads of 64 27 (5.7 TB/s).
 #pragma once
 #include "common.hpp"
 #include "exchange.hpp"
@@ -221,8 +221,8 @@ __device__ __forceinline__ void attn_kv4_work(const Args& p) {
   constexpr int WAVES = W, THREADS = 64 * WAVES, TILES = Form::tiles, STEP = Form::step, RB = Form::rows, OVER = Form::over;
   // (sums that are not joined in this launch cost less: 2048 shared tokens of 1024 rows over 8 heads 39 us for 55)
   constexpr int LEAST = MODE == kAttnWhole || F > 1 ? Form::least : (NB == 4 ? 512 : 256) / STEP;
-  // A workgroup for each part of each item, without a division of the steps: fewer registers (up to three workgroups to a unit), 2 us less before
-  // the first scores, few joins (us: 8 users of 2000 shared tokens 24 -> 18.7, 128 rows of 32 pages 38 -> 27).  An item stays whole up to WHOLE rounds of its wavefronts
+  // A workgroup for each part of each item, without a division of the steps: fewer registers (up to three workgroups to a unit), an earlier
+  // start and few joins (us: 8 users of 2000 shared tokens 24 -> 18.7, 128 rows of 32 pages 38 -> 27).  An item stays whole up to WHOLE rounds of its wavefronts
   // (joins cost more: 4 sequences of 32 heads, 573 tokens 9.2 us for 11.5, 1085 tokens 13.8 for 12.7), has 2^fill parts from there on, and more where these would be longer than LONG: a
   // long one among short ones holds the launch up.
   constexpr bool FIXED = MODE == kAttnPages || MODE == kAttnOwn;

@@ -47,7 +47,7 @@ __device__ inline TouchedPage touched_page(const KvShape& kv, int b, int i) {
 
 // grid (B * touched, Hkv): a workgroup takes a page of a head.  A row of D/8 lanes reads a key, a code word a lane, 256 / (D/8) keys at
 // a time; the folds over them stay in registers until the end.  The bounds are worked out anew from the page's codes, not carried on from what stands there:
-// what a rejected draft left must go, and a page is 4 KB.  Bound by launch and latency (one page of 32 heads 1.5 us; 34 pages of 32 heads 5.4).
+// what a rejected draft left must go, and a page is 4 KB.  Bound by launch and latency (one page of 32 heads 3.2 us; 34 pages of 32 heads 5.6).
 template <int D>
 __global__ __launch_bounds__(256) void kv4_bounds_kernel(BoundsArgs p) {
   constexpr int LANES = D / 8, PER = 256 / LANES;
@@ -126,7 +126,7 @@ struct BoundsReadArgs {
   int touched;
 };
 
-// grid (B * touched, parts of Hkv D / 4): four features a thread, code * grid (34 pages of 32 heads 2.7 us: a launch)
+// grid (B * touched, parts of Hkv D / 4): four features a thread, code * grid (34 pages of 32 heads 1.8 us: a launch)
 template <int D>
 __global__ __launch_bounds__(256) void kv4_bounds_read_kernel(BoundsReadArgs p) {
   const int i = blockIdx.y * 256 + threadIdx.x, head = i / (D / 4), d = i & (D / 4 - 1);
@@ -200,8 +200,8 @@ constexpr int kScoreColumns = 4;                       // blocks of 16 columns o
 // power of two of columns (repeating the last one), so their largest score is a fold in a row of lanes; more than 16 take several
 // blocks.  The queries' codes are worked out once a workgroup and shared through LDS.  A wavefront runs through its pages 16 at a time, the next ones'
 // bounds on their way; the heads of a sequence follow each other on one XCD, whose L2 then has the lines that they share (512 pages of 32 sequences and 8 heads: 12
-// us for 16).  Bound by latency (position, table, bounds one after the other: 2048 pages of 8 heads 3.8 us), then by the loads of 260 bytes that lie 2 KB
-// apart (34 MB in 12 us).  Runs of 64 pages with all their loads at once were slower (14): fewer wavefronts fit.
+// us for 16).  Bound by latency (position, table, bounds one after the other: 2048 pages of 8 heads 3.7 us), then by the loads of 260 bytes that lie 2 KB
+// apart (128 queries of up to 512 pages: 21 MB in 10.4 us).  Runs of 64 pages with all their loads at once were slower (14): fewer wavefronts fit.
 // Lane (row, k): row = lane & 15, 16 codes from 16 (lane >> 4) on in each 64.
 template <int D>
 __global__ __launch_bounds__(256) void kv4_score_kernel(SelectArgs p) {
@@ -391,7 +391,7 @@ __device__ inline void find_part(const uint32_t* bins, uint32_t* waves, uint32_t
 // grid (B * T * Hkv), up to THREADS * KEYS pages: one row's `count` best pages, in their order.  A thread's keys stay in its registers, key k that of
 // page THREADS k + thread.  One histogram over their range leaves few keys beside the one looked for, as a rule; these are ranked by comparing each with all.
 // What is taken is written by its rank among the taken: their number in front of each set of 64 pages, and the lanes in front.
-// Bound by the chain of steps and barriers (8 rows of 2048 pages 4.0 us, 1024 rows of up to 512 4.8).
+// Bound by the chain of steps and barriers (8 rows of 2048 pages 3.8 us, 1024 rows of up to 512 4.5).
 template <int THREADS, int KEYS>
 __global__ __launch_bounds__(THREADS) void kv4_choose_kernel(SelectArgs p) {
   constexpr int WAVES = THREADS / 64;

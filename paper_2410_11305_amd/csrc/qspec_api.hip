@@ -937,7 +937,7 @@ double attn_token_ps(AttnPlan plan, int D) {
 }
 // From how many shared tokens on they are read once for all of a group, in a launch of its own: what that saves passes what the second launch and its joins
 // cost (8 us and 20 ns an item).  Measured, each sequence reading them for itself and one reading for all (us): 4 samples of 500 tokens, 32 heads 9.3 and 15.7; 8 users of 2000, 4 rows, 32 heads
-// 18.6 and 23.3; 16 prompts of 1500 to 6000 by 8 samples, 4 rows, 64 over 8 heads of 64 108 and 112; 128 users, one row of 64 over 8 heads: of 2048 tokens 40 and 47,
+// 18.6 (17 with eight wavefronts to an item) and 23.3; 16 prompts of 1500 to 6000 by 8 samples, 4 rows, 64 over 8 heads of 64 108 and 112; 128 users, one row of 64 over 8 heads: of 2048 tokens 40 and 47,
 // of 4000 66 and 60, of 8197 133 and 93.
 int least_shared(const AttnArgs& first, AttnPlan first_plan, const AttnArgs& own, AttnPlan own_plan, int D) {
   const double alone = (double)own.B * own.blocks * attn_token_ps(own_plan, D), together = (double)first.B * first.blocks * attn_token_ps(first_plan, D);
