@@ -4,6 +4,7 @@
 #include "qspec.h"
 
 #include <hip/hip_runtime.h>
+#include <limits.h>
 #include <stdio.h>
 #include <stdlib.h>
 #include <string.h>
@@ -129,7 +130,12 @@ struct PlanOverrides {
 bool apply_override(PlanOverrides& o, const char* name, const char* value) {
   if (strcmp(name, "QSPEC_KERNEL") == 0) { o.generic = value && strcmp(value, "generic") == 0; return true; }
   if (strcmp(name, "QSPEC_MLP_SPIN") == 0) { o.mlp_spin = value ? (unsigned)strtoul(value, nullptr, 10) : 0u; return true; }
-  if (strcmp(name, "QSPEC_ATTN_SHARED") == 0) { o.attn_shared = value ? atoi(value) : -1; return true; }
+  if (strcmp(name, "QSPEC_ATTN_SHARED") == 0) {        // (0 is a value of its own here, so what is no number must not become one)
+    char* end = nullptr;
+    const long long v = value && *value >= '0' && *value <= '9' ? strtoll(value, &end, 10) : -1;
+    o.attn_shared = end && *end == '\0' && v <= INT_MAX ? (int)v : -1;
+    return true;
+  }
   for (int w4a4 = 0; w4a4 < 2; ++w4a4) {
     if (strcmp(name, w4a4 ? "QSPEC_STREAM_W4A4" : "QSPEC_STREAM_W4A16") == 0) {
       int* f = o.stream[w4a4];
