@@ -455,7 +455,7 @@ int qspec_kv4_bounds_read(const void* bounds, const int32_t* pos, const int32_t*
  * +-127: whole numbers but for powers of two, so the choice is exact.  The lower page among equals.  A page whose grid is NaN comes
  * before all others, a page that is not there after them; a row with a NaN or an infinity has zeros for c.
  *   pages  out, int32 [B, T, Hkv, count], below 2 GiB: `count` of them in ascending order, -1 behind the last where n < count.
- *   first, last >= 0, first + last <= count;  max_pages <= 2^24;
+ *   first, last >= 0, first + last <= count;  max_pages <= 2^24;  B * T * Hkv <= 2^24 - 8;
  *   workspace  qspec_kv4_select_workspace_bytes(...) bytes of scratch, 16-byte aligned, nothing to clear.
  */
 size_t qspec_kv4_select_workspace_bytes(int B, int T, int Hq, int Hkv, int max_pages);

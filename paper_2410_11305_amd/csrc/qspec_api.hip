@@ -961,7 +961,7 @@ inline bool page_is_block(int page_size) { return page_size >= kBlockTokens; }
 
 int check_select(int B, int T, int Hq, int Hkv, int max_pages) {
   if (B < 1 || T < 1 || T > (1 << 20) || Hkv < 1 || Hq < Hkv || Hq % Hkv != 0 || Hq / Hkv > 255 || max_pages < 1 || max_pages > (1 << 24)) return QSPEC_ERR_SHAPE;
-  if ((long long)B * T * Hkv > 0x7fffffffLL) return QSPEC_ERR_SHAPE;
+  if ((long long)B * T * Hkv > (1 << 24) - 8) return QSPEC_ERR_SHAPE;        // (rows in eights, 256 threads each: below 2^32)
   return QSPEC_OK;
 }
 
