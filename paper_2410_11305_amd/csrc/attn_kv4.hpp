@@ -44,7 +44,10 @@
 
 namespace qspec {
 
-constexpr size_t kAttnTicketBytes = 16384;   // arrival counters at the head of the workspace, two a workgroup
+// Arrival counters at the head of the workspace: two a workgroup where the work is divided on the device, otherwise one for each part that an item may
+// have, of which the item's first counts.
+constexpr size_t kAttnTicketBytes = 16384;
+constexpr int kAttnCounters = (int)(kAttnTicketBytes / sizeof(unsigned));
 constexpr int kAttnRounds = 8;               // rounds of whole items (more have little left to gain: one part of many)
 // The shape of an instance.  NB: blocks of 16 columns a wavefront carries; F: token tiles that share a block (below).
 // Two workgroups of four wavefronts to a compute unit: the loop is free of spills (a reload inside it waits for every load
@@ -54,7 +57,8 @@ constexpr int kAttnRounds = 8;               // rounds of whole items (more have
 template <int NB, int F>
 struct AttnForm {
   static constexpr int waves = 4;
-  static constexpr int workgroups = 512;                           // of a launch; two parts of an item each in the workspace at most
+  static constexpr int workgroups = 512;                           // of a launch that divides its work on the device
+  static constexpr int places = 2 * workgroups;                    // of parts of items in a workspace: two for each of them at most
   static constexpr int tiles = F > 1 ? 4 : 2;                      // 16-token tiles of a step (8 at F = 4: 27 us for 22 at 8 x 2048 tokens)
   static constexpr int step = 16 * tiles;                          // tokens of a step
   static constexpr int rows = 16 * NB / F;                         // rows of a block of an item
@@ -64,7 +68,7 @@ struct AttnForm {
   static constexpr int whole = 1024 / step;
   static constexpr int least = (NB == 1 ? 512 : NB == 2 ? 640 : 1280) / step;
   static_assert(over >= 2 * waves && least >= 2 * waves, "no workgroup's share rounds down to nothing");
-  static_assert(2 * workgroups * sizeof(unsigned) <= kAttnTicketBytes, "two counters for every workgroup");
+  static_assert(2 * workgroups <= kAttnCounters && 2 * workgroups <= places, "two counters and two places for every workgroup");
 };
 
 struct AttnArgs {
@@ -206,7 +210,7 @@ __host__ __device__ constexpr int attn_part_floats(int D) { return D + 4; }
 template <int D, int NB, int F>
 constexpr size_t attn_workspace() {
   typedef AttnForm<NB, F> Form;
-  return kAttnTicketBytes + (size_t)2 * Form::workgroups * Form::rows * attn_part_floats(D) * sizeof(float);
+  return kAttnTicketBytes + (size_t)Form::places * Form::rows * attn_part_floats(D) * sizeof(float);
 }
 
 // D features a head, NB blocks of 16 columns, F tiles of tokens to a block.

@@ -919,8 +919,32 @@ bool attn_counts(const AttnArgs& a, long long tokens) { return (long long)a.B * 
 // (the bounds of the scale keep every score inside binary32, and off the reference of a row that has seen nothing)
 inline bool scale_fits(float scale) { return scale >= 1e-10f && scale <= 1e10f; }
 
-// Parts of items that a call has places and counters for.
-inline long long attn_most_parts(AttnPlan plan) { return plan.nb == 4 ? 2048 : 4096; }
+// Parts of items, a workgroup to each, that qspec_attn_kv4_shared has counters and places for: the places of so many workspaces of qspec_attn_kv4 (those of
+// the largest instance have sixteen times the rows).  qspec_attn_kv4_blocks has one.
+constexpr int attn_part_sets(AttnPlan plan) { return plan.nb == 4 ? 2 : 4; }
+constexpr long long attn_most_parts(AttnPlan plan) { return (long long)attn_part_sets(plan) * AttnForm<1, 1>::places; }
+constexpr long long kFillParts = 256;        // a part to every compute unit
+static_assert(attn_most_parts({1, 4}) <= kAttnCounters && attn_most_parts({4, 1}) <= kAttnCounters, "a counter for every part");
+static_assert(kFillParts <= AttnForm<1, 1>::places && kFillParts <= attn_most_parts({4, 1}), "places and counters for the parts that fill the card");
+
+// Parts of an item, as their base-2 logarithm: ordinarily, and at most.
+struct AttnParts { int fill, split; };
+// Of a call with so many items of rows of up to `tokens`.  A part to every compute unit; long rows may leave one sequence with most of the work, so its items
+// are divided further (us, 30000 tokens beside 15 sequences of 1300, one row of 64 over 8 heads: 34, 100 without, 21 as the device divides the work of
+// qspec_attn_kv4; beside 127 of them 82, 102 and 54).
+AttnParts own_parts(long long items, long long tokens, AttnPlan plan) {
+  AttnParts p{0, 0};
+  while (p.fill < 4 && items << (p.fill + 1) <= kFillParts) ++p.fill;
+  p.split = p.fill;
+  while (p.split < 4 && items << (p.split + 1) <= attn_most_parts(plan) && tokens >> p.split > (p.split == p.fill ? 4096 : 2048)) ++p.split;
+  return p;
+}
+// Of lists, of so many steps: a step to a wavefront of a part at least.
+AttnParts list_parts(long long items, int steps) {
+  int split = 0;
+  while (split < 4 && items << (split + 1) <= kFillParts && steps >> (split + 1) >= 4) ++split;
+  return AttnParts{split, split};
+}
 // A call's workspace: what the second launch has for itself, then the first one's partial sums, their directory, and those that are whole.
 struct SharedWorkspace { size_t parts, items, joint, bytes; };
 SharedWorkspace attn_shared_workspace(int B, int T, int Hq, int Hkv, int D, int groups) {
@@ -930,7 +954,7 @@ SharedWorkspace attn_shared_workspace(int B, int T, int Hq, int Hkv, int D, int 
   const size_t items = (size_t)groups * (((size_t)rows * G + block - 1) / block) * Hkv;
   const auto up = [](size_t n) { return (n + 255) & ~(size_t)255; };
   SharedWorkspace w;
-  w.parts = up(attn_workspace_bytes(T, G, D) * (attn_plan(T, G).nb == 4 ? 2 : 4));        // (places for attn_most_parts)
+  w.parts = up(attn_workspace_bytes(T, G, D) * attn_part_sets(attn_plan(T, G)));        // (places for attn_most_parts)
   w.items = w.parts + up(attn_workspace_bytes(rows, G, D) - kAttnTicketBytes);
   w.joint = w.items + up(items * sizeof(int2));
   w.bytes = w.joint + (size_t)B * T * Hq * attn_part_floats(D) * sizeof(float);
@@ -1433,17 +1457,15 @@ int qspec_attn_kv4_shared(const void* q_f16, const void* cache, const int32_t* p
   first.least_shared = overrides().attn_shared >= 0 ? overrides().attn_shared : least_shared(first, plan, rest, rest_plan, D);
   const bool once = first.least_shared < tokens;         // (where no group can share so many, there is nothing to launch)
   rest.least_shared = once ? first.least_shared : 0x7fffffff;
-  // A part of an item to every compute unit.  Long rows may leave one sequence with most of the work: its items are divided further (us, 30000 tokens beside 15
-  // sequences of 1300, one row of 64 over 8 heads: 34, 100 without, 21 as the device divides the work of qspec_attn_kv4; beside 127 of them 82, 102 and 54).
   const long long items = (long long)B * rest.blocks * Hkv;
-  while (rest.fill < 4 && items << (rest.fill + 1) <= 256) ++rest.fill;
-  rest.split = rest.fill;
-  while (rest.split < 4 && items << (rest.split + 1) <= attn_most_parts(rest_plan) && tokens >> rest.split > (rest.split == rest.fill ? 4096 : 2048)) ++rest.split;
+  const AttnParts parts = own_parts(items, tokens, rest_plan);
+  rest.fill = parts.fill;
+  rest.split = parts.split;
   const unsigned workgroups = (unsigned)(items << rest.split);
   if (once && D == 128) launch_attn_part<128, kAttnPrefix>(first, plan, s);
   else if (once) launch_attn_part<64, kAttnPrefix>(first, plan, s);
   // a whole item to a compute unit: eight wavefronts (us, 256 items of 2300 tokens 16.4 for 18.8, of 4000 tokens 21.3 for 25.4)
-  if (rest.fill == 0 && items <= 256 && rest_plan.nb < 4) {
+  if (rest.fill == 0 && items <= kFillParts && rest_plan.nb < 4) {
     if (D == 128) launch_attn_waves<128, kAttnOwn, 8>(rest, rest_plan, s, workgroups);
     else launch_attn_waves<64, kAttnOwn, 8>(rest, rest_plan, s, workgroups);
   } else if (D == 128) launch_attn_part<128, kAttnOwn>(rest, rest_plan, s, workgroups);
@@ -1475,12 +1497,11 @@ int qspec_attn_kv4_blocks(const void* q_f16, const void* cache, const int32_t* p
   // 128 rows of 8 heads and 32 pages: 33 for 28).  Four to a workgroup otherwise, which share the items out among the compute units, a step
   // to a wavefront at least (64 items of 32 pages: 11 in 256 workgroups, 15 in 512).
   const bool single = plan.nb < 4 && (items >= 2048 || (items >= 1024 && steps <= 8));
-  int split = 0;
-  while (!single && split < 4 && items << (split + 1) <= 256 && steps >> (split + 1) >= 4) ++split;
-  const AttnPartArgs a{common, T, 1, nullptr, 0, nullptr, nullptr, nullptr, 0, 0, pages, count, split, split};
+  const AttnParts parts = single ? AttnParts{0, 0} : list_parts(items, steps);
+  const AttnPartArgs a{common, T, 1, nullptr, 0, nullptr, nullptr, nullptr, 0, 0, pages, count, parts.fill, parts.split};
   if (int st = check_device()) return st;
   const hipStream_t s = static_cast<hipStream_t>(stream);
-  const unsigned workgroups = (unsigned)(items << split);
+  const unsigned workgroups = (unsigned)(items << parts.split);
   if (single && D == 128) launch_attn_waves<128, kAttnPages, 1>(a, plan, s, workgroups);
   else if (single) launch_attn_waves<64, kAttnPages, 1>(a, plan, s, workgroups);
   else if (D == 128) launch_attn_part<128, kAttnPages>(a, plan, s, workgroups);
