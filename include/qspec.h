@@ -417,6 +417,8 @@ int qspec_attn_kv4(const void* q_f16, const void* cache, const int32_t* pos, con
  *   Where a group shares so little that one reading for all would save less than it costs, its sequences read the shared tokens for themselves; where the
  *   table's rows (max_pages * page_size tokens) are too short for anything else, that is one launch.  Otherwise there are two, with partial sums of the shared
  *   tokens in binary32 between them.
+ *   The items of a call (a sequence, block of rows and key/value head each) are divided alike, into 16 parts at most.  Where one sequence is many times longer than
+ *   the others, or few sequences of few key/value heads have long contexts of their own, qspec_attn_kv4 with the same table is faster, by up to three times.
  *   workspace  qspec_attn_kv4_shared_workspace_bytes(...) bytes; the workspace rule at qspec_workspace_bytes holds.
  */
 size_t qspec_attn_kv4_shared_workspace_bytes(int B, int T, int Hq, int Hkv, int D, int groups);
@@ -467,7 +469,8 @@ int qspec_kv4_select(const void* q_f16, const void* bounds, const int32_t* pos, 
  * Attention over chosen pages: row j of sequence b and its heads of key/value head h see the tokens t <= pos[b] + j of the pages that
  * pages[b][j][h] names, and no others.  A list is read from its start, min(count, n) entries of it (n as above); an entry that
  * is negative, not larger than the one before it, or at or past max_pages is left out, so ascending lists with -1 at their end, as qspec_kv4_select
- * writes them, are taken whole.  A row that sees nothing gets zeros.
+ * writes them, are taken whole.  (A list out of order that names a page again behind a smaller entry, 5 3 5, has its tokens count again.)  A row that
+ * sees nothing gets zeros.
  *   pages  int32 [B, T, Hkv, count], count >= 1, below 2 GiB;
  *   B * T * Hkv * blocks * (min(count, max_pages) * page_size / 32 + 64) < 2^31, blocks of 4, 8, 16, 32 or 64 of the Hq / Hkv heads as in qspec_attn_kv4,
  *   with which everything else, the values of NaN and the limits of scale and scores, agrees;

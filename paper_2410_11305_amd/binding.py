@@ -600,7 +600,8 @@ def attn_kv4_shared(q: torch.Tensor, cache: torch.Tensor, pos: torch.Tensor, sha
                     page_table: torch.Tensor = None, scale: float = None, out: torch.Tensor = None,
                     workspace: torch.Tensor = None) -> torch.Tensor:
     """attn_kv4 for sequences that share beginnings: shared int32 [groups], the B sequences being that many sets of neighbours; the
-    first shared[g] tokens of a set are read once, through the page table's row of its first sequence.  Hot loops pass out and a workspace."""
+    first shared[g] tokens of a set are read once, through the page table's row of its first sequence.  One sequence many times longer than the others, or few long
+    ones over few key/value heads, are faster with attn_kv4.  Hot loops pass out and a workspace."""
     B, T, Hq, D = q.shape
     groups = shared.shape[0]
     device, c, at, table, Bp, max_pages, n_pages = _kv4(cache, pos, page_table, Hkv, D, page_size, "qspec_attn_kv4_shared")

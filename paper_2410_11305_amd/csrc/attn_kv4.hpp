@@ -36,7 +36,8 @@
 // of sequences shares, once for all of its rows or by each sequence, those behind them, and the pages of a list.  Measured (device time): 4 samples of 500 shared
 // tokens, 32 heads 9.5 us; 8 users of 2000, 4 rows, 32 heads 17; 128 users of 8197 shared tokens and 100 to 1500 of their own, one row of 64 over 8 heads 94, of which
 // the shared ones 67 (530 TF/s) and the others 29 (3.5 TB/s); 16 pages of 6000 tokens, 32 heads 8.7; 64 of 2048 pages, 64 over 8 heads 10.5; 64 rows of 16 pages of 256,
-// 64 over 8 heads 49 (5.7 TB/s); 128 rows of 32 pages, 64 over 8 heads of 64 27 (5.7 TB/s).
+// 64 over 8 heads 49 (280 MB); 128 rows of 32 pages, 64 over 8 heads of 64 27 (153 MB; 5.7 TB/s both, on the same buffers every pass: some of them come from the
+// cache in front of the memory).
 #pragma once
 #include "common.hpp"
 #include "exchange.hpp"

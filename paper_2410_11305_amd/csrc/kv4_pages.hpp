@@ -4,8 +4,9 @@
 // outward to whole numbers of a grid e = 2^n, the smallest with max(|U|, |L|) <= 127 e over the features: 8 bits each.  For
 // every token t of the page,
 //   q . k[t] <= sum_d max(q[d] U[d], q[d] L[d]) = sum_d q+[d] U[d] + q-[d] L[d],     q+ = max(q, 0), q- = min(q, 0)
-// which is a matrix product over 2 D features.  The rows of a query (its G heads that share a key/value head) are rounded to 8 bits on one
-// grid of their own, the same for all pages, so it does not matter for the choice.
+// which is a matrix product over 2 D features.  The rows of a query (its G heads that share a key/value head) are rounded to 8 bits, to nearest, on one
+// grid of their own; the grid is the same for all pages, so its size does not matter for the choice.  The rounding does: a score can lie below what the
+// unrounded query bounds, and of 32 pages of 512 (random keys of 128 features, one or eight heads) 98 to 99 % are those that unrounded queries choose.
 //
 // Everything that decides is a whole number times a power of two: the sums are below 2^21 and exact in any order, and so is their
 // product with the grid in binary32.  Pages with equal scores are taken in their order.

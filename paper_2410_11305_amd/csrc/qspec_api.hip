@@ -1574,8 +1574,15 @@ int qspec_kv4_select(const void* q_f16, const void* bounds, const int32_t* pos, 
   const dim3 grid((unsigned)((rows + 7) / 8 * 8), chunks < 65535u ? chunks : 65535u);
   if (D == 128) launch_kernel(kv4_score_kernel<128>, grid, dim3(256), lds, s, a);
   else launch_kernel(kv4_score_kernel<64>, grid, dim3(256), lds, s, a);
-  // Sixteen wavefronts to a row where every row has a compute unit (us of the whole call, 8 rows of 2048 pages 10.0 for 11.6), four where they share them
-  // (1024 rows of 512 pages: 22 for 25), and no more keys to a thread than there can be (the same: 17.5 for 19.7).
+  // Sixteen wavefronts to a row where every row has a compute unit, four where they share them or have little to do, and no more keys to a thread than there
+  // can be.  The whole call in us, <256, 2>, <256, 8>, <1024, 2>, <1024, 8>, <256, 32> and the one for any number:
+  //   rows    pages                            rows    pages                           rows    pages
+  //      8      500  8.8  10  9.1  12  20 10     256      500  11  13  12  15  23  13    1024      500  18  20  23  37  35  20
+  //      8     2048   -   11  9.7  12  21 15     256     2048   -  20  18  21  30  25    1024     2048   -  43  46  60  57  48
+  //      8     4096   -    -   -   14  24 21     256     4096   -   -   -  29  39  39    1024     4096   -   -   -  88  87  87
+  //      8     8192   -    -   -   16  27 47     256     8192   -   -   -  43  53  74    1024     8192   -   -   - 141 139 208
+  // Past them one row of 8 heads takes 62 (12000 pages) to 110 (20000).  (Scores of many magnitudes, or of both signs, crowd into few parts of the histogram:
+  // 8 rows of 2048 pages 20.)
   const int lists = B * T * Hkv;
   const dim3 each((unsigned)lists);
   if (max_pages <= 512) launch_kernel((kv4_choose_kernel<256, 2>), each, dim3(256), 0, s, a);
